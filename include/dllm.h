@@ -417,6 +417,99 @@ dllm_status dllm_attention_noalloc(const void* d_q, const void* d_k, const void*
 dllm_status dllm_vverify_select(const void* d_vnew, void* d_vcache, float* d_sim, int32_t* d_idx, int B, int R,
                                 int width, int k, int dtype, void* stream);
 
+/* ---- weights and rows in 8-bit integers --------------------------------------
+ * (No counterpart in the paper.)  A step of few rows is bound by streaming the
+ * projections' weights; in 8-bit integers they are half as many bytes, and the
+ * tensor cores take them at twice the rate.  None of these calls allocates, and
+ * all run on the current device. */
+/* Rows of `dtype` (DLLM_FP32 / DLLM_BF16) to 8-bit integers, one scale per row:
+ * scale = max |x| / 127, q = rint(x / scale) (fp32, ties to even), within
+ * +-127.  A row of zeros gets scale 0 and codes 0; one that holds an infinity or
+ * a NaN gets codes 0 and that for a scale, so that its products are NaN.  ldx:
+ * elements between rows of x (>= cols); ldq: bytes between rows of q (>= cols, a
+ * multiple of 16; the bytes between cols and ldq stay as they are).  Serves
+ * weights (a row per output channel) and activations (a row per token) alike. */
+dllm_status dllm_quantize_rows_s8(const void* d_x, size_t ldx, int dtype, void* d_q, size_t ldq, float* d_scale,
+                                  int rows, int cols, void* stream);
+/* C[m, n] = (sum_k A[m, k] W[n, k]) * d_sa[m] * d_sw[n], exact 32-bit integer sums,
+ * scaled in fp32 in that order and rounded once to out_dtype (DLLM_FP32 /
+ * DLLM_BF16); C [M, N] contiguous.  lda / ldw: bytes between rows, multiples of
+ * 16; A and W 16-byte aligned; any M, N and K from 1, K < 131072 (so that the
+ * sums fit).  d_scratch: dllm_gemm_s8_scratch_bytes() on the device that is
+ * current (NULL where that is 0), 16-byte aligned; calls that may overlap on the
+ * GPU need one each. */
+size_t dllm_gemm_s8_scratch_bytes(int M, int N, int K);
+dllm_status dllm_gemm_s8(const void* d_A, size_t lda, const float* d_sa, const void* d_W, size_t ldw,
+                         const float* d_sw, void* d_C, int out_dtype, int M, int N, int K, void* d_scratch,
+                         size_t scratch_bytes, void* stream);
+/* Both in one call: y = x W^T with the rows of x (M of K elements, ldx apart)
+ * brought to 8-bit integers first.  The product's weights are requested while
+ * the rows are still being converted. */
+size_t dllm_linear_s8_scratch_bytes(int M, int N, int K);
+dllm_status dllm_linear_s8(const void* d_x, size_t ldx, int dtype, const void* d_W, size_t ldw, const float* d_sw,
+                           void* d_y, int out_dtype, int M, int N, int K, void* d_scratch, size_t scratch_bytes,
+                           void* stream);
+
+/* ---- a K / V cache held in 4 bits -----------------------------------------------
+ * (The memory overhead for long sequences that Sec. A.10 item (1) names: 0.27 of
+ * the bf16 cache.)  A head's K or V of one token, hd numbers, is hd / 2 bytes of
+ * codes (element 2i in the low half of byte i, 2i + 1 in the high half) and a pair
+ * (step, lo) of bf16; code u stands for lo + step * u.  Rows of one (sequence, KV
+ * head) are contiguous. */
+typedef struct {
+  void* d_k_codes;   /* [B, n_kv_heads, capacity, head_dim / 2] bytes, 16-byte aligned */
+  void* d_k_params;  /* [B, n_kv_heads, capacity, 2] bf16 (step, lo), 16-byte aligned */
+  void* d_v_codes;
+  void* d_v_params;
+  int32_t B, n_kv_heads, capacity, head_dim; /* capacity a multiple of 64, head_dim 64 or 128 */
+} dllm_kv4_cache;
+/* Rows of K and V into the cache.  d_k, d_v: B * a rows of n_kv_heads * head_dim
+ * elements of `dtype`, ldk / ldv elements apart (columns of a product for Q, K and V
+ * will do).  Row j of sequence b goes to position d_pos[b * a + j] (DEVICE int32), or
+ * to start + j where d_pos is NULL; rows whose position is not in [0, capacity) are
+ * left out, and of several rows of a sequence with one position the last one is
+ * stored.  lo = bf16(min x), step = bf16((max x - min x) / 15), 1 where that is 0,
+ * code = rint((x - lo) / step) within 0..15, in fp32.  A head's row that holds an
+ * infinity or a NaN (or whose spread has no bf16) is stored as NaN. */
+dllm_status dllm_kv4_store(const dllm_kv4_cache* cache, const void* d_k, size_t ldk, const void* d_v, size_t ldv,
+                           int dtype, int a, const int32_t* d_pos, int start, void* stream);
+/* The first n rows of every sequence as numbers of `dtype`, [B, n, n_kv_heads *
+ * head_dim] (the layout dllm_attention reads); d_k or d_v may be NULL.  Rows from
+ * d_lens[b] on (DEVICE int32 [B], may be NULL) are written as zeros. */
+dllm_status dllm_kv4_load(const dllm_kv4_cache* cache, int n, const int32_t* d_lens, void* d_k, void* d_v, int dtype,
+                          void* stream);
+/* dllm_attention over that cache: a query rows per sequence (bf16, n_heads heads of
+ * head_dim, rows ldq elements apart, 16-byte aligned) against the first
+ * d_lens[b] keys of their sequence (d_lens NULL: n; lengths are taken between 0 and
+ * n).  d_o bf16 [B * a, n_heads * head_dim]; d_lse (may be NULL) float [B * a,
+ * n_heads]: the natural logarithm of each row's sum of exp(q . k / sqrt(head_dim)).
+ * A row without keys gives zeros and -infinity.  Keys from the length on count for
+ * nothing whatever stands there.  The steps and offsets are applied in fp32 outside
+ * the matrix products, which work on the codes themselves. */
+size_t dllm_attention_kv4_scratch_bytes(int B, int a, int n, int n_heads, int n_kv_heads, int head_dim);
+dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, void* d_o, float* d_lse, int a,
+                               int n, int n_heads, const int32_t* d_lens, void* d_scratch, size_t scratch_bytes,
+                               void* stream);
+/* What every key gets of the rows' attention: d_weight[b, h, j] (float [B, n_kv_heads,
+ * capacity]) += the sum over the a queries and the query heads of KV head h of
+ * exp(q . k_j / sqrt(head_dim) - lse), for j below the sequence's length; the other
+ * weights stay as they are.  d_lse as dllm_attention_kv4 leaves it; a row whose lse is
+ * -infinity gives nothing.  Sums are taken in a fixed order. */
+dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, const float* d_lse,
+                                       float* d_weight, int a, int n, int n_heads, const int32_t* d_lens, void* stream);
+/* Keeps, per sequence and KV head, min(length, keep) keys: the first `first` and the
+ * last `last` of them (response rows, say) and, of the others, those with the largest
+ * weights (equal ones: the lowest index; a NaN counts as lowest), in their order; where
+ * the length is at most keep all stay.  Their K, V and weight go to rows 0, 1, .. of
+ * `to` and d_to_weight (float [B, n_kv_heads, to->capacity], zeros behind them),
+ * d_index (int32 [B, n_kv_heads, keep]) says where each came from (-1 behind them) and
+ * d_to_lens (int32 [B]) how many stayed.  first + last <= keep <= to->capacity; `to`
+ * must not overlap `from`.  Positions are in K already (it is cached rotated), so
+ * attention over `to` needs nothing but the new lengths. */
+dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, int n, int keep, int first, int last,
+                           const int32_t* d_lens, const dllm_kv4_cache* to, float* d_to_weight, int32_t* d_index,
+                           int32_t* d_to_lens, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

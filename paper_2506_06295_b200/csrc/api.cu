@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/dllm.h"
+#include "gemm_s8.cuh"
 #include "internal.h"
 #include "tma.cuh"
 
@@ -1354,6 +1355,7 @@ dllm_status dllm_debug_set_wait_limit_ns(uint64_t ns) {
   CU_TRY(nullptr, set_wait_limit_gemm_rows(ns));
   CU_TRY(nullptr, set_wait_limit_attention(ns));
   CU_TRY(nullptr, set_wait_limit_attention_umma(ns));
+  CU_TRY(nullptr, set_wait_limit_gemm_s8(ns));
   CU_TRY(nullptr, cudaDeviceSynchronize());
   return DLLM_OK;
 }

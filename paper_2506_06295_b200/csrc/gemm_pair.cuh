@@ -66,6 +66,16 @@ __device__ __forceinline__ bool group_all(int bar, bool v) { return bar == 1 ? g
 // SwiGLU, two rounds, 3.1 / 27.8-51.6 / 31.5-55.2; down in four 1.9 / 19.8 / 22.8.)
 template <typename FORM>
 constexpr int PAIR_THREADS = 64 + 128 * FORM::GROUPS;
+// The operands' type goes with the form: elements per stage (128 bytes of each row), instruction descriptor, MMA of 32
+// bytes of k.  bf16 unless a form's specialisation says otherwise.
+template <typename FORM>
+struct PairOperands {
+  static constexpr int STAGE_K = TILE_K;
+  static __host__ __device__ constexpr uint32_t idesc(int m, int n) { return make_idesc(m, n); }
+  static __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    umma_bf16_pair(d, a, b, idesc, accumulate);
+  }
+};
 template <int BN, typename FORM>
 struct PairLayout {
   static constexpr uint32_t A_HALF_BYTES = (BN / 2) * TILE_K * 2;
@@ -102,6 +112,7 @@ __global__ void __launch_bounds__(PAIR_THREADS<FORM>, 2)
                           int m_tiles, int n_pairs, int units, int STAGES, const __grid_constant__ FORM form,
                           int* __restrict__ status) {
   using PL = PairLayout<BN, FORM>;
+  using OP = PairOperands<FORM>;
   // column distance of the two accumulators: an allocation is a power of two, so 192-row tiles sit 256 apart
   constexpr uint32_t ACC = BN > 128 ? 256 : BN > 64 ? 128 : BN > 32 ? 64 : 32;
   extern __shared__ uint8_t smem_raw[];
@@ -159,7 +170,7 @@ __global__ void __launch_bounds__(PAIR_THREADS<FORM>, 2)
       for (int i = 0; i < pre; ++i) {
         if (leader) mbar_expect_tx(smem_u32(&full_bar[i]), 2 * PL::STAGE_BYTES);
         tma_load_2d_pair_weights<ONCE>(tiles_s + i * PL::STAGE_BYTES, &tmW, cluster_addr(smem_u32(&full_bar[i]), 0),
-                              (kb0 + i) * TILE_K, (2 * np + rank) * TILE_W);
+                              (kb0 + i) * OP::STAGE_K, (2 * np + rank) * TILE_W);
       }
     __syncwarp();
   }
@@ -187,9 +198,9 @@ __global__ void __launch_bounds__(PAIR_THREADS<FORM>, 2)
           const uint32_t dst = tiles_s + s * PL::STAGE_BYTES;
           if (issued >= pre) {
             if (leader) mbar_expect_tx(smem_u32(&full_bar[s]), 2 * PL::STAGE_BYTES);
-            tma_load_2d_pair_weights<ONCE>(dst, &tmW, fb, kb * TILE_K, n0);
+            tma_load_2d_pair_weights<ONCE>(dst, &tmW, fb, kb * OP::STAGE_K, n0);
           }
-          tma_load_2d_pair(dst + W_STAGE_BYTES, &tmA, fb, kb * TILE_K, m0);
+          tma_load_2d_pair(dst + W_STAGE_BYTES, &tmA, fb, kb * OP::STAGE_K, m0);
         }
         __syncwarp();
         if (++s == STAGES) {
@@ -201,7 +212,7 @@ __global__ void __launch_bounds__(PAIR_THREADS<FORM>, 2)
   } else if (warp == 1) {
     // ---------------- MMA issuer (first CTA of the pair) ----------------
     if (leader) {
-      constexpr uint32_t idesc = make_idesc(2 * TILE_W, BN);
+      constexpr uint32_t idesc = OP::idesc(2 * TILE_W, BN);
       int s = 0, j = 0;
       uint32_t ph = 0;
       bool ready = false;
@@ -233,8 +244,8 @@ __global__ void __launch_bounds__(PAIR_THREADS<FORM>, 2)
             const uint64_t dA = make_smem_desc(sW + W_STAGE_BYTES);
 #pragma unroll
             for (int k = 0; k < TILE_K / UMMA_K; ++k)
-              umma_bf16_pair(tmem_d + (uint32_t)a * ACC, dW + (uint64_t)(2 * k), dA + (uint64_t)(2 * k), idesc,
-                             (kb > kb0 || k > 0) ? 1u : 0u);
+              OP::mma(tmem_d + (uint32_t)a * ACC, dW + (uint64_t)(2 * k), dA + (uint64_t)(2 * k), idesc,
+                      (kb > kb0 || k > 0) ? 1u : 0u);
             umma_commit_pair(empty);  // both CTAs may refill the stage once these MMAs have read it
             if (kb == kb1 - 1) umma_commit_pair(smem_u32(&acc_full[a]));
           }

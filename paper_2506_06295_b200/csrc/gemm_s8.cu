@@ -1,0 +1,437 @@
+// Products of 8-bit integers:  C[M, N] = (A W^T)[m, n] * sA[m] * sW[n],  A [M, K] rows (tokens), W [N, K] output channels.
+//
+// The sums are exact 32-bit integers, so neither tile nor split changes a result; a product is scaled by its row's and its
+// column's scale in fp32 and rounded once to the output's type.  A product of few rows is bound by streaming W, half the
+// bytes of bf16; one of many rows by the tensor cores at twice the bf16 rate.
+//
+// Layout, ring and roles are those of the bf16 products (gemm_tcgen05.cu): a stage holds 128 bytes of k of each row, which
+// are 128 integers instead of 64 bf16, and one tcgen05.mma (kind::i8) takes 32 of them, so bytes, cycles and addresses per
+// stage are the same and only the number of stages halves.  Up to 128 rows one CTA per 128 weight rows with the k range
+// split until the chip streams; above that the persistent CTA pairs of gemm_pair.cuh.
+#include "../../include/dllm.h"
+#include "gemm_s8.cuh"
+#include "tma.cuh"
+#include "umma.cuh"
+#include "gemm_pair.cuh"
+
+namespace dllm {
+
+namespace {
+
+constexpr int S8_K = 128;    // integers of k per stage: one 128-byte swizzle row
+
+// W columns (rows of A) of a finished tile, TMEM lane = weight row: 128 threads, tl = 0..127 = lane.  split: the integers go
+// to the slab, for the sum over the slabs.
+template <int W, typename T>
+__device__ __forceinline__ void s8_epilogue(uint32_t tmem_d, int tl, int m0, int n0, int M, int N, const float* __restrict__ sa,
+                                            const float* __restrict__ sw, T* __restrict__ out, int* __restrict__ slab) {
+  const uint32_t tmem_w = tmem_d + ((uint32_t)(tl >> 5) << 21);
+  const int n = n0 + tl;
+  const float w = n < N ? sw[n] : 0.f;
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+  for (int c0 = 0; c0 < W; c0 += 16) {
+    if (m0 + c0 >= M) break;  // uniform across the warp
+    uint32_t r[16];
+    tmem_ld16(tmem_w + (uint32_t)c0, r);
+    tmem_ld16_wait(r);
+    if (n < N) {
+      const size_t first = (size_t)(m0 + c0) * N + n;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (m0 + c0 + j >= M) continue;
+        if (slab)
+          slab[first + (size_t)j * N] = (int)r[j];
+        else
+          out[first + (size_t)j * N] = from_f32<T>(__int2float_rn((int)r[j]) * sa[m0 + c0 + j] * w);
+      }
+    }
+  }
+}
+
+template <int BN>
+struct S8Layout {
+  static constexpr uint32_t STAGE_BYTES = (TILE_W + BN) * S8_K;
+  static constexpr uint32_t total(int stages) { return (uint32_t)stages * STAGE_BYTES + 1024; }
+  static constexpr int most() {
+    const int fit = (227 * 1024 - 1024 - 256) / (int)STAGE_BYTES;
+    return fit < MAX_STAGES ? fit : MAX_STAGES;
+  }
+};
+
+// One CTA: 128 weight rows x BN rows of A x a k range (blockIdx.z).  Warp 0 requests operands, warp 1 issues the MMAs, all
+// eight drain the accumulator, half of the columns per group of four.
+constexpr int S8_THREADS = 256;
+template <int BN, bool ONCE, typename T>
+__global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_constant__ CUtensorMap tmW,
+                                                             const __grid_constant__ CUtensorMap tmA,
+                                                             const float* __restrict__ sa, const float* __restrict__ sw,
+                                                             T* __restrict__ out, int* __restrict__ slabs, int M, int N,
+                                                             int num_kb, int kb_per_split, int stages, int* __restrict__ status) {
+  using SL = S8Layout<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t full_bar[MAX_STAGES];
+  __shared__ __align__(8) uint64_t empty_bar[MAX_STAGES];
+  __shared__ __align__(8) uint64_t accum_bar;
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int m0 = blockIdx.x * BN, n0 = blockIdx.y * TILE_W;
+  const int kb0 = blockIdx.z * kb_per_split, nkb = min(num_kb, kb0 + kb_per_split) - kb0;   // >= 1 by the plan
+  const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const int pre = min(stages, nkb);  // stages whose weight tile is requested before the dependency wait
+  if (warp == 0) {
+    if (elect_one()) {
+      abort_flag = 0;
+      for (int s = 0; s < stages; ++s) {
+        mbar_init(smem_u32(&full_bar[s]), 1);
+        mbar_init(smem_u32(&empty_bar[s]), 1);
+      }
+      mbar_init(smem_u32(&accum_bar), 1);
+      mbar_fence_init();
+      prefetch_tensormap(&tmW);
+      prefetch_tensormap(&tmA);
+      for (int i = 0; i < pre; ++i) {   // see launch_gemm_s8: no launch this one may overlap writes W
+        const uint32_t fb = smem_u32(&full_bar[i]);
+        mbar_expect_tx(fb, SL::STAGE_BYTES);
+        tma_load_2d_weights<ONCE>(tiles + i * SL::STAGE_BYTES, &tmW, fb, (kb0 + i) * S8_K, n0);
+      }
+    }
+    __syncwarp();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)),
+                 "r"((uint32_t)BN)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_d = tmem_base_slot;
+  volatile int* abortp = &abort_flag;
+  pdl_wait();
+  pdl_trigger();
+
+  if (warp == 0) {
+    int s = 0;
+    uint32_t ph = 0;
+    for (int i = 0; i < nkb; ++i) {
+      const uint32_t fb = smem_u32(&full_bar[s]), dst = tiles + s * SL::STAGE_BYTES;
+      const int kc = (kb0 + i) * S8_K;
+      if (i >= pre && !mbar_wait_warp(smem_u32(&empty_bar[s]), ph ^ 1u, abortp)) {
+        if (status && lane == 0) atomicCAS(status, ST_OK, ST_TIMEOUT_TMA);
+        break;
+      }
+      if (elect_one()) {
+        if (i >= pre) {
+          mbar_expect_tx(fb, SL::STAGE_BYTES);
+          tma_load_2d_weights<ONCE>(dst, &tmW, fb, kc, n0);
+        }
+        tma_load_2d(dst + W_STAGE_BYTES, &tmA, fb, kc, m0);
+      }
+      __syncwarp();
+      if (++s == stages) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+  } else if (warp == 1) {
+    constexpr uint32_t idesc = make_idesc_s8(TILE_W, BN);
+    int s = 0;
+    uint32_t ph = 0;
+    bool ready = false;
+    for (int i = 0; i < nkb; ++i) {
+      if (!mbar_wait_warp(smem_u32(&full_bar[s]), ph, abortp, ready)) {
+        if (status && lane == 0) atomicCAS(status, ST_OK, ST_TIMEOUT_MMA);
+        break;
+      }
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t sW = tiles + s * SL::STAGE_BYTES, empty = smem_u32(&empty_bar[s]);
+      if (++s == stages) {
+        s = 0;
+        ph ^= 1u;
+      }
+      ready = mbar_peek_warp(smem_u32(&full_bar[s]), ph);
+      if (elect_one()) {
+        const uint64_t dW = make_smem_desc(sW), dA = make_smem_desc(sW + W_STAGE_BYTES);
+#pragma unroll
+        for (int k = 0; k < S8_K / 32; ++k)   // 32 bytes along K inside the swizzle row
+          umma_s8(tmem_d, dW + (uint64_t)(2 * k), dA + (uint64_t)(2 * k), idesc, (i > 0 || k > 0) ? 1u : 0u);
+        umma_commit(empty);
+        if (i == nkb - 1) umma_commit(smem_u32(&accum_bar));
+      }
+      __syncwarp();
+    }
+  }
+  __syncwarp();
+
+  const bool have = mbar_wait(smem_u32(&accum_bar), 0u, abortp);
+  if (!have && threadIdx.x == 0 && status) atomicCAS(status, ST_OK, ST_TIMEOUT_EPI);
+  if (__all_sync(0xffffffffu, have)) {   // the TMEM loads are warp-collective
+    constexpr int W = BN / 2;
+    const int half = (int)threadIdx.x >> 7;
+    s8_epilogue<W, T>(tmem_d + (uint32_t)(half * W), (int)threadIdx.x & 127, m0 + half * W, n0, M, N, sa, sw, out,
+                      slabs ? slabs + (size_t)blockIdx.z * M * N : nullptr);
+  } else {
+    drain_delay();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_d), "r"((uint32_t)BN) : "memory");
+}
+
+// The pair kernel's form.
+template <typename T>
+struct S8Form {
+  const float *sa, *sw;
+  T* out;
+  int split;
+  static constexpr int GROUPS = 1;
+  template <int W>
+  static constexpr uint32_t ex_bytes() { return 0; }
+  template <int W>
+  struct Shared {};
+  template <int W>
+  __device__ __forceinline__ void ahead(Shared<W>&, int, int, int) const {}
+  template <int W>
+  __device__ __forceinline__ void drain(Shared<W>&, uint32_t tmem_d, float*, int tl, int, int m0, int n0, int, int M, int N,
+                                        float* slab) const {
+    s8_epilogue<W, T>(tmem_d, tl, m0, n0, M, N, sa, sw, out, split ? reinterpret_cast<int*>(slab) : nullptr);
+  }
+};
+template <typename T>
+struct PairOperands<S8Form<T>> {
+  static constexpr int STAGE_K = S8_K;
+  static __host__ __device__ constexpr uint32_t idesc(int m, int n) { return make_idesc_s8(m, n); }
+  static __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    umma_s8_pair(d, a, b, idesc, accumulate);
+  }
+};
+
+// Sum of a split product's slabs, scaled.
+template <typename T>
+__global__ void __launch_bounds__(256) s8_finish_kernel(const int* __restrict__ slabs, int S, const float* __restrict__ sa,
+                                                        const float* __restrict__ sw, T* __restrict__ out, int M, int N) {
+  pdl_wait();
+  pdl_trigger();
+  const int n = blockIdx.x * 256 + threadIdx.x;
+  if (n >= N) return;
+  const size_t slab = (size_t)M * N;
+  const float w = sw[n];
+  for (int m = blockIdx.y; m < M; m += gridDim.y) {
+    const int* p = slabs + (size_t)m * N + n;
+    int sum = 0;
+    for (int s = 0; s < S; ++s) sum += __ldcg(p + s * slab);
+    out[(size_t)m * N + n] = from_f32<T>(__int2float_rn(sum) * sa[m] * w);
+  }
+}
+
+// ---------------------------------------------------------------- rows of 8-bit integers
+// A CTA per row; VECS vectors of eight elements per thread stay in registers between the row's maximum and its codes, what
+// is beyond them is read twice.  VEC: rows start on 16-byte boundaries.
+constexpr int QS_VECS = 4;
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_upto8(const T* p, int left, float (&v)[8]) {
+  if (VEC && left >= 8) {
+    Vec8<T>::load(p, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < left ? to_f32<T>(p[i]) : 0.f;
+  }
+}
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(1024) quantize_rows_s8_kernel(const T* __restrict__ x, size_t ldx, int8_t* __restrict__ q,
+                                                                size_t ldq, float* __restrict__ scale, int cols) {
+  __shared__ uint32_t red[32];
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x, step = blockDim.x * 8;
+  const T* row = x + (size_t)blockIdx.x * ldx;
+  int8_t* dst = q + (size_t)blockIdx.x * ldq;
+  float v[QS_VECS][8];
+  uint32_t top = 0;   // largest |x| as its bits: an infinity above every number, a NaN above that
+#pragma unroll
+  for (int i = 0; i < QS_VECS; ++i) load_upto8<T, VEC>(row + tid * 8 + i * step, cols - (tid * 8 + i * step), v[i]);
+#pragma unroll
+  for (int i = 0; i < QS_VECS; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7FFFFFFFu);
+  for (int c = tid * 8 + QS_VECS * step; c < cols; c += step) {
+    float u[8];
+    load_upto8<T, VEC>(row + c, cols - c, u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(u[e]) & 0x7FFFFFFFu);
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((tid & 31) == 0) red[tid >> 5] = top;
+  __syncthreads();
+  top = __reduce_max_sync(0xffffffffu, (tid & 31) < (blockDim.x >> 5) ? red[tid & 31] : 0u);
+  const float s = __fdiv_rn(__uint_as_float(top), 127.f);
+  const bool zero = s == 0.f || top >= 0x7F800000u;   // codes 0; the scale then shows an infinity or a NaN
+  if (tid == 0) scale[blockIdx.x] = s;
+  auto put = [&](int c, const float (&u)[8]) {
+    int8_t code[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      code[e] = zero ? (int8_t)0 : (int8_t)fminf(fmaxf(rintf(__fdiv_rn(u[e], s)), -127.f), 127.f);
+    if (c + 8 <= cols) {
+      uint2 w;
+      w.x = (uint8_t)code[0] | (uint32_t)(uint8_t)code[1] << 8 | (uint32_t)(uint8_t)code[2] << 16 | (uint32_t)(uint8_t)code[3] << 24;
+      w.y = (uint8_t)code[4] | (uint32_t)(uint8_t)code[5] << 8 | (uint32_t)(uint8_t)code[6] << 16 | (uint32_t)(uint8_t)code[7] << 24;
+      *reinterpret_cast<uint2*>(dst + c) = w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < cols) dst[c + e] = code[e];
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < QS_VECS; ++i)
+    if (tid * 8 + i * step < cols) put(tid * 8 + i * step, v[i]);
+  for (int c = tid * 8 + QS_VECS * step; c < cols; c += step) {
+    float u[8];
+    load_upto8<T, VEC>(row + c, cols - c, u);
+    put(c, u);
+  }
+}
+
+template <int BN, bool ONCE, typename T>
+cudaError_t launch_one_s8(const Launch& L, const CUtensorMap& tmW, const CUtensorMap& tmA, const float* sa, const float* sw,
+                          T* out, int* slabs, int M, int N, const GemmPlan& plan) {
+  using SL = S8Layout<BN>;
+  static DeviceOnce once;
+  cudaError_t e0 = once.run([] {
+    return cudaFuncSetAttribute(gemm_s8_kernel<BN, ONCE, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                (int)SL::total(SL::most()));
+  });
+  if (e0 != cudaSuccess) return e0;
+  const int stages = plan.stages < 2 ? 2 : plan.stages > SL::most() ? SL::most() : plan.stages;
+  const dim3 grid(plan.m_tiles, (N + TILE_W - 1) / TILE_W, plan.S_max);
+  cudaError_t e = launch_k(L, gemm_s8_kernel<BN, ONCE, T>, grid, dim3(S8_THREADS), SL::total(stages), tmW, tmA, sa, sw, out,
+                           slabs, M, N, plan.num_kb, plan.upc, stages, L.d_status);
+  L.count();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_as(const Launch& L, const CUtensorMap& tmW, const CUtensorMap& tmA, const float* sa, const float* sw, T* out,
+                      int* slabs, int M, int N, const GemmPlan& plan) {
+  int* const part = plan.S_max > 1 ? slabs : nullptr;
+  const bool once = plan.w_stream && plan.m_tiles == 1;
+  cudaError_t e;
+  if (plan.pair) {
+    const S8Form<T> form{sa, sw, out, part != nullptr};
+    float* const slab = reinterpret_cast<float*>(part);
+    if (plan.BN == 128)
+      e = launch_pair_form<128, false>(L, tmW, tmA, slab, M, N, plan.num_kb, plan, form, false);
+    else if (plan.BN == 192)
+      e = once ? launch_pair_form<192, true>(L, tmW, tmA, slab, M, N, plan.num_kb, plan, form, false)
+               : launch_pair_form<192, false>(L, tmW, tmA, slab, M, N, plan.num_kb, plan, form, false);
+    else
+      e = once ? launch_pair_form<256, true>(L, tmW, tmA, slab, M, N, plan.num_kb, plan, form, false)
+               : launch_pair_form<256, false>(L, tmW, tmA, slab, M, N, plan.num_kb, plan, form, false);
+  } else if (plan.BN == 32) {
+    e = once ? launch_one_s8<32, true, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan)
+             : launch_one_s8<32, false, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan);
+  } else if (plan.BN == 64) {
+    e = once ? launch_one_s8<64, true, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan)
+             : launch_one_s8<64, false, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan);
+  } else {
+    e = launch_one_s8<128, false, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan);
+  }
+  if (e != cudaSuccess || !part) return e;
+  Launch behind = L;
+  behind.pdl = true;
+  const dim3 grid((N + 255) / 256, std::min(M, 4096));
+  e = launch_k(behind, s8_finish_kernel<T>, grid, dim3(256), 0, (const int*)part, plan.S_max, sa, sw, out, M, N);
+  L.count();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+// Tile, ring and split as for the bf16 products of as many bytes (plan_gemm_bf16, whose figures hold per stage: a stage has
+// the same bytes and takes the same cycles): up to 128 rows, and for more rows of small weights, one CTA per tile; CTA pairs
+// otherwise, their tile and split by the same estimate.
+GemmPlan plan_gemm_s8(int M, int N, int K) {
+  GemmPlan p;
+  const int sms = sm_count(), pairs = sms / 2;
+  const long n_tiles = (N + TILE_W - 1) / TILE_W, n_pairs = (N + 2 * TILE_W - 1) / (2 * TILE_W);
+  p.num_kb = (K + S8_K - 1) / S8_K;
+  p.w_stream = (long)N * K >= 16L << 20;
+  int S = 0;
+  const bool many_rows = ((M + 255) / 256) * n_tiles > sms || (M >= 768 && K >= 2048);
+  if (M > 128 && ((long)N * K >= 1L << 22 || many_rows)) {
+    p.pair = 1;
+    double best = -1.0;
+    for (int BN : {256, 192, 128}) {
+      const long tiles = n_pairs * ((M + BN - 1) / BN);
+      const double issue = BN == 256 ? 0.33 : BN == 192 ? 0.27 : 0.25, bytes = (TILE_W + BN / 2) * (double)S8_K;
+      for (int s = 1; s == 1 || (s <= 16 && s * tiles <= pairs && s <= p.num_kb / 4); ++s) {
+        const long units = tiles * s, rounds = (units + pairs - 1) / pairs;
+        const double ctas = 2.0 * (units < pairs ? units : pairs), fabric = bytes * ctas / 12.0e6;
+        const double us = (double)rounds * ((p.num_kb + s - 1) / s) * (issue > fabric ? issue : fabric) +
+                          (s > 1 ? s * (double)M * N * 8.0 / 10.0e6 : 0.0);
+        if (best < 0.0 || us < best) {
+          best = us;
+          p.BN = BN;
+          S = s;
+        }
+      }
+    }
+  } else {
+    p.BN = M <= 32 ? 32 : M <= 64 ? 64 : 128;
+    if (M > 64 && n_tiles * ((M + 63) / 64) <= sms) p.BN = 64;
+  }
+  p.stages = p.pair ? MAX_STAGES : p.BN == 128 ? 3 : 4;
+  p.m_tiles = (M + p.BN - 1) / p.BN;
+  if (S == 0) {
+    const long tiles = (long)p.m_tiles * n_tiles;
+    const bool two_per_sm = p.BN == 128 || (p.BN == 64 && p.m_tiles > 1);
+    S = two_per_sm ? (int)(2L * sms / tiles) : (int)((sms + tiles - 1) / tiles);
+    S = std::max(1, std::min(S, p.num_kb / 4));
+  }
+  p.upc = (p.num_kb + S - 1) / S;
+  p.S_max = (p.num_kb + p.upc - 1) / p.upc;
+  return p;
+}
+
+size_t gemm_s8_scratch_bytes(int M, int N, const GemmPlan& plan) {
+  return plan.S_max > 1 ? (size_t)plan.S_max * M * N * 4 : 0;
+}
+
+cudaError_t launch_gemm_s8(const Launch& L, const int8_t* A, size_t lda, const float* sa, const int8_t* W, size_t ldw,
+                           const float* sw, void* out, int out_dtype, int M, int N, int K, const GemmPlan& plan, void* scratch,
+                           const char** err) {
+  CUtensorMap tmW, tmA;
+  if (!make_tensor_map_s8(W, (uint64_t)N, (uint64_t)K, ldw, TILE_W, &tmW) ||
+      !make_tensor_map_s8(A, (uint64_t)M, (uint64_t)K, lda, (uint32_t)(plan.pair ? plan.BN / 2 : plan.BN), &tmA)) {
+    if (err) *err = "cuTensorMapEncodeTiled failed or is unavailable";
+    return cudaErrorInvalidValue;
+  }
+  return out_dtype == DLLM_BF16 ? launch_as(L, tmW, tmA, sa, sw, (__nv_bfloat16*)out, (int*)scratch, M, N, plan)
+                                : launch_as(L, tmW, tmA, sa, sw, (float*)out, (int*)scratch, M, N, plan);
+}
+
+template <typename T>
+static cudaError_t quantize_as(const Launch& L, const T* x, size_t ldx, int8_t* q, size_t ldq, float* scale, int rows, int cols) {
+  const int want = (cols + 8 * QS_VECS - 1) / (8 * QS_VECS), threads = std::min(1024, std::max(64, (want + 31) / 32 * 32));
+  const bool vec = !((uintptr_t)x & 15) && !(ldx * sizeof(T) & 15);
+  cudaError_t e = vec ? launch_k(L, quantize_rows_s8_kernel<T, true>, dim3(rows), dim3(threads), 0, x, ldx, q, ldq, scale, cols)
+                      : launch_k(L, quantize_rows_s8_kernel<T, false>, dim3(rows), dim3(threads), 0, x, ldx, q, ldq, scale, cols);
+  L.count();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+cudaError_t launch_quantize_rows_s8(const Launch& L, const void* x, size_t ldx, int dtype, int8_t* q, size_t ldq, float* scale,
+                                    int rows, int cols) {
+  return dtype == DLLM_BF16 ? quantize_as(L, (const __nv_bfloat16*)x, ldx, q, ldq, scale, rows, cols)
+                            : quantize_as(L, (const float*)x, ldx, q, ldq, scale, rows, cols);
+}
+
+}  // namespace dllm
+
+DLLM_WAIT_LIMIT_HOOK(gemm_s8)

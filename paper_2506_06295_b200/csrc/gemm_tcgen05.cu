@@ -535,6 +535,15 @@ bool get_tensor_map_3d(const void* base, uint64_t batch, uint64_t rows, uint64_t
                        CUtensorMap* out) {
   return get_map(MapKey{base, batch, rows, cols, box_rows, current_device()}, out);
 }
+bool make_tensor_map_s8(const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows, CUtensorMap* out) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld};
+  cuuint32_t box[2] = {128, box_rows}, estr[2] = {1, 1};
+  return enc(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 int sm_count() {
   static std::atomic<int> per_device[64];  // zero-initialised: not yet asked

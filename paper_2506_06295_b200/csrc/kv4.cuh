@@ -1,0 +1,77 @@
+// The K / V cache held in 4 bits: its layout and the conversions the kernels share.
+//
+// A head's K (or V) of one token, HD numbers, is a row of HD / 2 bytes (element 2i in the low half of byte i, 2i + 1 in
+// the high half) and a pair (step, lo) of bf16: code u stands for lo + step * u.  Rows of one (sequence, KV head) are
+// contiguous ([B, Hkv, capacity, .]), so a tile of keys is one block of memory; capacity is a multiple of KV4_KEYS, so a
+// whole tile may be read wherever a sequence ends.
+//
+// No kernel multiplies the numbers themselves.  With v = u - 8 (a small integer, exact in fp16 and bf16)
+//     q . k   = step * (q . v) + (lo + 8 step) * sum(q)
+//     sum p k = sum (p step) v + sum p (lo + 8 step)
+// so the matrix instructions work on exact integers, the steps and offsets stay in fp32 outside, and centring the codes
+// keeps the rounding of p * step from being multiplied by the offset.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "../../include/dllm.h"
+#include "common.cuh"
+#include "internal.h"
+
+namespace dllm {
+
+constexpr int KV4_KEYS = 64;  // keys per tile, and what a cache's capacity is a multiple of
+
+// Two codes of a word -> two halves holding u - 8.  LO: nibbles 0 and 4, i.e. bits 0-3 and 16-19; HI: nibbles 1 and 5.
+// 0x6400 is 1024 in fp16, whose last place is 1: or-ing a nibble in adds it (16 times it for the high one).
+__device__ __forceinline__ uint32_t kv4_half_lo(uint32_t w) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, 0x000F000F, 0x64006400, 0xEA;" : "=r"(r) : "r"(w));
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&r), __half2half2(__ushort_as_half(0x6408)));  // - 1032
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t kv4_half_hi(uint32_t w) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, 0x00F000F0, 0x64006400, 0xEA;" : "=r"(r) : "r"(w));
+  const __half2 h = __hfma2(*reinterpret_cast<const __half2*>(&r), __half2half2(__ushort_as_half(0x2C00)),   // / 16
+                            __half2half2(__ushort_as_half(0xD480)));                                         // - 72
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The eight codes of a word as four pairs: p[i] = elements i and i + 4.
+__device__ __forceinline__ void kv4_word(uint32_t w, uint32_t (&p)[4]) {
+  p[0] = kv4_half_lo(w);
+  p[1] = kv4_half_hi(w);
+  p[2] = kv4_half_lo(w >> 8);
+  p[3] = kv4_half_hi(w >> 8);
+}
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float kv4_step(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float kv4_lo(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
+
+// What the host hands to the kernels.
+struct Kv4 {
+  uint8_t* k = nullptr;      // codes [B, Hkv, cap, hd / 2]
+  uint32_t* kp = nullptr;    // (step, lo) [B, Hkv, cap], step in the low half
+  uint8_t* v = nullptr;
+  uint32_t* vp = nullptr;
+  int B = 0, Hkv = 0, cap = 0, hd = 0;
+};
+
+// kv4_rows.cu
+cudaError_t launch_kv4_store(const Launch& L, const Kv4& c, const void* k, const void* v, size_t ldk, size_t ldv, int dtype,
+                             int a, const int32_t* pos, int start);
+cudaError_t launch_kv4_load(const Launch& L, const Kv4& c, int n, const int32_t* lens, void* k, void* v, int dtype);
+cudaError_t launch_kv4_evict(const Launch& L, const Kv4& src, const float* weight, int n, int keep, int first, int last,
+                             const int32_t* lens, const Kv4& dst, float* dst_weight, int32_t* index, int32_t* new_lens);
+// kv4_attention.cu
+size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd);
+cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n,
+                                 int H, const int32_t* lens, float* scratch, size_t scratch_floats);
+cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
+                               int a, int n, int H, const int32_t* lens);
+
+}  // namespace dllm

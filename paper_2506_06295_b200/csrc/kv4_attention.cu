@@ -1,0 +1,559 @@
+// Attention over the 4-bit K / V cache, and what every key gets of it.
+//
+// kv4_attn_kernel: 16 rows ((query, head of the group) pairs of one KV head) per CTA and split of the key range.  Its four
+// warps take key tiles of 64 in turn, each with a ring of its own that cp.async fills, so no warp waits for another before
+// the end; what they have is merged through shared memory there, splits by kv4_combine_kernel.  In a tile
+//     S = Q v_K^T, O += P~ v_V   mma.sync m16n8k16 on fp16, v = code - 8 made from the codes in registers
+// Q enters as fp16 scaled by a power of two per row (its bf16 mantissas are exact in it; what lies 2^38 below the row's
+// largest element is lost), P~ = p * step_V * 2^x with x from the largest step seen, so that it uses fp16's range: rounding
+// it costs 2^-12 of each term instead of bf16's 2^-9.  Maxima, sums, steps, offsets and outputs stay in fp32.
+// The order of the contraction's elements is free, which lets a thread's share of K be sixteen consecutive bytes of a key
+// and lets ldmatrix.trans bring pairs of keys together for V.
+#include <algorithm>
+
+#include "kv4.cuh"
+
+namespace dllm {
+
+namespace {
+
+constexpr int KA_THREADS = 128, KA_ROWS = 16, KA_STAGES = 3;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Power of two that brings a number with exponent field `ex` to [2^13, 2^14), and its inverse.  Fields below 20 count as 20.
+__device__ __forceinline__ float kv4_up(int ex) { return __uint_as_float((uint32_t)(267 - max(ex, 20)) << 23); }
+__device__ __forceinline__ float kv4_down(int ex) { return __uint_as_float((uint32_t)(max(ex, 20) - 13) << 23); }
+
+// A lane's share of a row of Q: elements [t * HD / 4, (t + 1) * HD / 4) as fp16 pairs in the order of kv4_word, scaled by
+// kv4_up of the row's largest; the four lanes of a row must call it together.  alpha: what the scaled product has to be
+// multiplied by, beta: the row's sum, both times scale_log2.
+template <int HD>
+__device__ __forceinline__ void q_share(const __nv_bfloat16* row, bool live, int t, float scale_log2, uint32_t (&w)[HD / 8],
+                                        float& alpha, float& beta) {
+  uint4 raw[HD / 32];
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+    raw[i] = live ? *reinterpret_cast<const uint4*>(row + t * (HD / 4) + i * 8) : make_uint4(0, 0, 0, 0);
+  float top = 0.f, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) {
+    const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float a = __uint_as_float(u[k] << 16), b = __uint_as_float(u[k] & 0xFFFF0000u);
+      top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+      sum += a + b;
+    }
+  }
+#pragma unroll
+  for (int o = 1; o <= 2; o <<= 1) {
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  }
+  const int ex = (int)(__float_as_uint(top) >> 23);
+  const float up = kv4_up(ex);
+  alpha = scale_log2 * kv4_down(ex);
+  beta = scale_log2 * sum;
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) {
+    const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+    float e[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      e[2 * k] = __uint_as_float(u[k] << 16) * up;
+      e[2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u) * up;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[4 * i + k] = half_pair(e[k], e[k + 4]);
+  }
+}
+
+template <int HD>
+struct KaSmem {
+  static constexpr int ROW = HD / 2;                                    // bytes of a key's codes
+  static constexpr int K = 0, V = KV4_KEYS * ROW, KP = 2 * V, VP = KP + KV4_KEYS * 4, STAGE = VP + KV4_KEYS * 4;
+  static constexpr int WARP = KA_STAGES * STAGE, TOTAL = 4 * WARP;
+  static constexpr int XS = HD + 4;                                     // floats per exchanged row
+  static_assert(KA_ROWS * XS * 4 <= WARP, "a warp's outputs replace its ring");
+  // place of the 16-byte chunk c of a key's V codes: eight keys' same chunks lie in eight different banks
+  static __device__ __forceinline__ int v_chunk(int key, int c) {
+    return key * ROW + ((HD == 128 ? c ^ ((key >> 1) & 3) : c ^ ((key >> 2) & 1)) << 4);
+  }
+};
+
+template <int HD>
+__global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c,
+                                                              const int32_t* __restrict__ lens,
+                                                              __nv_bfloat16* __restrict__ o, float* __restrict__ lse,
+                                                              float* __restrict__ o_part, float2* __restrict__ ml_part, int a,
+                                                              int n, int H, int S, float scale_log2) {
+  using SM = KaSmem<HD>;
+  constexpr int KS = HD / 16, CH = HD / 32;    // k-steps of Q K^T; 16-byte chunks of a row
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ float x_m[4][KA_ROWS], x_l[4][KA_ROWS];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int G = H / c.Hkv, kh = blockIdx.y, b = blockIdx.z / S, split = blockIdx.z - b * S;
+  const int rows = a * G, row0 = blockIdx.x * KA_ROWS;
+  pdl_wait();
+  pdl_trigger();
+  const int len = lens ? min(max(lens[b], 0), n) : n;
+  const int tiles_all = (len + KV4_KEYS - 1) / KV4_KEYS, per_split = (tiles_all + S - 1) / S;
+  const int tile_lo = min(split * per_split, tiles_all), tile_hi = min(tile_lo + per_split, tiles_all);
+  const size_t plane = ((size_t)b * c.Hkv + kh) * c.cap;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * SM::WARP;
+  uint8_t* const ring_g = smem + warp * SM::WARP;
+
+  auto request = [&](int tile, int stage) {
+    if (tile < tile_hi) {
+      const size_t key = plane + (size_t)tile * KV4_KEYS;
+      const uint32_t dst = ring + stage * SM::STAGE;
+      const uint8_t* ks = c.k + key * SM::ROW;
+      const uint8_t* vs = c.v + key * SM::ROW;
+#pragma unroll
+      for (int i = 0; i < KV4_KEYS * CH / 32; ++i) {
+        const int u = i * 32 + lane, r = u / CH, ch = u % CH;
+        cp_async16(dst + SM::K + u * 16, ks + u * 16);
+        cp_async16(dst + SM::V + SM::v_chunk(r, ch), vs + u * 16);
+      }
+      const uint32_t* ps = lane < 16 ? c.kp + key + lane * 4 : c.vp + key + (lane - 16) * 4;
+      cp_async16(dst + (lane < 16 ? SM::KP + lane * 16 : SM::VP + (lane - 16) * 16), ps);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int s = 0; s < KA_STAGES - 1; ++s) request(tile_lo + warp + 4 * s, s);
+
+  // rows g and g + 8 of the CTA's
+  uint32_t aq[KS][4];
+  float alpha[2], beta[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = row0 + g + 8 * h, i = r / G;
+    uint32_t w[HD / 8];
+    q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + r - i * G) * HD, r < rows, t, scale_log2, w, alpha[h], beta[h]);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      aq[ks][h] = w[2 * ks];
+      aq[ks][2 + h] = w[2 * ks + 1];
+    }
+  }
+
+  float acc[HD / 8][4];
+#pragma unroll
+  for (int i = 0; i < HD / 8; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};
+  int v_ex = 20;   // exponent field of the largest step of V so far
+
+  int stage = 0;
+  for (int tile = tile_lo + warp; tile < tile_hi; tile += 4) {
+    request(tile + 4 * (KA_STAGES - 1), stage == 0 ? KA_STAGES - 1 : stage - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(KA_STAGES - 1) : "memory");
+    __syncwarp();
+    const uint8_t* kt = ring_g + stage * SM::STAGE;
+    const uint32_t vt = ring + stage * SM::STAGE + SM::V;
+    const int valid = len - tile * KV4_KEYS;   // >= 1
+
+    float s[8][4];
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+      uint32_t w[CH];
+      const uint8_t* src = kt + SM::K + (nt * 8 + g) * SM::ROW + t * (SM::ROW / 4);
+      if constexpr (HD == 128) {
+        const uint4 x = *reinterpret_cast<const uint4*>(src);
+        w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(src);
+        w[0] = x.x; w[1] = x.y;
+      }
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        uint32_t p[4];
+        kv4_word(w[i], p);
+        mma_f16_16816(s[nt], aq[2 * i], p[0], p[1]);
+        mma_f16_16816(s[nt], aq[2 * i + 1], p[2], p[3]);
+      }
+    }
+    // scores in log2 units; their maxima
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+      const uint2 kp = *reinterpret_cast<const uint2*>(kt + SM::KP + (nt * 8 + 2 * t) * 4);
+      const uint32_t pr[2] = {kp.x, kp.y};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float step = kv4_step(pr[e]), off = fmaf(8.f, step, kv4_lo(pr[e]));
+        const bool out = nt * 8 + 2 * t + e >= valid;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float& x = s[nt][2 * h + e];
+          x = out ? -INFINITY : fmaf(x * step, alpha[h], off * beta[h]);
+          top[h] = fmaxf(top[h], x);
+        }
+      }
+    }
+    // the steps of V: two keys per lane
+    const uint2 vp_mine = *reinterpret_cast<const uint2*>(kt + SM::VP + lane * 8);
+    const uint32_t e0 = 2 * lane < valid ? (vp_mine.x >> 7) & 255u : 0u, e1 = 2 * lane + 1 < valid ? (vp_mine.y >> 7) & 255u : 0u;
+    const int ex = max(v_ex, (int)__reduce_max_sync(0xffffffffu, max(e0, e1)));
+    float corr[2];
+    bool same = ex == v_ex;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+      top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
+      const float now = fmaxf(m[h], top[h]);
+      corr[h] = now == m[h] ? 1.f : exp2_fast(m[h] - now);
+      same = same && now == m[h];
+      m[h] = now;
+    }
+    if (!__all_sync(0xffffffffu, same)) {
+      const float shrink = kv4_up(ex) * kv4_down(v_ex);   // 2^(v_ex - ex)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        l[h] *= corr[h];
+        z[h] *= corr[h];
+        corr[h] *= shrink;
+      }
+#pragma unroll
+      for (int i = 0; i < HD / 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][e] *= corr[e >> 1];
+      v_ex = ex;
+    }
+    const float up = kv4_up(v_ex);
+    const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt) {
+      const uint2 vp = *reinterpret_cast<const uint2*>(kt + SM::VP + (nt * 8 + 2 * t) * 4);
+      const uint32_t pr[2] = {vp.x, vp.y};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const bool out = nt * 8 + 2 * t + e >= valid;   // whatever stands there counts for nothing
+        const float step = out ? 0.f : kv4_step(pr[e]), off = out ? 0.f : fmaf(8.f, step, kv4_lo(pr[e])), w = step * up;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float p = exp2_fast(s[nt][2 * h + e] - ref[h]);
+          l[h] += p;
+          z[h] = fmaf(p, off, z[h]);
+          s[nt][2 * h + e] = p * w;
+        }
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < KV4_KEYS / 16; ++ks) {
+      const uint32_t ap[4] = {half_pair(s[2 * ks][0], s[2 * ks][1]), half_pair(s[2 * ks][2], s[2 * ks][3]),
+                              half_pair(s[2 * ks + 1][0], s[2 * ks + 1][1]), half_pair(s[2 * ks + 1][2], s[2 * ks + 1][3])};
+#pragma unroll
+      for (int cb = 0; cb < CH / 2; ++cb) {
+        const int key = ks * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
+        uint32_t r[4];
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(vt + SM::v_chunk(key, cb * 2 + (lane >> 4)))
+                     : "memory");
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint32_t b0[4], b1[4];
+          kv4_word(r[2 * x], b0);
+          kv4_word(r[2 * x + 1], b1);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mma_f16_16816(acc[(cb * 2 + x) * 4 + e], ap, b0[e], b1[e]);
+        }
+      }
+    }
+    __syncwarp();   // the stage is free once every lane has read it
+    stage = stage == KA_STAGES - 1 ? 0 : stage + 1;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+
+  // ---- the warps' rows, unnormalised, one after the other in shared memory
+  float* const xo = reinterpret_cast<float*>(smem + warp * SM::WARP);
+  const float down = kv4_down(v_ex);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int x = 1; x <= 2; x <<= 1) {
+      l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
+      z[h] += __shfl_xor_sync(0xffffffffu, z[h], x);
+    }
+    if (t == 0) {
+      x_m[warp][g + 8 * h] = m[h];
+      x_l[warp][g + 8 * h] = l[h];
+    }
+    // columns 2t and 2t + 1 of block (ch, e) are elements 32 ch + 8t + e and 32 ch + 8t + 4 + e
+#pragma unroll
+    for (int ch = 0; ch < CH; ++ch)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float4 v;
+        float* f = &v.x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = fmaf(acc[ch * 4 + e][2 * h + half], down, z[h]);
+        *reinterpret_cast<float4*>(xo + (g + 8 * h) * SM::XS + ch * 32 + t * 8 + half * 4) = v;
+      }
+  }
+  __syncthreads();
+  constexpr int PER = HD * KA_ROWS / KA_THREADS;   // consecutive elements per thread
+  const int r = tid / (HD / PER), col = tid % (HD / PER) * PER, vr = row0 + r;
+  if (vr >= rows) return;
+  float top = x_m[0][r];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) top = fmaxf(top, x_m[w][r]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, out[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) out[e] = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float f = exp2_fast(x_m[w][r] - ref);
+    const float* x = reinterpret_cast<const float*>(smem + w * SM::WARP) + r * SM::XS + col;
+    sum = fmaf(f, x_l[w][r], sum);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) out[e] = fmaf(f, x[e], out[e]);
+  }
+  const int i = vr / G;
+  const size_t orow = ((size_t)b * a + i) * H + kh * G + (vr - i * G);
+  if (S > 1) {
+    const size_t at = (size_t)split * ((size_t)gridDim.z / S * a * H) + orow;
+    if (col == 0) ml_part[at] = make_float2(top, sum);
+#pragma unroll
+    for (int e = 0; e < PER; e += 4)
+      *reinterpret_cast<float4*>(o_part + at * HD + col + e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
+    return;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row without keys: zeros
+#pragma unroll
+  for (int e = 0; e < PER; e += 8) {
+    float v[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x] = out[e + x] * inv;
+    Vec8<__nv_bfloat16>::store(o + orow * HD + col + e, v);
+  }
+  if (lse && col == 0) lse[orow] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+}
+
+// A warp per (row, head): the splits' parts in their order.
+template <int HD>
+__global__ void __launch_bounds__(256) kv4_combine_kernel(const float* __restrict__ o_part, const float2* __restrict__ ml_part,
+                                                          __nv_bfloat16* __restrict__ o, float* __restrict__ lse, size_t total,
+                                                          int S) {
+  constexpr int PER = HD / 32;
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  const size_t row = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= total) return;
+  float top = -INFINITY;
+  for (int s = lane; s < S; s += 32) top = fmaxf(top, __ldcg(&ml_part[s * total + row].x));
+  top = warp_max(top);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, out[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) out[e] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < S; ++s) {
+    const float2 ml = __ldcg(&ml_part[s * total + row]);
+    const float f = exp2_fast(ml.x - ref);
+    sum = fmaf(f, ml.y, sum);
+    const float* p = o_part + (s * total + row) * HD + lane * PER;
+    float x[PER];
+    if constexpr (PER == 4) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
+      const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
+      x[0] = v.x; x[1] = v.y;
+    }
+#pragma unroll
+    for (int e = 0; e < PER; ++e) out[e] = fmaf(f, x[e], out[e]);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  __nv_bfloat16* dst = o + row * HD + lane * PER;
+#pragma unroll
+  for (int e = 0; e < PER; e += 2)
+    *reinterpret_cast<__nv_bfloat162*>(dst + e) = __floats2bfloat162_rn(out[e] * inv, out[e + 1] * inv);
+  if (lse && lane == 0) lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+}
+
+// ---------------------------------------------------------------- weights
+// S^T = v_K Q^T with the keys along the rows: a warp holds 32 keys in registers and goes over all rows of its KV head, 64 at
+// a time in shared memory; a key's probabilities add up in its threads' registers (fp32, in the order of the rows), the four
+// threads of a key at the end.  No two CTAs add to the same key.
+constexpr int KW_KEYS = 128, KW_ROWS = 64;
+template <int HD>
+__global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c,
+                                                          const float* __restrict__ lse, const int32_t* __restrict__ lens,
+                                                          float* __restrict__ weight, int a, int n, int H, float scale_log2) {
+  constexpr int KS = HD / 16, CH = HD / 32, UNITS = HD / 32;   // units: two k-steps of a lane's share of Q, 16 bytes
+  __shared__ uint4 qs[UNITS][KW_ROWS][4];
+  __shared__ float4 par[KW_ROWS];    // alpha, beta, lse in log2 units
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int G = H / c.Hkv, kh = blockIdx.y, b = blockIdx.z, rows = a * G;
+  pdl_wait();
+  pdl_trigger();
+  const int len = lens ? min(max(lens[b], 0), n) : n;
+  if (blockIdx.x * KW_KEYS >= len) return;
+  const size_t plane = ((size_t)b * c.Hkv + kh) * c.cap;
+  const int key0 = blockIdx.x * KW_KEYS + warp * 32 + g;       // keys key0 + 8 i, i = 0..3
+  uint32_t ak[2][KS][4];
+  float step[4], off[4], got[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int key = min(key0 + 8 * i, len - 1);
+    const uint8_t* src = c.k + (plane + key) * (HD / 2) + t * (HD / 8);
+    uint32_t w[CH];
+    if constexpr (HD == 128) {
+      const uint4 x = *reinterpret_cast<const uint4*>(src);
+      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    } else {
+      const uint2 x = *reinterpret_cast<const uint2*>(src);
+      w[0] = x.x; w[1] = x.y;
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      uint32_t p[4];
+      kv4_word(w[k], p);
+      ak[i >> 1][2 * k][i & 1] = p[0];
+      ak[i >> 1][2 * k][2 + (i & 1)] = p[1];
+      ak[i >> 1][2 * k + 1][i & 1] = p[2];
+      ak[i >> 1][2 * k + 1][2 + (i & 1)] = p[3];
+    }
+    const uint32_t pr = c.kp[plane + key];
+    step[i] = kv4_step(pr);
+    off[i] = fmaf(8.f, step[i], kv4_lo(pr));
+    got[i] = 0.f;
+  }
+  for (int base = 0; base < rows; base += KW_ROWS) {
+    __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < KW_ROWS / 32; ++pass) {
+      const int r = pass * 32 + tid / 4, vr = base + r, i = vr / G, share = tid & 3;
+      const bool live = vr < rows;
+      uint32_t w[HD / 8];
+      float alpha, beta;
+      q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + vr - i * G) * HD, live, share, scale_log2, w, alpha, beta);
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) qs[u][r][share] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
+      if (share == 0) {
+        float x = INFINITY;      // rows past the last one and rows that saw no key give nothing
+        if (live) {
+          const float e = lse[((size_t)b * a + i) * H + kh * G + (vr - i * G)];
+          if (e != -INFINITY) x = e * 1.4426950408889634f;
+        }
+        par[r] = make_float4(alpha, beta, x, 0.f);
+      }
+    }
+    __syncthreads();
+#pragma unroll 2
+    for (int nt = 0; nt < KW_ROWS / 8; ++nt) {
+      if (base + nt * 8 >= rows) break;
+      float s[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[i][e] = 0.f;
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        const uint4 x = qs[u][nt * 8 + g][t];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          mma_f16_16816(s[i], ak[i][2 * u], x.x, x.y);
+          mma_f16_16816(s[i], ak[i][2 * u + 1], x.z, x.w);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float4 p = par[nt * 8 + 2 * t + e];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          got[i] += exp2_fast(fmaf(s[i >> 1][2 * (i & 1) + e] * step[i], p.x, fmaf(off[i], p.y, -p.z)));
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int x = 1; x <= 2; x <<= 1) got[i] += __shfl_xor_sync(0xffffffffu, got[i], x);
+    if (t == 0 && key0 + 8 * i < len) weight[plane + key0 + 8 * i] += got[i];
+  }
+}
+
+int attention_splits(int B, int a, int n, int H, int Hkv) {
+  const long base = (long)((a * (H / Hkv) + KA_ROWS - 1) / KA_ROWS) * Hkv * B, tiles = (n + KV4_KEYS - 1) / KV4_KEYS;
+  long S = 2L * sm_count() / base;          // two CTAs per SM are resident
+  S = std::min(S, (tiles + 3) / 4);         // a tile per warp at least
+  return (int)std::max(1L, std::min(S, 64L));
+}
+
+template <int HD>
+cudaError_t attention_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, const Kv4& c, __nv_bfloat16* o, float* lse, int a,
+                         int n, int H, const int32_t* lens, float* scratch, size_t scratch_floats) {
+  static DeviceOnce once;
+  cudaError_t e = once.run([] {
+    return cudaFuncSetAttribute(kv4_attn_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KaSmem<HD>::TOTAL);
+  });
+  if (e != cudaSuccess) return e;
+  const size_t total = (size_t)c.B * a * H, part = total * (HD + 2);
+  int S = attention_splits(c.B, a, n, H, c.Hkv);
+  if (S > 1) S = (int)std::min<size_t>(S, scratch ? scratch_floats / part : 0);
+  S = std::max(S, 1);
+  float* const o_part = scratch;
+  float2* const ml_part = reinterpret_cast<float2*>(scratch + (S > 1 ? (size_t)S * total * HD : 0));
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
+  const dim3 grid((a * (H / c.Hkv) + KA_ROWS - 1) / KA_ROWS, c.Hkv, c.B * S);
+  e = launch_k(L, kv4_attn_kernel<HD>, grid, dim3(KA_THREADS), KaSmem<HD>::TOTAL, q, ldq, c, lens, o, lse, o_part, ml_part, a, n,
+               H, S, scale_log2);
+  L.count();
+  if (e != cudaSuccess || S == 1) return e != cudaSuccess ? e : cudaGetLastError();
+  Launch behind = L;
+  behind.pdl = true;
+  e = launch_k(behind, kv4_combine_kernel<HD>, dim3((unsigned)((total + 7) / 8)), dim3(256), 0, (const float*)o_part,
+               (const float2*)ml_part, o, lse, total, S);
+  L.count();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd) {
+  const int S = attention_splits(B, a, n, H, Hkv);
+  return S > 1 ? (size_t)S * B * a * H * (hd + 2) : 0;
+}
+
+cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n,
+                                 int H, const int32_t* lens, float* scratch, size_t scratch_floats) {
+  auto* const qb = (const __nv_bfloat16*)q;
+  auto* const ob = (__nv_bfloat16*)o;
+  return c.hd == 64 ? attention_as<64>(L, qb, ldq, c, ob, lse, a, n, H, lens, scratch, scratch_floats)
+                    : attention_as<128>(L, qb, ldq, c, ob, lse, a, n, H, lens, scratch, scratch_floats);
+}
+
+cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
+                               int a, int n, int H, const int32_t* lens) {
+  const dim3 grid((n + KW_KEYS - 1) / KW_KEYS, c.Hkv, c.B);
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)c.hd);
+  cudaError_t e = c.hd == 64 ? launch_k(L, kv4_weights_kernel<64>, grid, dim3(128), 0, (const __nv_bfloat16*)q, ldq, c, lse,
+                                        lens, weight, a, n, H, scale_log2)
+                             : launch_k(L, kv4_weights_kernel<128>, grid, dim3(128), 0, (const __nv_bfloat16*)q, ldq, c, lse,
+                                        lens, weight, a, n, H, scale_log2);
+  L.count();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace dllm

@@ -198,4 +198,8 @@ bool get_tensor_map_2d(const void* base, uint64_t rows, uint64_t cols, uint32_t 
 bool get_tensor_map_3d(const void* base, uint64_t batch, uint64_t rows, uint64_t cols, uint32_t box_rows,
                        CUtensorMap* out);
 
+// 8-bit integers [rows, cols] whose rows start ld bytes apart (a multiple of 16), box box_rows x 128, the same swizzle;
+// encoded anew at every call.
+bool make_tensor_map_s8(const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows, CUtensorMap* out);
+
 }  // namespace dllm

@@ -40,8 +40,13 @@ class Config(C.Structure):
                 ("rope_theta", C.c_float), ("dtype", C.c_int32)]
 
 
+class Kv4CacheStruct(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_params", C.c_void_p), ("v_codes", C.c_void_p), ("v_params", C.c_void_p),
+                ("B", C.c_int32), ("n_kv_heads", C.c_int32), ("capacity", C.c_int32), ("head_dim", C.c_int32)]
+
+
 # every symbol include/dllm.h declares, with its C signature
-_P, _I, _F, _SZ = C.c_void_p, C.c_int, C.c_float, C.c_size_t
+_P, _I, _F, _SZ, _KV4 = C.c_void_p, C.c_int, C.c_float, C.c_size_t, C.POINTER(Kv4CacheStruct)
 SIGNATURES = {
     "dllm_last_error": (C.c_char_p, [_P]),
     "dllm_weights_bytes": (_SZ, [C.POINTER(Config)]),
@@ -102,6 +107,17 @@ SIGNATURES = {
     "dllm_debug_skip_one_load": (_I, [_I]),
     "dllm_debug_attention_plan": (_I, [_I, _I, _I, _I]),
     "dllm_debug_gemm_plan": (_I, [_I]),
+    "dllm_quantize_rows_s8": (_I, [_P, _SZ, _I, _P, _SZ, _P, _I, _I, _P]),
+    "dllm_gemm_s8_scratch_bytes": (_SZ, [_I, _I, _I]),
+    "dllm_gemm_s8": (_I, [_P, _SZ, _P, _P, _SZ, _P, _P, _I, _I, _I, _I, _P, _SZ, _P]),
+    "dllm_linear_s8_scratch_bytes": (_SZ, [_I, _I, _I]),
+    "dllm_linear_s8": (_I, [_P, _SZ, _I, _P, _SZ, _P, _P, _I, _I, _I, _I, _P, _SZ, _P]),
+    "dllm_kv4_store": (_I, [_KV4, _P, _SZ, _P, _SZ, _I, _I, _P, _I, _P]),
+    "dllm_kv4_load": (_I, [_KV4, _I, _P, _P, _P, _I, _P]),
+    "dllm_attention_kv4_scratch_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
+    "dllm_attention_kv4": (_I, [_P, _SZ, _KV4, _P, _P, _I, _I, _I, _P, _P, _SZ, _P]),
+    "dllm_attention_weights_kv4": (_I, [_P, _SZ, _KV4, _P, _P, _I, _I, _I, _P, _P]),
+    "dllm_kv4_evict": (_I, [_KV4, _P, _I, _I, _I, _I, _P, _KV4, _P, _P, _P, _P]),
 }
 for _name, (_res, _args) in SIGNATURES.items():
     _fn = getattr(lib, _name)
@@ -524,3 +540,270 @@ def debug_set_wait_limit_ns(ns: int) -> None:
 def debug_skip_one_load(enable: bool) -> None:
     """Test hook: the first CTA of every one-CTA bf16 GEMM launch leaves out one tile copy (its waits run out)."""
     _check(lib.dllm_debug_skip_one_load(int(enable)))
+
+
+# -- weights and rows in 8-bit integers; the K / V cache in 4 bits -------------
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise DllmError(INVALID_ARG, what)
+
+
+def _dtype(t) -> int:
+    import torch
+    if t.dtype is torch.bfloat16:
+        return BF16
+    _need(t.dtype is torch.float32, f"{t.dtype}: rows must be float32 or bfloat16")
+    return FP32
+
+
+def _like(t, x, dtype, shape, name: str) -> None:
+    _need(t.device == x.device and t.dtype is dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
+          f"{name} must be contiguous, {dtype}, {tuple(shape)} and on {x.device}")
+
+
+class _Place:
+    """The device of a call's tensors made current, and the stream it runs on (`stream`, or that device's current one).
+    On another stream than the current one what the call allocates belongs to that stream, and its inputs are kept
+    from being reused before it has run."""
+
+    __slots__ = ("device", "stream", "inputs", "contexts")
+
+    def __init__(self, device, stream, *inputs):
+        self.device, self.stream, self.inputs, self.contexts = device, stream, inputs, ()
+
+    def __enter__(self):
+        import torch
+        _need(self.device.type == "cuda", "tensors must be on a CUDA device")
+        for t in self.inputs:
+            _need(t is None or t.device == self.device, f"all tensors must be on {self.device}")
+        if torch.cuda.current_device() != self.device.index:
+            self.contexts += (torch.cuda.device(self.device),)
+            self.contexts[0].__enter__()
+        current = torch.cuda.current_stream()
+        if self.stream is None or self.stream.cuda_stream == current.cuda_stream:
+            return current.cuda_stream
+        self.contexts += (torch.cuda.stream(self.stream),)
+        self.contexts[-1].__enter__()
+        for t in self.inputs:
+            if t is not None:
+                t.record_stream(self.stream)
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc):
+        for c in reversed(self.contexts):
+            c.__exit__(*exc)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _row_pitch(t, cols: int, name: str) -> int:
+    """Elements between the rows of [..., rows, cols] whose rows are evenly spaced through all leading dimensions."""
+    _need(t.dim() >= 2 and t.shape[-1] == cols and t.stride(-1) == 1, f"{name}: rows of {cols} adjacent elements")
+    rows, pitch = 1, 0
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if rows == 1:
+            pitch = stride
+        _need(stride == pitch * rows, f"{name}: rows must be evenly spaced")
+        rows *= size
+    return pitch if rows > 1 else -(-cols // 16) * 16
+
+
+def quantize_rows_s8(x, stream=None):
+    """Rows of x [rows, cols] (float32 / bfloat16) as 8-bit integers and a scale each: (q int8 [rows, cols], whose rows
+    lie a multiple of 16 bytes apart as gemm_s8 needs them, scale float32 [rows])."""
+    import torch
+    _need(x.dim() == 2, "x must be a matrix")
+    rows, cols = x.shape
+    with _Place(x.device, stream, x) as sp:
+        ldq = -(-cols // 16) * 16
+        q = torch.empty((rows, ldq), dtype=torch.int8, device=x.device)
+        scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+        _check(lib.dllm_quantize_rows_s8(x.data_ptr(), _row_pitch(x, cols, "x"), _dtype(x), q.data_ptr(), ldq,
+                                         scale.data_ptr(), rows, cols, sp))
+    return q[:, :cols], scale
+
+
+def _product_args(W, w_scale, out_dtype, x, out, N):
+    import torch
+    out_dtype = out_dtype if out_dtype is not None else out.dtype if out is not None else torch.float32
+    _need(out_dtype in (torch.float32, torch.bfloat16), "the output is float32 or bfloat16")
+    _need(W.dtype is torch.int8 and W.dim() == 2 and x.dim() == 2 and x.shape[1] == W.shape[1],
+          "x [M, K] and W int8 [N, K]")
+    _like(w_scale, x, torch.float32, (N,), "w_scale")
+    if out is not None:
+        _like(out, x, out_dtype, (x.shape[0], N), "out")
+    return out_dtype
+
+
+def _scratch_for(x, nbytes: int, scratch):
+    import torch
+    if scratch is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
+    _need(scratch.is_contiguous() and scratch.device == x.device, "scratch must be contiguous and on the device")
+    return scratch
+
+
+def gemm_s8(A, a_scale, W, w_scale, out_dtype=None, out=None, scratch=None, stream=None):
+    """(A @ W.T) * a_scale[:, None] * w_scale[None, :] with A int8 [M, K], W int8 [N, K] (rows a multiple of 16 bytes
+    apart) and exact integer sums; float32 (default) or bfloat16 [M, N].  `scratch`: a contiguous tensor of at least
+    dllm_gemm_s8_scratch_bytes to use instead of a new one; calls that may overlap need one each."""
+    import torch
+    (M, K), N = A.shape, W.shape[0]
+    _need(A.dtype is torch.int8, "A must be int8")
+    with _Place(A.device, stream, A, a_scale, W, w_scale, out, scratch) as sp:
+        out_dtype = _product_args(W, w_scale, out_dtype, A, out, N)
+        _like(a_scale, A, torch.float32, (M,), "a_scale")
+        y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=A.device)
+        s = _scratch_for(A, lib.dllm_gemm_s8_scratch_bytes(M, N, K), scratch)
+        _check(lib.dllm_gemm_s8(A.data_ptr(), _row_pitch(A, K, "A"), a_scale.data_ptr(), W.data_ptr(),
+                                _row_pitch(W, K, "W"), w_scale.data_ptr(), y.data_ptr(), _dtype(y), M, N, K, _ptr(s),
+                                s.numel() * s.element_size() if s is not None else 0, sp))
+    return y
+
+
+def linear_s8(x, W, w_scale, out_dtype=None, out=None, scratch=None, stream=None):
+    """x @ (W * w_scale[:, None]).T with the rows of x [M, K] (float32 / bfloat16) brought to 8-bit integers within the
+    call; the rest as gemm_s8 (scratch: dllm_linear_s8_scratch_bytes)."""
+    import torch
+    _need(x.dim() == 2 and W.dim() == 2, "x [M, K] and W int8 [N, K]")
+    (M, K), N = x.shape, W.shape[0]
+    with _Place(x.device, stream, x, W, w_scale, out, scratch) as sp:
+        out_dtype = _product_args(W, w_scale, out_dtype, x, out, N)
+        y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=x.device)
+        s = _scratch_for(x, lib.dllm_linear_s8_scratch_bytes(M, N, K), scratch)
+        _check(lib.dllm_linear_s8(x.data_ptr(), _row_pitch(x, K, "x"), _dtype(x), W.data_ptr(),
+                                  _row_pitch(W, K, "W"), w_scale.data_ptr(), y.data_ptr(), _dtype(y), M, N, K, _ptr(s),
+                                  s.numel() * s.element_size() if s is not None else 0, sp))
+    return y
+
+
+class KV4Cache:
+    """One layer's K / V cache of B sequences in 4 bits (see include/dllm.h): k_codes, v_codes uint8 [B, Hkv, capacity,
+    hd / 2] and k_params, v_params bfloat16 [B, Hkv, capacity, 2] (step, lo).  New caches hold zeros; the capacity is
+    rounded up to a multiple of 64."""
+
+    def __init__(self, B: int, Hkv: int, capacity: int, hd: int, device="cuda:0"):
+        import torch
+        cap = -(-capacity // 64) * 64
+        self._bind(*(torch.zeros((B, Hkv, cap, w), dtype=dt, device=device)
+                     for w, dt in ((hd // 2, torch.uint8), (2, torch.bfloat16)) * 2))
+
+    @classmethod
+    def from_tensors(cls, k_codes, k_params, v_codes, v_params) -> "KV4Cache":
+        """A cache over existing tensors (which it keeps)."""
+        self = cls.__new__(cls)
+        self._bind(k_codes, k_params, v_codes, v_params)
+        return self
+
+    def _bind(self, k_codes, k_params, v_codes, v_params) -> None:
+        import torch
+        _need(k_codes.dim() == 4, "codes must be [B, Hkv, capacity, hd / 2]")
+        B, Hkv, cap, half = k_codes.shape
+        for t in (k_codes, v_codes):
+            _like(t, k_codes, torch.uint8, (B, Hkv, cap, half), "codes")
+        for t in (k_params, v_params):
+            _like(t, k_codes, torch.bfloat16, (B, Hkv, cap, 2), "params")
+        self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
+        self.B, self.Hkv, self.capacity, self.hd, self.device = B, Hkv, cap, 2 * half, k_codes.device
+        self.c = Kv4CacheStruct(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(), v_params.data_ptr(),
+                                B, Hkv, cap, 2 * half)
+        self.ref = C.byref(self.c)
+
+    def tensors(self):
+        return self.k_codes, self.k_params, self.v_codes, self.v_params
+
+
+def _lens_ok(lens, cache) -> None:
+    import torch
+    if lens is not None:
+        _like(lens, cache.k_codes, torch.int32, (cache.B,), "lens")
+
+
+def kv4_store(cache: KV4Cache, k, v, pos=None, start: int = 0, stream=None) -> None:
+    """Rows of K and V, [B, a, Hkv * hd] or [B * a, Hkv * hd] (float32 / bfloat16, evenly spaced rows), into the cache: row j
+    of a sequence at pos[b, j] (int32 [B, a]; outside of the capacity: nowhere) or start + j."""
+    import torch
+    width = cache.Hkv * cache.hd
+    rows = k.numel() // width
+    _need(k.dtype is v.dtype and k.shape == v.shape and rows % cache.B == 0 and rows > 0,
+          "k and v must have the same type and shape, B * a rows")
+    a = rows // cache.B
+    with _Place(cache.device, stream, k, v, pos, *cache.tensors()) as sp:
+        if pos is not None:
+            _like(pos, k, torch.int32, (cache.B, a), "pos")
+        _check(lib.dllm_kv4_store(cache.ref, k.data_ptr(), _row_pitch(k, width, "k"), v.data_ptr(),
+                                  _row_pitch(v, width, "v"), _dtype(k), a, _ptr(pos), start, sp))
+
+
+def kv4_load(cache: KV4Cache, n: int, lens=None, dtype=None, stream=None):
+    """(K, V) of the first n rows of every sequence as numbers, [B, n, Hkv * hd] in float32 or bfloat16 (the layout
+    attention() reads); zeros from lens[b] on."""
+    import torch
+    dtype = torch.float32 if dtype is None else dtype
+    with _Place(cache.device, stream, lens, *cache.tensors()) as sp:
+        _lens_ok(lens, cache)
+        _need(0 < n <= cache.capacity, "n must lie within the capacity")
+        k, v = (torch.empty((cache.B, n, cache.Hkv * cache.hd), dtype=dtype, device=cache.device) for _ in range(2))
+        _check(lib.dllm_kv4_load(cache.ref, n, _ptr(lens), k.data_ptr(), v.data_ptr(), _dtype(k), sp))
+    return k, v
+
+
+def _queries(q, cache, a, H) -> int:
+    import torch
+    _need(q.dtype is torch.bfloat16, "queries must be bfloat16")
+    _need(H > 0 and q.numel() == cache.B * a * H * cache.hd, "q must hold B * a rows of H * hd")
+    return _row_pitch(q, H * cache.hd, "q")
+
+
+def attention_kv4(q, cache: KV4Cache, a: int, n: int, H: int, lens=None, scratch=None, stream=None):
+    """attention() over a 4-bit cache: q bfloat16 [B * a, H * hd] (evenly spaced rows) against the first lens[b] (int32 [B];
+    None: n) keys.  Returns (o bfloat16 [B * a, H * hd], lse float32 [B * a, H])."""
+    import torch
+    with _Place(cache.device, stream, q, lens, scratch, *cache.tensors()) as sp:
+        ldq = _queries(q, cache, a, H)
+        _lens_ok(lens, cache)
+        o = torch.empty((cache.B * a, H * cache.hd), dtype=torch.bfloat16, device=cache.device)
+        lse = torch.empty((cache.B * a, H), dtype=torch.float32, device=cache.device)
+        s = _scratch_for(q, lib.dllm_attention_kv4_scratch_bytes(cache.B, a, n, H, cache.Hkv, cache.hd), scratch)
+        _check(lib.dllm_attention_kv4(q.data_ptr(), ldq, cache.ref, o.data_ptr(), lse.data_ptr(), a, n, H, _ptr(lens),
+                                      _ptr(s), s.numel() * s.element_size() if s is not None else 0, sp))
+    return o, lse
+
+
+def attention_weights_kv4(q, cache: KV4Cache, lse, weight, a: int, n: int, H: int, lens=None, stream=None) -> None:
+    """Adds to weight (float32 [B, Hkv, capacity]) what every key gets of the rows' attention, summed over the a queries and
+    the query heads of its KV head; lse as attention_kv4 returns it."""
+    import torch
+    with _Place(cache.device, stream, q, lse, weight, lens, *cache.tensors()) as sp:
+        ldq = _queries(q, cache, a, H)
+        _lens_ok(lens, cache)
+        _like(lse, q, torch.float32, (cache.B * a, H), "lse")
+        _like(weight, q, torch.float32, (cache.B, cache.Hkv, cache.capacity), "weight")
+        _check(lib.dllm_attention_weights_kv4(q.data_ptr(), ldq, cache.ref, lse.data_ptr(), weight.data_ptr(), a, n, H,
+                                              _ptr(lens), sp))
+
+
+def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: int = 0, lens=None, to=None, stream=None):
+    """Keeps min(length, keep) keys per sequence and KV head: the first `first`, the last `last`, and of the others those
+    with the largest weights (ties: lowest index), in their order.  Returns (cache, weight, index, lens): the smaller
+    cache (`to`, or a new one) with its weights (float32 [B, Hkv, its capacity]), where its rows came from (int32 [B, Hkv,
+    keep], -1 behind the last) and the sequences' new lengths (int32 [B])."""
+    import torch
+    with _Place(cache.device, stream, weight, lens, *cache.tensors(), *(to.tensors() if to is not None else ())) as sp:
+        _lens_ok(lens, cache)
+        _like(weight, cache.k_codes, torch.float32, (cache.B, cache.Hkv, cache.capacity), "weight")
+        _need(keep > 0, "keep must be positive")
+        dev, B, Hkv, cap = cache.device, cache.B, cache.Hkv, -(-keep // 64) * 64
+        if to is None:
+            to = KV4Cache.from_tensors(*(torch.empty((B, Hkv, cap, w), dtype=dt, device=dev)
+                                         for w, dt in ((cache.hd // 2, torch.uint8), (2, torch.bfloat16)) * 2))
+        new_weight = torch.empty((B, Hkv, to.capacity), dtype=torch.float32, device=dev)
+        index = torch.empty((B, Hkv, keep), dtype=torch.int32, device=dev)
+        new_lens = torch.empty((B,), dtype=torch.int32, device=dev)
+        _check(lib.dllm_kv4_evict(cache.ref, weight.data_ptr(), n, keep, first, last, _ptr(lens), to.ref,
+                                  new_weight.data_ptr(), index.data_ptr(), new_lens.data_ptr(), sp))
+    return to, new_weight, index, new_lens

@@ -1,0 +1,383 @@
+"""The 4-bit K / V cache: rows in and out, attention over it, weights and eviction, against 64-bit forms.
+
+Tolerances.  What is stored, read back, chosen and moved is defined in float32 arithmetic and compared for equality; a number
+read back is lo + step * code rounded once.  Attention and weights: see lowbit_ref."""
+import math
+
+import pytest
+import torch
+
+from tests import lowbit_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dllm():
+    from paper_2506_06295_b200 import build as build_mod
+    build_mod.build()
+    from paper_2506_06295_b200 import dllm as d
+    return d
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def lens_of(values):
+    return None if values is None else torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+# ---------------------------------------------------------------- rows in and out
+def expected_store(codes, params, x, pos, B, Hkv, hd):
+    """Plain store of x [B, a, Hkv * hd] at pos [B][a] into clones of codes / params."""
+    codes, params = codes.clone(), params.clone()
+    code, step, lo = ref.encode4(x.reshape(B, -1, Hkv, hd))
+    packed, pair = ref.pack4(code), torch.stack([step, lo], -1).bfloat16()
+    for b in range(B):
+        for j, p in enumerate(pos[b]):
+            if 0 <= p < codes.shape[2]:
+                codes[b, :, p], params[b, :, p] = packed[b, j], pair[b, j]
+    return codes, params
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,a,cap,Hkv,hd,kind", [(1, 1, 64, 1, 64, "start"), (2, 5, 128, 3, 128, "start"), (1, 64, 768, 32, 128, "pos"),
+                                                 (3, 100, 192, 4, 64, "pos"), (2, 130, 192, 7, 128, "odd"), (1, 700, 768, 2, 64, "odd")])
+def test_store_and_load(dllm, B, a, cap, Hkv, hd, kind, dtype):
+    g = gen(a + cap)
+    W = Hkv * hd
+    lead = W if kind != "odd" else 3                  # odd: rows off every 16-byte boundary
+    rows = torch.randn((B, a, lead + 2 * W + (lead == 3)), generator=g, device="cuda").to(dtype)
+    k, v = rows[:, :, lead:lead + W], rows[:, :, lead + W:lead + 2 * W]
+    cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
+    before = [t.clone() for t in cache.tensors()]
+    start, pos = 0, None
+    if kind == "start":
+        start = cap - a - 1
+        places = [list(range(start, start + a))] * B
+    else:
+        pos = torch.stack([torch.randperm(cap, generator=g, device="cuda")[:a] for _ in range(B)]).int()
+        if kind == "odd":                             # left out, and named twice
+            pos[0, 0], pos[0, 1], pos[0, 2] = -1, cap, 2 ** 31 - 1
+            pos[B - 1, 3] = pos[B - 1, a - 1]
+            pos[B - 1, 5] = pos[B - 1, 6] = pos[B - 1, a // 2]
+        places = pos.tolist()
+    dllm.kv4_store(cache, k, v, pos=pos, start=start)
+    for which, x in ((0, k), (2, v)):
+        codes, params = expected_store(before[which], before[which + 1], x, places, B, Hkv, hd)
+        assert torch.equal(cache.tensors()[which], codes)
+        assert torch.equal(cache.tensors()[which + 1], params)
+    lens = lens_of([cap // 2 + 7 * b for b in range(B)])
+    for n, ln, out in ((cap, None, torch.float32), (cap - 3, lens, torch.float32), (1, None, torch.bfloat16), (cap - 1, lens, torch.bfloat16)):
+        got = dllm.kv4_load(cache, n, lens=ln, dtype=out)
+        for which in (0, 1):
+            codes, par = cache.tensors()[2 * which], cache.tensors()[2 * which + 1].double()
+            want = (ref.unpack4(codes) * par[..., :1] + par[..., 1:]).float().to(out)[:, :, :n].transpose(1, 2).reshape(B, n, W).clone()
+            for b in range(B if ln is not None else 0):
+                want[b, int(ln[b]):] = 0
+            assert torch.equal(got[which], want)
+
+
+def test_a_stored_row_is_near_what_it_was(dllm):
+    """Half a step, and the roundings of step and lo to bf16 (2^-8 of 15 steps and of lo)."""
+    x = torch.randn((1, 50, 256), generator=gen(3), device="cuda").bfloat16()
+    cache = dllm.KV4Cache(1, 2, 50, 128)
+    dllm.kv4_store(cache, x, x)
+    k, v = dllm.kv4_load(cache, 50)
+    assert torch.equal(k, v)
+    spread = x.float().reshape(50, 2, 128)
+    step = (spread.amax(-1) - spread.amin(-1)) / 15
+    bound = (0.5 + 15 * 2.0 ** -8) * step + 2.0 ** -8 * spread.amin(-1).abs() + 1e-6
+    assert bool(((k - x.float()).reshape(50, 2, 128).abs() <= bound[..., None]).all())
+
+
+def test_rows_without_a_spread_and_without_numbers(dllm):
+    x = torch.randn((1, 6, 128), generator=gen(4), device="cuda")
+    x[0, 0], x[0, 1] = 0.0, 1.3
+    x[0, 2, 5], x[0, 3, 70], x[0, 4, 1] = math.nan, math.inf, -math.inf
+    x[0, 5, :64], x[0, 5, 64:] = 3e38, -3e38
+    cache = dllm.KV4Cache(1, 2, 6, 64)
+    dllm.kv4_store(cache, x, x)
+    k, _ = dllm.kv4_load(cache, 6)
+    h = k.reshape(6, 2, 64)
+    assert not h[0].any() and torch.equal(h[1], torch.full_like(h[1], 1.3).bfloat16().float())
+    assert h[2, 0].isnan().all() and h[2, 1].isfinite().all() and h[3, 1].isnan().all() and h[3, 0].isfinite().all()
+    assert h[4, 0].isnan().all() and h[5].isfinite().all()      # each head's half of row 5 has one value
+    wide = torch.cat([x[:, 5:, :64], x[:, 5:, 64:]], 1).transpose(1, 2).reshape(1, 1, 128).contiguous()   # alternating +-3e38
+    dllm.kv4_store(cache, wide, wide)
+    k, _ = dllm.kv4_load(cache, 1)
+    assert k.isnan().all()
+
+
+# ---------------------------------------------------------------- attention
+SHAPES = [  # B, a, n, H, Hkv, hd, lens
+    (1, 1, 1, 1, 1, 64, None),
+    (1, 1, 1, 7, 1, 128, None),
+    (1, 3, 65, 4, 4, 128, None),
+    (2, 1, 64, 8, 8, 64, [64, 0]),
+    (3, 2, 200, 14, 2, 128, [200, 1, 129]),
+    (1, 64, 768, 4, 4, 128, None),
+    (4, 5, 1000, 8, 2, 64, [1000, 999, 63, -5]),
+    (1, 17, 4128, 2, 2, 128, None),
+    (2, 9, 3000, 28, 4, 128, [2999, 5000]),
+    (1, 130, 513, 6, 3, 64, None),
+    (1, 200, 300, 7, 1, 128, [257]),
+    (2, 300, 450, 4, 2, 128, [450, 33]),
+    (1, 2, 20000, 8, 1, 128, None),
+]
+
+
+def queries(g, B, a, H, hd, scale=1.0):
+    return (scale * torch.randn((B * a, H * hd), generator=g, device="cuda")).bfloat16()
+
+
+def check_attention(q, cache, a, n, H, lens, o, lse):
+    want, wl, oe, se = ref.attention(q, cache, a, n, H, lens)
+    B, hd = cache.B, cache.hd
+    o, lse = o.double().reshape(B, a, H, hd), lse.double().reshape(B, a, H)
+    empty = torch.isneginf(wl)
+    assert torch.equal(torch.isneginf(lse), empty)
+    assert not o[empty].any()
+    assert bool(((lse - wl).abs()[~empty] <= se[~empty] + 2.0 ** -23 * wl[~empty].abs()).all())
+    bound = oe + 2.0 ** -8 * want.abs() * 1.01 + 1e-30
+    assert bool(((o - want).abs() <= bound).all()), float(((o - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("B,a,n,H,Hkv,hd,lens", SHAPES)
+def test_attention(dllm, B, a, n, H, Hkv, hd, lens):
+    g = gen(n + a)
+    cache = ref.random_cache(dllm, g, B, Hkv, -(-n // 64) * 64, hd)
+    q, lens = queries(g, B, a, H, hd), lens_of(lens)
+    o, lse = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+    check_attention(q, cache, a, n, H, lens, o, lse)
+    again, lse2 = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+    assert torch.equal(o, again) and torch.equal(lse, lse2)
+    dllm.kernel_status()
+
+
+@pytest.mark.parametrize("a,H,Hkv,n", [(2, 8, 2, 150), (90, 8, 2, 700)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_ignores_what_lies_behind_a_length(dllm, hd, a, H, Hkv, n):
+    """NaN, infinities and the largest numbers behind every length, inside of a tile and behind n; rows of Q inside of wider rows."""
+    g = gen(5)
+    cap = -(-n // 64) * 64
+    cache = ref.random_cache(dllm, g, 2, Hkv, cap, hd)
+    rows = queries(g, 2, a, 3 * H, hd)
+    q = rows[:, H * hd:2 * H * hd]
+    lens = lens_of([n - 50, n - 9])
+    o, lse = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+    check_attention(q, cache, a, n, H, lens, o, lse)
+    w = torch.zeros((2, Hkv, cap), device="cuda")
+    dllm.attention_weights_kv4(q, cache, lse, w, a, n, H, lens=lens)
+    for bad in (math.nan, math.inf, -math.inf, 3.3e38):
+        for b in range(2):
+            for t in (cache.k_params, cache.v_params):
+                t[b, :, int(lens[b]):] = bad
+            for t in (cache.k_codes, cache.v_codes):
+                t[b, :, int(lens[b]):] = 255
+        o2, lse2 = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+        w2 = torch.zeros((2, Hkv, cap), device="cuda")
+        dllm.attention_weights_kv4(q, cache, lse, w2, a, n, H, lens=lens)
+        assert torch.equal(w, w2)
+
+
+@pytest.mark.parametrize("a", [3, 80])
+def test_attention_of_a_row_with_a_nan(dllm, a):
+    """A NaN among the keys or values of one head shows in that head's rows and in no other's; so does one in a query."""
+    g = gen(6)
+    cache = ref.random_cache(dllm, g, 1, 2, 192, 128)
+    q = queries(g, 1, a, 4, 128)
+    clean, clean_lse = dllm.attention_kv4(q, cache, a, 190, 4)
+    for t in (cache.k_params, cache.v_params):
+        keep = t.clone()
+        t[0, 1, 77] = math.nan
+        o, _ = dllm.attention_kv4(q, cache, a, 190, 4)
+        assert o.reshape(a, 4, 128)[:, 2:].isnan().all()
+        assert torch.equal(o.reshape(a, 4, 128)[:, :2], clean.reshape(a, 4, 128)[:, :2])
+        t.copy_(keep)
+    q2 = q.clone()
+    q2[1, 5] = math.nan
+    o, lse = dllm.attention_kv4(q2, cache, a, 190, 4)
+    assert o[1, :128].isnan().all() and lse[1, 0].isnan()
+    o[1, :128], lse[1, 0] = clean[1, :128], clean_lse[1, 0]
+    assert torch.equal(o, clean) and torch.equal(lse, clean_lse)
+
+
+@pytest.mark.parametrize("a,qs,cs", [(4, 40.0, 1.0), (100, 40.0, 1.0), (4, 1e-30, 1.0), (4, 1e30, 1e-30), (100, 1e30, 1e-30), (4, 1.0, 1e-20),
+                                     (100, 1.0, 1e-20), (4, 1e-4, 1e4), (100, 1e-4, 1e4)])
+def test_attention_of_very_large_and_very_small_numbers(dllm, a, qs, cs):
+    """One key ahead of all others, scores of zero, numbers near the ends of bf16's range."""
+    g = gen(7)
+    cache = ref.random_cache(dllm, g, 1, 2, 320, 128, scale=cs)
+    q = queries(g, 1, a, 2, 128, scale=qs)
+    o, lse = dllm.attention_kv4(q, cache, a, 311, 2)
+    check_attention(q, cache, a, 311, 2, None, o, lse)
+
+
+@pytest.mark.parametrize("a", [4, 100])
+def test_attention_over_values_of_very_different_steps(dllm, a):
+    g = gen(8)
+    cache = ref.random_cache(dllm, g, 1, 1, 640, 128)
+    cache.v_params.mul_(2.0 ** torch.randint(-12, 13, (1, 1, 640, 1), generator=g, device="cuda").float())
+    cache.v_params[0, 0, 10:20, 0] = 0          # no spread at all
+    cache.k_params[0, 0, 30:40] = 0
+    q = queries(g, 1, a, 1, 128)
+    o, lse = dllm.attention_kv4(q, cache, a, 640, 1)
+    # terms far below the largest step's are rounded at 2^-24 of 2^-13 of it instead of at 2^-11 of themselves
+    want, wl, oe, se = ref.attention(q, cache, a, 640, 1)
+    floor = 640 * 2.0 ** -38 * 8 * float(cache.v_params[..., 0].abs().max()) * 2
+    assert bool(((o.double().reshape(want.shape) - want).abs() <= oe + 2.0 ** -8 * 1.01 * want.abs() + floor).all())
+    assert bool(((lse.double().reshape(wl.shape) - wl).abs() <= se + 2.0 ** -23 * wl.abs()).all())
+
+
+def test_attention_past_four_gigabytes(dllm):
+    """The last plane of a cache whose codes take 4.3 GB a tensor."""
+    B, Hkv, cap, hd = 1, 8, 64 * 131200, 128
+    cache = dllm.KV4Cache(B, Hkv, cap, hd)
+    assert cache.k_codes.numel() > 2 ** 32
+    g = gen(9)
+    small = ref.random_cache(dllm, g, 1, 1, 128, hd)
+    n0 = cap - 128
+    k, v = dllm.kv4_load(small, 128, dtype=torch.bfloat16)
+    dllm.kv4_store(cache, k.repeat(1, 1, Hkv), v.repeat(1, 1, Hkv), start=n0)
+    got_k, _ = dllm.kv4_load(dllm.KV4Cache.from_tensors(*(t[:, :, n0:].contiguous() for t in cache.tensors())), 128)
+    again = dllm.KV4Cache(1, 1, 128, hd)
+    dllm.kv4_store(again, k, v)
+    want_k, _ = dllm.kv4_load(again, 128)
+    assert torch.equal(got_k.reshape(128, Hkv, hd)[:, -1], want_k.reshape(128, hd))
+    # the other keys get scores of -10^4 or less, so the last ones alone count
+    cache.k_params[:, :, :n0, 1] = -1e4
+    q = torch.ones((1, Hkv * hd), device="cuda").bfloat16()
+    o, lse = dllm.attention_kv4(q, cache, 1, cap, Hkv)
+    want, wl, oe, se = ref.attention(torch.ones((1, hd), device="cuda").bfloat16(), again, 1, 128, 1)
+    assert bool(((o.double().reshape(Hkv, hd) - want.reshape(1, hd)).abs() <= oe.reshape(1, hd) + 2.0 ** -8 * 1.01 * want.abs().reshape(1, hd)).all())
+    assert bool(((lse.double().reshape(-1) - wl.reshape(1)).abs() <= se.reshape(1) + 2.0 ** -22 * wl.abs().reshape(1)).all())
+    w = torch.zeros((B, Hkv, cap), device="cuda")
+    dllm.attention_weights_kv4(q, cache, lse, w, 1, cap, Hkv)
+    assert bool((w.double().sum(-1) - 1).abs().max() < 1e-4) and not w[:, :, :n0].any()
+
+
+def test_attention_on_another_stream_and_in_a_graph(dllm):
+    g = gen(10)
+    cache = ref.random_cache(dllm, g, 1, 2, 2048, 128)
+    q = queries(g, 1, 4, 4, 128)
+    lens = lens_of([2000])
+    scratch = torch.empty(dllm.lib.dllm_attention_kv4_scratch_bytes(1, 4, 2048, 4, 2, 128), dtype=torch.uint8, device="cuda")
+    assert scratch.numel() > 0
+    want = dllm.attention_kv4(q, cache, 4, 2048, 4, lens=lens)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = dllm.attention_kv4(q, cache, 4, 2048, 4, lens=lens, stream=side)
+    side.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, lse = dllm.attention_kv4(q, cache, 4, 2048, 4, lens=lens, scratch=scratch)
+    q.copy_(queries(g, 1, 4, 4, 128))
+    lens.fill_(777)
+    graph.replay()
+    torch.cuda.synchronize()
+    check_attention(q, cache, 4, 2048, 4, lens, o, lse)
+
+
+# ---------------------------------------------------------------- weights
+@pytest.mark.parametrize("B,a,n,H,Hkv,hd,lens", SHAPES)
+def test_weights(dllm, B, a, n, H, Hkv, hd, lens):
+    g = gen(n + 2 * a)
+    cap = -(-n // 64) * 64
+    cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
+    q, lens = queries(g, B, a, H, hd), lens_of(lens)
+    _, lse = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+    if a > 2:
+        lse[1, 0] = -math.inf                     # a row that saw nothing
+    had = torch.rand((B, Hkv, cap), generator=g, device="cuda")
+    w = had.clone()
+    dllm.attention_weights_kv4(q, cache, lse, w, a, n, H, lens=lens)
+    got, err = ref.weights(q, cache, lse, a, n, H, lens)
+    want = had.double() + got
+    bound = err + 2.0 ** -23 * want
+    assert bool(((w.double() - want).abs() <= bound).all()), float(((w.double() - want).abs() / bound).max())
+    for b in range(B):
+        L = n if lens is None else min(max(int(lens[b]), 0), n)
+        assert torch.equal(w[b, :, L:], had[b, :, L:])
+    again = had.clone()
+    dllm.attention_weights_kv4(q, cache, lse, again, a, n, H, lens=lens)
+    assert torch.equal(w, again)
+
+
+# ---------------------------------------------------------------- eviction
+@pytest.mark.parametrize("B,n,keep,first,last,Hkv,hd,lens,ties", [
+    (1, 1, 1, 0, 0, 1, 64, None, False), (1, 100, 1, 0, 0, 2, 128, None, False), (1, 100, 40, 0, 0, 2, 128, None, True),
+    (2, 700, 300, 4, 32, 3, 64, [700, 299], True), (3, 5000, 777, 0, 777, 2, 128, [5000, 0, 778], False),
+    (1, 5000, 2500, 2500, 0, 1, 64, None, False), (2, 20000, 9999, 5, 5, 1, 64, [20000, 19999], True), (1, 130, 192, 3, 3, 2, 128, None, False),
+    (1, 9000, 8999, 1, 1, 1, 64, [9001], False)])
+def test_evict(dllm, B, n, keep, first, last, Hkv, hd, lens, ties):
+    g = gen(n + keep)
+    cap = -(-n // 64) * 64
+    cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
+    w = torch.rand((B, Hkv, cap), generator=g, device="cuda").pow(6)
+    if ties:
+        w = (w * 20).floor() / 4 - 0.5
+        w[0, 0, n // 3] = math.nan
+        w[0, 0, n // 2] = math.inf
+        w[0, 0, n // 2 + 1] = -math.inf
+        w[0, 0, 5:30:2] = -0.0
+        w[0, 0, 6:30:2] = 0.0
+    lens = lens_of(lens)
+    was = [t.clone() for t in (*cache.tensors(), w)]
+    to = dllm.KV4Cache(B, Hkv, keep + 64, hd)
+    for t in to.tensors():
+        t.fill_(3)
+    to, nw, index, new = dllm.kv4_evict(cache, w, n, keep, first, last, lens=lens, to=to)
+    want, want_lens = ref.evict(w, n, keep, first, last, lens)
+    assert torch.equal(index.cpu(), want) and torch.equal(new.cpu(), want_lens)
+    for x, y in zip((*cache.tensors(), w), was):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))       # the source stays as it is
+    for b in range(B):
+        L = int(want_lens[b])
+        for h in range(Hkv):
+            rows = index[b, h, :L].long()
+            for src, dst in zip(cache.tensors(), to.tensors()):
+                assert torch.equal(dst[b, h, :L], src[b, h, rows])
+                assert bool((dst[b, h, L:] == 3).all())                    # rows behind the last one as they were
+            assert torch.equal(nw[b, h, :L].nan_to_num(-9), w[b, h, rows].nan_to_num(-9)) and not nw[b, h, L:].any()
+
+
+# ---------------------------------------------------------------- as they are used together
+def test_a_prompt_is_cached_scored_and_thinned_out(dllm):
+    """Prompt and response rows go into the cache, the response's queries attend and score, half of the prompt leaves, and
+    attention over what stayed equals attention over those rows of the old cache."""
+    g = gen(11)
+    B, P, R, H, Hkv, hd = 2, 500, 24, 8, 2, 128
+    n = P + R
+    cache = dllm.KV4Cache(B, Hkv, n, hd)
+    qkv = torch.randn((B, n, (H + 2 * Hkv) * hd), generator=g, device="cuda").bfloat16()
+    k, v = qkv[..., H * hd:(H + Hkv) * hd], qkv[..., (H + Hkv) * hd:]
+    dllm.kv4_store(cache, k[:, :P].contiguous(), v[:, :P].contiguous())
+    dllm.kv4_store(cache, k[:, P:].contiguous(), v[:, P:].contiguous(), start=P)
+    q = qkv[:, P:, :H * hd].contiguous().reshape(B * R, H * hd)
+    o, lse = dllm.attention_kv4(q, cache, R, n, H)
+    check_attention(q, cache, R, n, H, None, o, lse)
+    weight = torch.zeros((B, Hkv, cache.capacity), device="cuda")
+    dllm.attention_weights_kv4(q, cache, lse, weight, R, n, H)
+    assert float((weight.sum(-1) - R * (H // Hkv)).abs().max()) < 1e-2      # every row gives one in all
+    keep = P // 2 + R
+    small, w2, index, lens = dllm.kv4_evict(cache, weight, n, keep, first=4, last=R)
+    assert bool((index[:, :, -R:] == torch.arange(P, n, device="cuda")).all()) and lens.tolist() == [keep] * B
+    o2, lse2 = dllm.attention_kv4(q, small, R, keep, H, lens=lens)
+    rows = index.long()[..., None]
+    pick = dllm.KV4Cache(B, Hkv, keep, hd)
+    for src, dst in zip(cache.tensors(), pick.tensors()):
+        dst[:, :, :keep] = src.gather(2, rows.expand(-1, -1, -1, src.shape[-1]))
+    check_attention(q, pick, R, keep, H, None, o2, lse2)
+    # the response goes on: its new rows replace the old ones at their new places
+    pos = torch.arange(keep - R, keep, device="cuda", dtype=torch.int32).expand(B, R).contiguous()
+    dllm.kv4_store(small, k[:, :R].contiguous(), v[:, :R].contiguous(), pos=pos)
+    dllm.kv4_store(pick, k[:, :R].contiguous(), v[:, :R].contiguous(), start=keep - R)
+    o3, lse3 = dllm.attention_kv4(q, small, R, keep, H, lens=lens)
+    check_attention(q, pick, R, keep, H, None, o3, lse3)
+    dllm.kernel_status()
