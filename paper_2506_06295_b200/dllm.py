@@ -543,108 +543,126 @@ def debug_skip_one_load(enable: bool) -> None:
 
 
 # -- weights and rows in 8-bit integers; the K / V cache in 4 bits -------------
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise DllmError(INVALID_ARG, what)
+# A call of a few rows takes the GPU some microseconds, so the checks below cost little where they pass: messages are put
+# together only for a refusal, and the current device and stream are asked for as numbers.
+def _refuse(what: str):
+    raise DllmError(INVALID_ARG, what)
 
 
 def _dtype(t) -> int:
     import torch
     if t.dtype is torch.bfloat16:
         return BF16
-    _need(t.dtype is torch.float32, f"{t.dtype}: rows must be float32 or bfloat16")
-    return FP32
+    return FP32 if t.dtype is torch.float32 else _refuse(f"{t.dtype}: rows must be float32 or bfloat16")
 
 
-def _like(t, x, dtype, shape, name: str) -> None:
-    _need(t.device == x.device and t.dtype is dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(),
-          f"{name} must be contiguous, {dtype}, {tuple(shape)} and on {x.device}")
+def _like(t, dtype, shape, name: str) -> None:
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name} must be contiguous, {dtype} and {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
 
 
-class _Place:
-    """The device of a call's tensors made current, and the stream it runs on (`stream`, or that device's current one).
-    On another stream than the current one what the call allocates belongs to that stream, and its inputs are kept
-    from being reused before it has run."""
+def _elsewhere(t, stream) -> bool:
+    """Whether a call has to be placed first: it names a stream, or another device than its tensors' is current."""
+    import torch
+    if not t.is_cuda:
+        _refuse("tensors must be on a CUDA device")
+    return stream is not None or t.get_device() != torch._C._cuda_getDevice()
 
-    __slots__ = ("device", "stream", "inputs", "contexts")
 
-    def __init__(self, device, stream, *inputs):
-        self.device, self.stream, self.inputs, self.contexts = device, stream, inputs, ()
+class _Placed:
+    """The device of a call's tensors made current, and `stream` (None: that device's current one).  What the call
+    allocates then belongs to that stream, and its inputs are kept from being reused before it has run."""
+
+    def __init__(self, stream, *inputs):
+        import torch
+        self.device = torch.cuda.device(inputs[0].device)
+        self.stream = torch.cuda.stream(stream)
+        self.inputs = inputs if stream is not None else ()
+        self.on = stream
 
     def __enter__(self):
-        import torch
-        _need(self.device.type == "cuda", "tensors must be on a CUDA device")
+        self.device.__enter__()
+        self.stream.__enter__()
         for t in self.inputs:
-            _need(t is None or t.device == self.device, f"all tensors must be on {self.device}")
-        if torch.cuda.current_device() != self.device.index:
-            self.contexts += (torch.cuda.device(self.device),)
-            self.contexts[0].__enter__()
-        current = torch.cuda.current_stream()
-        if self.stream is None or self.stream.cuda_stream == current.cuda_stream:
-            return current.cuda_stream
-        self.contexts += (torch.cuda.stream(self.stream),)
-        self.contexts[-1].__enter__()
-        for t in self.inputs:
-            if t is not None:
-                t.record_stream(self.stream)
-        return self.stream.cuda_stream
+            if t is not None and t.is_cuda:
+                t.record_stream(self.on)
 
     def __exit__(self, *exc):
-        for c in reversed(self.contexts):
-            c.__exit__(*exc)
+        self.stream.__exit__(*exc)
+        self.device.__exit__(*exc)
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _stream_of(*tensors) -> int:
+    """The current stream of the tensors' device, which has to be one."""
+    import torch
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            _refuse("all tensors must be on one CUDA device")
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _row_pitch(t, cols: int, name: str) -> int:
     """Elements between the rows of [..., rows, cols] whose rows are evenly spaced through all leading dimensions."""
-    _need(t.dim() >= 2 and t.shape[-1] == cols and t.stride(-1) == 1, f"{name}: rows of {cols} adjacent elements")
+    shape, strides = t.shape, t.stride()
+    if len(shape) < 2 or shape[-1] != cols or (strides[-1] != 1 and cols > 1):
+        _refuse(f"{name}: rows of {cols} adjacent elements are needed")
     rows, pitch = 1, 0
-    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
-        if size == 1:
+    for d in range(len(shape) - 2, -1, -1):
+        if shape[d] == 1:
             continue
         if rows == 1:
-            pitch = stride
-        _need(stride == pitch * rows, f"{name}: rows must be evenly spaced")
-        rows *= size
+            pitch = strides[d]
+        if strides[d] != pitch * rows:
+            _refuse(f"{name}: rows must be evenly spaced")
+        rows *= shape[d]
     return pitch if rows > 1 else -(-cols // 16) * 16
+
+
+def _space(x, need: int, scratch):
+    """(address, bytes, tensor) of a call's scratch: the caller's, or a new one."""
+    import torch
+    if scratch is None:
+        if not need:
+            return None, 0, None
+        t = torch.empty(need, dtype=torch.uint8, device=x.device)
+        return t.data_ptr(), need, t
+    if not scratch.is_contiguous():
+        _refuse("scratch must be contiguous")
+    return scratch.data_ptr(), scratch.numel() * scratch.element_size(), scratch
 
 
 def quantize_rows_s8(x, stream=None):
     """Rows of x [rows, cols] (float32 / bfloat16) as 8-bit integers and a scale each: (q int8 [rows, cols], whose rows
     lie a multiple of 16 bytes apart as gemm_s8 needs them, scale float32 [rows])."""
     import torch
-    _need(x.dim() == 2, "x must be a matrix")
+    if _elsewhere(x, stream):
+        with _Placed(stream, x):
+            return quantize_rows_s8(x)
+    if x.dim() != 2:
+        _refuse("x must be a matrix")
     rows, cols = x.shape
-    with _Place(x.device, stream, x) as sp:
-        ldq = -(-cols // 16) * 16
-        q = torch.empty((rows, ldq), dtype=torch.int8, device=x.device)
-        scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
-        _check(lib.dllm_quantize_rows_s8(x.data_ptr(), _row_pitch(x, cols, "x"), _dtype(x), q.data_ptr(), ldq,
-                                         scale.data_ptr(), rows, cols, sp))
+    ldq = -(-cols // 16) * 16
+    q = torch.empty((rows, ldq), dtype=torch.int8, device=x.device)
+    scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    _check(lib.dllm_quantize_rows_s8(x.data_ptr(), _row_pitch(x, cols, "x"), _dtype(x), q.data_ptr(), ldq, scale.data_ptr(),
+                                     rows, cols, _stream_of(x)))
     return q[:, :cols], scale
 
 
-def _product_args(W, w_scale, out_dtype, x, out, N):
+def _product(x, W, w_scale, out_dtype, out):
+    """The checks the two products share; (M, N, K, output)."""
     import torch
-    out_dtype = out_dtype if out_dtype is not None else out.dtype if out is not None else torch.float32
-    _need(out_dtype in (torch.float32, torch.bfloat16), "the output is float32 or bfloat16")
-    _need(W.dtype is torch.int8 and W.dim() == 2 and x.dim() == 2 and x.shape[1] == W.shape[1],
-          "x [M, K] and W int8 [N, K]")
-    _like(w_scale, x, torch.float32, (N,), "w_scale")
+    if x.dim() != 2 or W.dim() != 2 or W.dtype is not torch.int8 or x.shape[1] != W.shape[1]:
+        _refuse("a product takes rows [M, K] and W int8 [N, K]")
+    M, K = x.shape
+    N = W.shape[0]
+    _like(w_scale, torch.float32, (N,), "w_scale")
     if out is not None:
-        _like(out, x, out_dtype, (x.shape[0], N), "out")
-    return out_dtype
-
-
-def _scratch_for(x, nbytes: int, scratch):
-    import torch
-    if scratch is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=x.device) if nbytes else None
-    _need(scratch.is_contiguous() and scratch.device == x.device, "scratch must be contiguous and on the device")
-    return scratch
+        _like(out, out.dtype if out_dtype is None else out_dtype, (M, N), "out")
+    else:
+        out = torch.empty((M, N), dtype=torch.float32 if out_dtype is None else out_dtype, device=x.device)
+    return M, N, K, out
 
 
 def gemm_s8(A, a_scale, W, w_scale, out_dtype=None, out=None, scratch=None, stream=None):
@@ -652,32 +670,31 @@ def gemm_s8(A, a_scale, W, w_scale, out_dtype=None, out=None, scratch=None, stre
     apart) and exact integer sums; float32 (default) or bfloat16 [M, N].  `scratch`: a contiguous tensor of at least
     dllm_gemm_s8_scratch_bytes to use instead of a new one; calls that may overlap need one each."""
     import torch
-    (M, K), N = A.shape, W.shape[0]
-    _need(A.dtype is torch.int8, "A must be int8")
-    with _Place(A.device, stream, A, a_scale, W, w_scale, out, scratch) as sp:
-        out_dtype = _product_args(W, w_scale, out_dtype, A, out, N)
-        _like(a_scale, A, torch.float32, (M,), "a_scale")
-        y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=A.device)
-        s = _scratch_for(A, lib.dllm_gemm_s8_scratch_bytes(M, N, K), scratch)
-        _check(lib.dllm_gemm_s8(A.data_ptr(), _row_pitch(A, K, "A"), a_scale.data_ptr(), W.data_ptr(),
-                                _row_pitch(W, K, "W"), w_scale.data_ptr(), y.data_ptr(), _dtype(y), M, N, K, _ptr(s),
-                                s.numel() * s.element_size() if s is not None else 0, sp))
+    if _elsewhere(A, stream):
+        with _Placed(stream, A, a_scale, W, w_scale, out, scratch):
+            return gemm_s8(A, a_scale, W, w_scale, out_dtype, out, scratch)
+    if A.dtype is not torch.int8:
+        _refuse("A must be int8")
+    M, N, K, y = _product(A, W, w_scale, out_dtype, out)
+    _like(a_scale, torch.float32, (M,), "a_scale")
+    at, size, keep = _space(A, lib.dllm_gemm_s8_scratch_bytes(M, N, K), scratch)
+    _check(lib.dllm_gemm_s8(A.data_ptr(), _row_pitch(A, K, "A"), a_scale.data_ptr(), W.data_ptr(), _row_pitch(W, K, "W"),
+                            w_scale.data_ptr(), y.data_ptr(), _dtype(y), M, N, K, at, size,
+                            _stream_of(A, a_scale, W, w_scale, y, keep)))
     return y
 
 
 def linear_s8(x, W, w_scale, out_dtype=None, out=None, scratch=None, stream=None):
     """x @ (W * w_scale[:, None]).T with the rows of x [M, K] (float32 / bfloat16) brought to 8-bit integers within the
     call; the rest as gemm_s8 (scratch: dllm_linear_s8_scratch_bytes)."""
-    import torch
-    _need(x.dim() == 2 and W.dim() == 2, "x [M, K] and W int8 [N, K]")
-    (M, K), N = x.shape, W.shape[0]
-    with _Place(x.device, stream, x, W, w_scale, out, scratch) as sp:
-        out_dtype = _product_args(W, w_scale, out_dtype, x, out, N)
-        y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=x.device)
-        s = _scratch_for(x, lib.dllm_linear_s8_scratch_bytes(M, N, K), scratch)
-        _check(lib.dllm_linear_s8(x.data_ptr(), _row_pitch(x, K, "x"), _dtype(x), W.data_ptr(),
-                                  _row_pitch(W, K, "W"), w_scale.data_ptr(), y.data_ptr(), _dtype(y), M, N, K, _ptr(s),
-                                  s.numel() * s.element_size() if s is not None else 0, sp))
+    if _elsewhere(x, stream):
+        with _Placed(stream, x, W, w_scale, out, scratch):
+            return linear_s8(x, W, w_scale, out_dtype, out, scratch)
+    M, N, K, y = _product(x, W, w_scale, out_dtype, out)
+    at, size, keep = _space(x, lib.dllm_linear_s8_scratch_bytes(M, N, K), scratch)
+    _check(lib.dllm_linear_s8(x.data_ptr(), _row_pitch(x, K, "x"), _dtype(x), W.data_ptr(), _row_pitch(W, K, "W"),
+                              w_scale.data_ptr(), y.data_ptr(), _dtype(y), M, N, K, at, size,
+                              _stream_of(x, W, w_scale, y, keep)))
     return y
 
 
@@ -688,9 +705,15 @@ class KV4Cache:
 
     def __init__(self, B: int, Hkv: int, capacity: int, hd: int, device="cuda:0"):
         import torch
+        self._bind(*self._tensors(torch.zeros, B, Hkv, capacity, hd, device))
+
+    @staticmethod
+    def _tensors(make, B, Hkv, capacity, hd, device):
+        import torch
         cap = -(-capacity // 64) * 64
-        self._bind(*(torch.zeros((B, Hkv, cap, w), dtype=dt, device=device)
-                     for w, dt in ((hd // 2, torch.uint8), (2, torch.bfloat16)) * 2))
+        codes, pairs = (B, Hkv, cap, hd // 2), (B, Hkv, cap, 2)
+        return (make(codes, dtype=torch.uint8, device=device), make(pairs, dtype=torch.bfloat16, device=device),
+                make(codes, dtype=torch.uint8, device=device), make(pairs, dtype=torch.bfloat16, device=device))
 
     @classmethod
     def from_tensors(cls, k_codes, k_params, v_codes, v_params) -> "KV4Cache":
@@ -701,12 +724,15 @@ class KV4Cache:
 
     def _bind(self, k_codes, k_params, v_codes, v_params) -> None:
         import torch
-        _need(k_codes.dim() == 4, "codes must be [B, Hkv, capacity, hd / 2]")
-        B, Hkv, cap, half = k_codes.shape
-        for t in (k_codes, v_codes):
-            _like(t, k_codes, torch.uint8, (B, Hkv, cap, half), "codes")
-        for t in (k_params, v_params):
-            _like(t, k_codes, torch.bfloat16, (B, Hkv, cap, 2), "params")
+        if k_codes.dim() != 4:
+            _refuse("codes must be [B, Hkv, capacity, hd / 2]")
+        shape = B, Hkv, cap, half = k_codes.shape
+        _like(k_codes, torch.uint8, shape, "k_codes")
+        _like(v_codes, torch.uint8, shape, "v_codes")
+        _like(k_params, torch.bfloat16, (B, Hkv, cap, 2), "k_params")
+        _like(v_params, torch.bfloat16, (B, Hkv, cap, 2), "v_params")
+        if not k_codes.device == k_params.device == v_codes.device == v_params.device:
+            _refuse("a cache's tensors must be on one device")
         self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
         self.B, self.Hkv, self.capacity, self.hd, self.device = B, Hkv, cap, 2 * half, k_codes.device
         self.c = Kv4CacheStruct(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(), v_params.data_ptr(),
@@ -717,45 +743,54 @@ class KV4Cache:
         return self.k_codes, self.k_params, self.v_codes, self.v_params
 
 
-def _lens_ok(lens, cache) -> None:
+def _lens(lens, cache):
     import torch
-    if lens is not None:
-        _like(lens, cache.k_codes, torch.int32, (cache.B,), "lens")
+    if lens is None:
+        return None
+    _like(lens, torch.int32, (cache.B,), "lens")
+    return lens.data_ptr()
 
 
 def kv4_store(cache: KV4Cache, k, v, pos=None, start: int = 0, stream=None) -> None:
     """Rows of K and V, [B, a, Hkv * hd] or [B * a, Hkv * hd] (float32 / bfloat16, evenly spaced rows), into the cache: row j
     of a sequence at pos[b, j] (int32 [B, a]; outside of the capacity: nowhere) or start + j."""
     import torch
+    if _elsewhere(cache.k_codes, stream):
+        with _Placed(stream, *cache.tensors(), k, v, pos):
+            return kv4_store(cache, k, v, pos, start)
     width = cache.Hkv * cache.hd
     rows = k.numel() // width
-    _need(k.dtype is v.dtype and k.shape == v.shape and rows % cache.B == 0 and rows > 0,
-          "k and v must have the same type and shape, B * a rows")
+    if k.dtype is not v.dtype or k.shape != v.shape or rows % cache.B or not rows:
+        _refuse("k and v must have the same type and shape, B * a rows")
     a = rows // cache.B
-    with _Place(cache.device, stream, k, v, pos, *cache.tensors()) as sp:
-        if pos is not None:
-            _like(pos, k, torch.int32, (cache.B, a), "pos")
-        _check(lib.dllm_kv4_store(cache.ref, k.data_ptr(), _row_pitch(k, width, "k"), v.data_ptr(),
-                                  _row_pitch(v, width, "v"), _dtype(k), a, _ptr(pos), start, sp))
+    if pos is not None:
+        _like(pos, torch.int32, (cache.B, a), "pos")
+    _check(lib.dllm_kv4_store(cache.ref, k.data_ptr(), _row_pitch(k, width, "k"), v.data_ptr(), _row_pitch(v, width, "v"),
+                              _dtype(k), a, None if pos is None else pos.data_ptr(), start,
+                              _stream_of(cache.k_codes, k, v, pos)))
 
 
 def kv4_load(cache: KV4Cache, n: int, lens=None, dtype=None, stream=None):
     """(K, V) of the first n rows of every sequence as numbers, [B, n, Hkv * hd] in float32 or bfloat16 (the layout
     attention() reads); zeros from lens[b] on."""
     import torch
-    dtype = torch.float32 if dtype is None else dtype
-    with _Place(cache.device, stream, lens, *cache.tensors()) as sp:
-        _lens_ok(lens, cache)
-        _need(0 < n <= cache.capacity, "n must lie within the capacity")
-        k, v = (torch.empty((cache.B, n, cache.Hkv * cache.hd), dtype=dtype, device=cache.device) for _ in range(2))
-        _check(lib.dllm_kv4_load(cache.ref, n, _ptr(lens), k.data_ptr(), v.data_ptr(), _dtype(k), sp))
+    if _elsewhere(cache.k_codes, stream):
+        with _Placed(stream, *cache.tensors(), lens):
+            return kv4_load(cache, n, lens, dtype)
+    if not 0 < n <= cache.capacity:
+        _refuse("n must lie within the capacity")
+    shape, dtype = (cache.B, n, cache.Hkv * cache.hd), torch.float32 if dtype is None else dtype
+    k = torch.empty(shape, dtype=dtype, device=cache.device)
+    v = torch.empty(shape, dtype=dtype, device=cache.device)
+    _check(lib.dllm_kv4_load(cache.ref, n, _lens(lens, cache), k.data_ptr(), v.data_ptr(), _dtype(k),
+                             _stream_of(cache.k_codes, lens)))
     return k, v
 
 
 def _queries(q, cache, a, H) -> int:
     import torch
-    _need(q.dtype is torch.bfloat16, "queries must be bfloat16")
-    _need(H > 0 and q.numel() == cache.B * a * H * cache.hd, "q must hold B * a rows of H * hd")
+    if q.dtype is not torch.bfloat16 or H <= 0 or q.numel() != cache.B * a * H * cache.hd:
+        _refuse("q must be bfloat16 and hold B * a rows of H * hd")
     return _row_pitch(q, H * cache.hd, "q")
 
 
@@ -763,14 +798,15 @@ def attention_kv4(q, cache: KV4Cache, a: int, n: int, H: int, lens=None, scratch
     """attention() over a 4-bit cache: q bfloat16 [B * a, H * hd] (evenly spaced rows) against the first lens[b] (int32 [B];
     None: n) keys.  Returns (o bfloat16 [B * a, H * hd], lse float32 [B * a, H])."""
     import torch
-    with _Place(cache.device, stream, q, lens, scratch, *cache.tensors()) as sp:
-        ldq = _queries(q, cache, a, H)
-        _lens_ok(lens, cache)
-        o = torch.empty((cache.B * a, H * cache.hd), dtype=torch.bfloat16, device=cache.device)
-        lse = torch.empty((cache.B * a, H), dtype=torch.float32, device=cache.device)
-        s = _scratch_for(q, lib.dllm_attention_kv4_scratch_bytes(cache.B, a, n, H, cache.Hkv, cache.hd), scratch)
-        _check(lib.dllm_attention_kv4(q.data_ptr(), ldq, cache.ref, o.data_ptr(), lse.data_ptr(), a, n, H, _ptr(lens),
-                                      _ptr(s), s.numel() * s.element_size() if s is not None else 0, sp))
+    if _elsewhere(q, stream):
+        with _Placed(stream, q, *cache.tensors(), lens, scratch):
+            return attention_kv4(q, cache, a, n, H, lens, scratch)
+    ldq, rows = _queries(q, cache, a, H), cache.B * a
+    o = torch.empty((rows, H * cache.hd), dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((rows, H), dtype=torch.float32, device=q.device)
+    at, size, keep = _space(q, lib.dllm_attention_kv4_scratch_bytes(cache.B, a, n, H, cache.Hkv, cache.hd), scratch)
+    _check(lib.dllm_attention_kv4(q.data_ptr(), ldq, cache.ref, o.data_ptr(), lse.data_ptr(), a, n, H, _lens(lens, cache),
+                                  at, size, _stream_of(q, cache.k_codes, lens, keep)))
     return o, lse
 
 
@@ -778,13 +814,14 @@ def attention_weights_kv4(q, cache: KV4Cache, lse, weight, a: int, n: int, H: in
     """Adds to weight (float32 [B, Hkv, capacity]) what every key gets of the rows' attention, summed over the a queries and
     the query heads of its KV head; lse as attention_kv4 returns it."""
     import torch
-    with _Place(cache.device, stream, q, lse, weight, lens, *cache.tensors()) as sp:
-        ldq = _queries(q, cache, a, H)
-        _lens_ok(lens, cache)
-        _like(lse, q, torch.float32, (cache.B * a, H), "lse")
-        _like(weight, q, torch.float32, (cache.B, cache.Hkv, cache.capacity), "weight")
-        _check(lib.dllm_attention_weights_kv4(q.data_ptr(), ldq, cache.ref, lse.data_ptr(), weight.data_ptr(), a, n, H,
-                                              _ptr(lens), sp))
+    if _elsewhere(q, stream):
+        with _Placed(stream, q, *cache.tensors(), lse, weight, lens):
+            return attention_weights_kv4(q, cache, lse, weight, a, n, H, lens)
+    ldq = _queries(q, cache, a, H)
+    _like(lse, torch.float32, (cache.B * a, H), "lse")
+    _like(weight, torch.float32, (cache.B, cache.Hkv, cache.capacity), "weight")
+    _check(lib.dllm_attention_weights_kv4(q.data_ptr(), ldq, cache.ref, lse.data_ptr(), weight.data_ptr(), a, n, H,
+                                          _lens(lens, cache), _stream_of(q, cache.k_codes, lse, weight, lens)))
 
 
 def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: int = 0, lens=None, to=None, stream=None):
@@ -793,17 +830,19 @@ def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: 
     cache (`to`, or a new one) with its weights (float32 [B, Hkv, its capacity]), where its rows came from (int32 [B, Hkv,
     keep], -1 behind the last) and the sequences' new lengths (int32 [B])."""
     import torch
-    with _Place(cache.device, stream, weight, lens, *cache.tensors(), *(to.tensors() if to is not None else ())) as sp:
-        _lens_ok(lens, cache)
-        _like(weight, cache.k_codes, torch.float32, (cache.B, cache.Hkv, cache.capacity), "weight")
-        _need(keep > 0, "keep must be positive")
-        dev, B, Hkv, cap = cache.device, cache.B, cache.Hkv, -(-keep // 64) * 64
-        if to is None:
-            to = KV4Cache.from_tensors(*(torch.empty((B, Hkv, cap, w), dtype=dt, device=dev)
-                                         for w, dt in ((cache.hd // 2, torch.uint8), (2, torch.bfloat16)) * 2))
-        new_weight = torch.empty((B, Hkv, to.capacity), dtype=torch.float32, device=dev)
-        index = torch.empty((B, Hkv, keep), dtype=torch.int32, device=dev)
-        new_lens = torch.empty((B,), dtype=torch.int32, device=dev)
-        _check(lib.dllm_kv4_evict(cache.ref, weight.data_ptr(), n, keep, first, last, _ptr(lens), to.ref,
-                                  new_weight.data_ptr(), index.data_ptr(), new_lens.data_ptr(), sp))
+    if _elsewhere(weight, stream):
+        with _Placed(stream, weight, *cache.tensors(), lens, *(to.tensors() if to is not None else ())):
+            return kv4_evict(cache, weight, n, keep, first, last, lens, to)
+    B, Hkv, dev = cache.B, cache.Hkv, cache.device
+    _like(weight, torch.float32, (B, Hkv, cache.capacity), "weight")
+    if keep <= 0:
+        _refuse("keep must be positive")
+    if to is None:
+        to = KV4Cache.from_tensors(*KV4Cache._tensors(torch.empty, B, Hkv, keep, cache.hd, dev))
+    new_weight = torch.empty((B, Hkv, to.capacity), dtype=torch.float32, device=dev)
+    index = torch.empty((B, Hkv, keep), dtype=torch.int32, device=dev)
+    new_lens = torch.empty((B,), dtype=torch.int32, device=dev)
+    _check(lib.dllm_kv4_evict(cache.ref, weight.data_ptr(), n, keep, first, last, _lens(lens, cache), to.ref,
+                              new_weight.data_ptr(), index.data_ptr(), new_lens.data_ptr(),
+                              _stream_of(cache.k_codes, weight, lens, to.k_codes)))
     return to, new_weight, index, new_lens

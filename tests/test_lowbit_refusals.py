@@ -122,7 +122,7 @@ def test_binding_refuses_what_the_library_cannot_see(dllm):
     c = dllm.KV4Cache(1, 2, 64, 64, device="cpu")
     assert c.capacity == 64 and dllm.KV4Cache(1, 2, 65, 64, device="cpu").capacity == 128
     with pytest.raises(dllm.DllmError):
-        dllm.kv4_load(c, 10)
+        dllm.kv4_load(c, 10)          # on the CPU
     with pytest.raises(dllm.DllmError):
         dllm.kv4_store(c, torch.zeros(1, 3, 128), torch.zeros(1, 4, 128))
     # rows that no single pitch describes
