@@ -18,6 +18,7 @@
 
 #include "../../include/dllm.h"
 #include "gemm_s8.cuh"
+#include "kv4.cuh"
 #include "internal.h"
 #include "tma.cuh"
 
@@ -1356,6 +1357,7 @@ dllm_status dllm_debug_set_wait_limit_ns(uint64_t ns) {
   CU_TRY(nullptr, set_wait_limit_attention(ns));
   CU_TRY(nullptr, set_wait_limit_attention_umma(ns));
   CU_TRY(nullptr, set_wait_limit_gemm_s8(ns));
+  CU_TRY(nullptr, set_wait_limit_kv4_umma(ns));
   CU_TRY(nullptr, cudaDeviceSynchronize());
   return DLLM_OK;
 }

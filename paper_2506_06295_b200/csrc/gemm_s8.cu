@@ -60,14 +60,22 @@ struct S8Layout {
 };
 
 // One CTA: 128 weight rows x BN rows of A x a k range (blockIdx.z).  Warp 0 requests operands, warp 1 issues the MMAs, all
-// eight drain the accumulator, half of the columns per group of four.
-constexpr int S8_THREADS = 256;
+// eight drain the accumulator, half of the columns per group of four.  The CTAs of a split tile are a cluster: each leaves its
+// integers in its own shared memory (the drained ring), and each adds up every S-th row of the tile over all of them, scales it
+// and writes it.  (3 x 4096 x 4096 in five splits with slabs in global memory and a launch that adds them: 10.5 us with the
+// row quantisation, and a third launch for the host; so: FIGURE.)
+constexpr int S8_THREADS = 256, S8_MOST_SPLITS = 8;
+__device__ __forceinline__ int4 remote4(uint32_t addr) {
+  int4 r;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr));
+  return r;
+}
 template <int BN, bool ONCE, typename T>
 __global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_constant__ CUtensorMap tmW,
                                                              const __grid_constant__ CUtensorMap tmA,
                                                              const float* __restrict__ sa, const float* __restrict__ sw,
-                                                             T* __restrict__ out, int* __restrict__ slabs, int M, int N,
-                                                             int num_kb, int kb_per_split, int stages, int* __restrict__ status) {
+                                                             T* __restrict__ out, int M, int N, int num_kb, int kb_per_split,
+                                                             int stages, int* __restrict__ status) {
   using SL = S8Layout<BN>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[MAX_STAGES];
@@ -169,13 +177,60 @@ __global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_consta
 
   const bool have = mbar_wait(smem_u32(&accum_bar), 0u, abortp);
   if (!have && threadIdx.x == 0 && status) atomicCAS(status, ST_OK, ST_TIMEOUT_EPI);
-  if (__all_sync(0xffffffffu, have)) {   // the TMEM loads are warp-collective
-    constexpr int W = BN / 2;
-    const int half = (int)threadIdx.x >> 7;
-    s8_epilogue<W, T>(tmem_d + (uint32_t)(half * W), (int)threadIdx.x & 127, m0 + half * W, n0, M, N, sa, sw, out,
-                      slabs ? slabs + (size_t)blockIdx.z * M * N : nullptr);
+  const bool warp_ok = __all_sync(0xffffffffu, have);   // the TMEM loads are warp-collective
+  constexpr int W = BN / 2;
+  const int half = (int)threadIdx.x >> 7, tl = (int)threadIdx.x & 127, S = (int)gridDim.z;
+  const uint32_t tmem_h = tmem_d + (uint32_t)(half * W);
+  if (!warp_ok) drain_delay();
+  if (S == 1) {
+    if (warp_ok) s8_epilogue<W, T>(tmem_h, tl, m0 + half * W, n0, M, N, sa, sw, out, nullptr);
   } else {
-    drain_delay();
+    int* const ex = reinterpret_cast<int*>(smem_raw + (tiles - smem_u32(smem_raw)));   // [BN][128]
+    const int rows = min(BN, M - m0);
+    if (warp_ok) {
+      const uint32_t tmem_w = tmem_h + ((uint32_t)(tl >> 5) << 21);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+      for (int c0 = 0; c0 < W && half * W + c0 < rows; c0 += 16) {
+        uint32_t r[16];
+        tmem_ld16(tmem_w + (uint32_t)c0, r);
+        tmem_ld16_wait(r);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) ex[(half * W + c0 + j) * 128 + tl] = (int)r[j];
+      }
+    }
+    cluster_sync();
+    const int rank = (int)cluster_ctarank(), n = n0 + lane * 4;   // four columns per lane, a row per warp
+    float w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = n + e < N ? sw[n + e] : 0.f;
+    const bool whole = n + 4 <= N && !(N & 3) && !((uintptr_t)out & (4 * sizeof(T) - 1));
+    for (int row = rank + warp * S; row < rows; row += S * (S8_THREADS / 32)) {
+      const uint32_t at = tiles + (uint32_t)(row * 128 + lane * 4) * 4u;
+      int4 sum = make_int4(0, 0, 0, 0);
+#pragma unroll
+      for (int s = 0; s < S8_MOST_SPLITS; ++s) {
+        if (s >= S) break;
+        const int4 x = remote4(cluster_addr(at, s));
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+      }
+      const float a = sa[m0 + row], y[4] = {__int2float_rn(sum.x) * a * w[0], __int2float_rn(sum.y) * a * w[1],
+                                            __int2float_rn(sum.z) * a * w[2], __int2float_rn(sum.w) * a * w[3]};
+      T* const dst = out + (size_t)(m0 + row) * N + n;
+      if (whole) {
+        if constexpr (sizeof(T) == 4) {
+          *reinterpret_cast<float4*>(dst) = make_float4(y[0], y[1], y[2], y[3]);
+        } else {
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(y[0], y[1]), hi = __floats2bfloat162_rn(y[2], y[3]);
+          *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < N) dst[e] = from_f32<T>(y[e]);
+      }
+    }
+    cluster_sync();   // no CTA leaves while another one reads its integers
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -272,20 +327,33 @@ __global__ void __launch_bounds__(1024) quantize_rows_s8_kernel(const T* __restr
   const float s = __fdiv_rn(__uint_as_float(top), 127.f);
   const bool zero = s == 0.f || top >= 0x7F800000u;   // codes 0; the scale then shows an infinity or a NaN
   if (tid == 0) scale[blockIdx.x] = s;
+  // The quotient by a product with the reciprocal (off by 2^-22 of at most 127), rounded by adding 1.5 * 2^23; divided where it
+  // lies within 2^-13 of a tie, or where the scale is so small that its reciprocal is not one.
+  const bool tiny = s < 1e-37f;
+  const float inv = tiny ? 0.f : __frcp_rn(s);
   auto put = [&](int c, const float (&u)[8]) {
-    int8_t code[8];
+    uint32_t code[8];
+    bool divide = tiny;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      code[e] = zero ? (int8_t)0 : (int8_t)fminf(fmaxf(rintf(__fdiv_rn(u[e], s)), -127.f), 127.f);
+    for (int e = 0; e < 8; ++e) {
+      const float p = __fmul_rn(u[e], inv), t = __fadd_rn(p, 12582912.f);
+      divide |= !(fabsf(__fsub_rn(p, __fsub_rn(t, 12582912.f))) < 0.5f - 1.f / 8192.f);
+      code[e] = __float_as_uint(t) & 255u;
+    }
+    if (divide) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        code[e] = zero ? 0u : (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(u[e], s)), -127.f), 127.f) & 255u;
+    }
     if (c + 8 <= cols) {
       uint2 w;
-      w.x = (uint8_t)code[0] | (uint32_t)(uint8_t)code[1] << 8 | (uint32_t)(uint8_t)code[2] << 16 | (uint32_t)(uint8_t)code[3] << 24;
-      w.y = (uint8_t)code[4] | (uint32_t)(uint8_t)code[5] << 8 | (uint32_t)(uint8_t)code[6] << 16 | (uint32_t)(uint8_t)code[7] << 24;
+      w.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+      w.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
       *reinterpret_cast<uint2*>(dst + c) = w;
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (c + e < cols) dst[c + e] = code[e];
+        if (c + e < cols) dst[c + e] = (int8_t)code[e];
     }
   };
 #pragma unroll
@@ -300,7 +368,7 @@ __global__ void __launch_bounds__(1024) quantize_rows_s8_kernel(const T* __restr
 
 template <int BN, bool ONCE, typename T>
 cudaError_t launch_one_s8(const Launch& L, const CUtensorMap& tmW, const CUtensorMap& tmA, const float* sa, const float* sw,
-                          T* out, int* slabs, int M, int N, const GemmPlan& plan) {
+                          T* out, int M, int N, const GemmPlan& plan) {
   using SL = S8Layout<BN>;
   static DeviceOnce once;
   cudaError_t e0 = once.run([] {
@@ -310,8 +378,11 @@ cudaError_t launch_one_s8(const Launch& L, const CUtensorMap& tmW, const CUtenso
   if (e0 != cudaSuccess) return e0;
   const int stages = plan.stages < 2 ? 2 : plan.stages > SL::most() ? SL::most() : plan.stages;
   const dim3 grid(plan.m_tiles, (N + TILE_W - 1) / TILE_W, plan.S_max);
-  cudaError_t e = launch_k(L, gemm_s8_kernel<BN, ONCE, T>, grid, dim3(S8_THREADS), SL::total(stages), tmW, tmA, sa, sw, out,
-                           slabs, M, N, plan.num_kb, plan.upc, stages, L.d_status);
+  cudaError_t e = plan.S_max == 1 ? launch_k(L, gemm_s8_kernel<BN, ONCE, T>, grid, dim3(S8_THREADS), SL::total(stages), tmW, tmA,
+                                             sa, sw, out, M, N, plan.num_kb, plan.upc, stages, L.d_status)
+                                  : launch_k_cluster(L, gemm_s8_kernel<BN, ONCE, T>, grid, dim3(S8_THREADS), SL::total(stages),
+                                                     dim3(1, 1, plan.S_max), tmW, tmA, sa, sw, out, M, N, plan.num_kb, plan.upc,
+                                                     stages, L.d_status);
   L.count();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -334,15 +405,15 @@ cudaError_t launch_as(const Launch& L, const CUtensorMap& tmW, const CUtensorMap
       e = once ? launch_pair_form<256, true>(L, tmW, tmA, slab, M, N, plan.num_kb, plan, form, false)
                : launch_pair_form<256, false>(L, tmW, tmA, slab, M, N, plan.num_kb, plan, form, false);
   } else if (plan.BN == 32) {
-    e = once ? launch_one_s8<32, true, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan)
-             : launch_one_s8<32, false, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan);
+    e = once ? launch_one_s8<32, true, T>(L, tmW, tmA, sa, sw, out, M, N, plan)
+             : launch_one_s8<32, false, T>(L, tmW, tmA, sa, sw, out, M, N, plan);
   } else if (plan.BN == 64) {
-    e = once ? launch_one_s8<64, true, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan)
-             : launch_one_s8<64, false, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan);
+    e = once ? launch_one_s8<64, true, T>(L, tmW, tmA, sa, sw, out, M, N, plan)
+             : launch_one_s8<64, false, T>(L, tmW, tmA, sa, sw, out, M, N, plan);
   } else {
-    e = launch_one_s8<128, false, T>(L, tmW, tmA, sa, sw, out, part, M, N, plan);
+    e = launch_one_s8<128, false, T>(L, tmW, tmA, sa, sw, out, M, N, plan);
   }
-  if (e != cudaSuccess || !part) return e;
+  if (e != cudaSuccess || !part || !plan.pair) return e;
   Launch behind = L;
   behind.pdl = true;
   const dim3 grid((N + 255) / 256, std::min(M, 4096));
@@ -392,7 +463,7 @@ GemmPlan plan_gemm_s8(int M, int N, int K) {
     const long tiles = (long)p.m_tiles * n_tiles;
     const bool two_per_sm = p.BN == 128 || (p.BN == 64 && p.m_tiles > 1);
     S = two_per_sm ? (int)(2L * sms / tiles) : (int)((sms + tiles - 1) / tiles);
-    S = std::max(1, std::min(S, p.num_kb / 4));
+    S = std::max(1, std::min({S, p.num_kb / 4, S8_MOST_SPLITS}));
   }
   p.upc = (p.num_kb + S - 1) / S;
   p.S_max = (p.num_kb + p.upc - 1) / p.upc;
@@ -400,7 +471,7 @@ GemmPlan plan_gemm_s8(int M, int N, int K) {
 }
 
 size_t gemm_s8_scratch_bytes(int M, int N, const GemmPlan& plan) {
-  return plan.S_max > 1 ? (size_t)plan.S_max * M * N * 4 : 0;
+  return plan.pair && plan.S_max > 1 ? (size_t)plan.S_max * M * N * 4 : 0;   // one-tile CTAs add up in shared memory
 }
 
 cudaError_t launch_gemm_s8(const Launch& L, const int8_t* A, size_t lda, const float* sa, const int8_t* W, size_t ldw,

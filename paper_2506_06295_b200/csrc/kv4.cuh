@@ -71,6 +71,10 @@ cudaError_t launch_kv4_evict(const Launch& L, const Kv4& src, const float* weigh
 size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd);
 cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n,
                                  int H, const int32_t* lens, float* scratch, size_t scratch_floats);
+// kv4_umma.cu
+cudaError_t launch_kv4_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n, int H,
+                            const int32_t* lens, float* o_part, float2* ml_part, int S);
+cudaError_t set_wait_limit_kv4_umma(unsigned long long ns);
 cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                int a, int n, int H, const int32_t* lens);
 

@@ -17,6 +17,8 @@ namespace dllm {
 
 namespace {
 
+// rows per KV head above which the tcgen05 kernel is taken
+constexpr int KV4_UMMA_ROWS = 64;
 constexpr int KA_THREADS = 128, KA_ROWS = 16, KA_STAGES = 3;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -494,11 +496,25 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
   }
 }
 
-int attention_splits(int B, int a, int n, int H, int Hkv) {
-  const long base = (long)((a * (H / Hkv) + KA_ROWS - 1) / KA_ROWS) * Hkv * B, tiles = (n + KV4_KEYS - 1) / KV4_KEYS;
-  long S = 2L * sm_count() / base;          // two CTAs per SM are resident
-  S = std::min(S, (tiles + 3) / 4);         // a tile per warp at least
-  return (int)std::max(1L, std::min(S, 64L));
+// Which kernel, and how many ranges the keys are cut into.
+struct Kv4Plan {
+  bool umma;
+  int S;
+};
+Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
+  const long rows = (long)a * (H / Hkv), tiles = (n + KV4_KEYS - 1) / KV4_KEYS;
+  Kv4Plan p;
+  p.umma = rows > KV4_UMMA_ROWS;
+  long S;
+  if (p.umma) {
+    const long base = (rows + 255) / 256 * Hkv * B;    // one CTA per SM
+    S = std::min(sm_count() / base, (tiles + 3) / 4);
+  } else {
+    const long base = (rows + KA_ROWS - 1) / KA_ROWS * Hkv * B;
+    S = std::min(2L * sm_count() / base, (tiles + 3) / 4);   // two CTAs per SM; a tile per warp at least
+  }
+  p.S = (int)std::max(1L, std::min(S, 64L));
+  return p;
 }
 
 template <int HD>
@@ -510,16 +526,20 @@ cudaError_t attention_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, co
   });
   if (e != cudaSuccess) return e;
   const size_t total = (size_t)c.B * a * H, part = total * (HD + 2);
-  int S = attention_splits(c.B, a, n, H, c.Hkv);
-  if (S > 1) S = (int)std::min<size_t>(S, scratch ? scratch_floats / part : 0);
-  S = std::max(S, 1);
+  const Kv4Plan plan = plan_kv4(c.B, a, n, H, c.Hkv);
+  int S = plan.S;
+  if (S > 1) S = std::max(1, (int)std::min<size_t>(S, scratch ? scratch_floats / part : 0));
   float* const o_part = scratch;
   float2* const ml_part = reinterpret_cast<float2*>(scratch + (S > 1 ? (size_t)S * total * HD : 0));
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
   const dim3 grid((a * (H / c.Hkv) + KA_ROWS - 1) / KA_ROWS, c.Hkv, c.B * S);
-  e = launch_k(L, kv4_attn_kernel<HD>, grid, dim3(KA_THREADS), KaSmem<HD>::TOTAL, q, ldq, c, lens, o, lse, o_part, ml_part, a, n,
-               H, S, scale_log2);
-  L.count();
+  if (plan.umma) {
+    e = launch_kv4_umma(L, q, ldq, c, o, lse, a, n, H, lens, o_part, ml_part, S);
+  } else {
+    e = launch_k(L, kv4_attn_kernel<HD>, grid, dim3(KA_THREADS), KaSmem<HD>::TOTAL, q, ldq, c, lens, o, lse, o_part, ml_part, a,
+                 n, H, S, scale_log2);
+    L.count();
+  }
   if (e != cudaSuccess || S == 1) return e != cudaSuccess ? e : cudaGetLastError();
   Launch behind = L;
   behind.pdl = true;
@@ -532,7 +552,7 @@ cudaError_t attention_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, co
 }  // namespace
 
 size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd) {
-  const int S = attention_splits(B, a, n, H, Hkv);
+  const int S = plan_kv4(B, a, n, H, Hkv).S;
   return S > 1 ? (size_t)S * B * a * H * (hd + 2) : 0;
 }
 

@@ -11,55 +11,122 @@
 #include <algorithm>
 
 #include "kv4.cuh"
+#include "tma.cuh"
 
 namespace dllm {
 
 namespace {
 
-// Eight elements of a row.  VEC: the row starts on a 16-byte boundary.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
+// Sixteen elements of a row and, over the LANES lanes that share it, the row's least and largest one (NaN where there is a
+// NaN).  VEC: the row starts on a 16-byte boundary.  bf16: two numbers per instruction, and the pair (least, -largest) goes
+// through the shuffles as one word.
+template <int LANES, bool VEC>
+__device__ __forceinline__ void load_row(const float* p, float (&x)[16], float& lo, float& hi) {
   if constexpr (VEC) {
-    Vec8<T>::load(p, v);
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(p + i);
+      x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_f32<T>(p[i]);
+    for (int i = 0; i < 16; ++i) x[i] = p[i];
   }
-}
-
-// The codes of eight elements per lane, LANES lanes per row, and the row's pair.
-template <int LANES>
-__device__ __forceinline__ uint32_t encode8(const float (&x)[8], uint32_t& pair) {
-  float lo = x[0], hi = x[0], odd = 0.f;
+  auto least = [](float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+  };
+  float top = -x[0];
+  lo = x[0];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, x[i]);
-    hi = fmaxf(hi, x[i]);
-    odd += x[i] - x[i];   // 0, or NaN for an infinity or a NaN
+  for (int i = 1; i < 16; ++i) {
+    lo = least(lo, x[i]);
+    top = least(top, -x[i]);
   }
 #pragma unroll
   for (int o = LANES / 2; o > 0; o >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    odd += __shfl_xor_sync(0xffffffffu, odd, o);
+    lo = least(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+    top = least(top, __shfl_xor_sync(0xffffffffu, top, o));
   }
+  hi = -top;
+}
+template <int LANES, bool VEC>
+__device__ __forceinline__ void load_row(const __nv_bfloat16* p, float (&x)[16], float& lo, float& hi) {
+  uint32_t w[8];
+  if constexpr (VEC) {
+    const uint4 a = *reinterpret_cast<const uint4*>(p), b = *reinterpret_cast<const uint4*>(p + 8);
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      w[i] = (uint32_t)__bfloat16_as_ushort(p[2 * i]) | (uint32_t)__bfloat16_as_ushort(p[2 * i + 1]) << 16;
+  }
+  auto as2 = [](uint32_t u) { return *reinterpret_cast<const __nv_bfloat162*>(&u); };
+  __nv_bfloat162 least = as2(w[0]), most = as2(w[0]);
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    least = __hmin2_nan(least, as2(w[i]));
+    most = __hmax2_nan(most, as2(w[i]));
+  }
+  __nv_bfloat162 both = __hmin2_nan(__lows2bfloat162(least, __hneg2(most)), __highs2bfloat162(least, __hneg2(most)));
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1)
+    both = __hmin2_nan(both, as2(__shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&both), o)));
+  lo = __low2float(both);
+  hi = -__high2float(both);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+
+// The codes of a lane's sixteen elements of a row with least `lo` and largest `hi`, and the row's pair.
+__device__ __forceinline__ uint2 encode16(const float (&x)[16], float lo, float hi, uint32_t& pair) {
   const __nv_bfloat16 lo_b = __float2bfloat16_rn(lo);
   __nv_bfloat16 step_b = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
   if (__bfloat162float(step_b) == 0.f) step_b = __float2bfloat16_rn(1.f);
   const float lo_f = __bfloat162float(lo_b), step = __bfloat162float(step_b);
-  uint32_t w = 0;
+  // rint of the quotient by a product with the reciprocal, rounded by adding 1.5 * 2^23.  u is the quotient's nearest integer
+  // where what is left, e = d - u * step (exact: u * step has 12 bits, and d is at least half a step wherever u is not 0), is
+  // less than half a step; otherwise (a tie, or the product fell on a tie's other side) it is divided, and so are the rows
+  // whose quotients may leave 0..15 (fp32 rows whose offset was rounded up or down by more than a step's share).  The
+  // quotient's own rounding never makes a tie: half steps are exact, and the nearest other d is further off than half a unit
+  // of the quotient.  Four codes add up to 16 bits in fp32.  (Store of 16 x 1536 tokens of 32 heads, bf16: with a division per
+  // element and eight elements per lane 310 us; FIGURE.)
+  const float inv = __frcp_rn(step), half = 0.5f * step;
+  bool divide = !(lo >= lo_f) || !(__fsub_rn(hi, lo_f) <= 15.4f * step);
+  uint32_t q[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float u = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], lo_f), step)), 0.f), 15.f);
-    w |= (uint32_t)u << (4 * i);
+  for (int i = 0; i < 4; ++i) {
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 3; k >= 0; --k) {
+      const float d = __fsub_rn(x[4 * i + k], lo_f);
+      const float u = __fsub_rn(__fadd_rn(__fmul_rn(d, inv), 12582912.f), 12582912.f);
+      divide |= !(fabsf(__fmaf_rn(-u, step, d)) < half);
+      sum = k == 3 ? u : __fmaf_rn(sum, 16.f, u);
+    }
+    q[i] = (uint32_t)sum;
+  }
+  if (divide) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      q[i] = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float u = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[4 * i + k], lo_f), step)), 0.f), 15.f);
+        q[i] |= (uint32_t)u << (4 * k);
+      }
+    }
   }
   pair = (uint32_t)__bfloat16_as_ushort(step_b) | ((uint32_t)__bfloat16_as_ushort(lo_b) << 16);
-  // also where the spread overflows: no step stands for it
-  if (odd != 0.f || !(step < INFINITY) || !(fabsf(lo_f) < INFINITY)) {
+  if (!(step < INFINITY) || !(fabsf(lo_f) < INFINITY)) {   // an infinity, a NaN, or a spread that no step stands for
     pair = 0x7FC07FC0u;
-    w = 0;
+    return make_uint2(0, 0);
   }
-  return w;
+  return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
 }
 
 // A CTA takes `per` consecutive source rows (of all sequences together), LANES lanes per head of a row.  Rows whose
@@ -70,7 +137,7 @@ template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(ST_THREADS) kv4_store_kernel(Kv4 c, const T* __restrict__ k, const T* __restrict__ v,
                                                                size_t ldk, size_t ldv, int a, int rows, int per,
                                                                const int32_t* __restrict__ pos, int start) {
-  constexpr int LANES = HD / 8;
+  constexpr int LANES = HD / 16;
   __shared__ int at[ST_ROWS];          // where row r goes, -1: nowhere
   __shared__ uint32_t bits[32];
   pdl_wait();
@@ -100,15 +167,15 @@ __global__ void __launch_bounds__(ST_THREADS) kv4_store_kernel(Kv4 c, const T* _
     const int i = i0 + tid / LANES;
     const bool live = i < heads;
     const int r = live ? i / c.Hkv : 0, h = live ? i - r * c.Hkv : 0;
-    float x[8], y[8];
-    load8<T, VEC>(k + (size_t)(r0 + r) * ldk + h * HD + lane * 8, x);
-    load8<T, VEC>(v + (size_t)(r0 + r) * ldv + h * HD + lane * 8, y);
+    float x[16], y[16], x_lo, x_hi, y_lo, y_hi;
+    load_row<LANES, VEC>(k + (size_t)(r0 + r) * ldk + h * HD + lane * 16, x, x_lo, x_hi);
+    load_row<LANES, VEC>(v + (size_t)(r0 + r) * ldv + h * HD + lane * 16, y, y_lo, y_hi);
     uint32_t kpair, vpair;
-    const uint32_t kw = encode8<LANES>(x, kpair), vw = encode8<LANES>(y, vpair);
+    const uint2 kw = encode16(x, x_lo, x_hi, kpair), vw = encode16(y, y_lo, y_hi, vpair);
     if (!live || at[r] < 0) continue;
     const size_t row = ((size_t)((r0 + r) / a) * c.Hkv + h) * c.cap + at[r];
-    reinterpret_cast<uint32_t*>(c.k)[row * LANES + lane] = kw;
-    reinterpret_cast<uint32_t*>(c.v)[row * LANES + lane] = vw;
+    reinterpret_cast<uint2*>(c.k)[row * LANES + lane] = kw;
+    reinterpret_cast<uint2*>(c.v)[row * LANES + lane] = vw;
     if (lane == 0) {
       c.kp[row] = kpair;
       c.vp[row] = vpair;
@@ -116,44 +183,58 @@ __global__ void __launch_bounds__(ST_THREADS) kv4_store_kernel(Kv4 c, const T* _
   }
 }
 
-// One word of eight codes per thread and trip; blockIdx.y: K or V.
+// A thread has 16 bytes of output (four numbers in fp32, eight in bf16) of one token per trip, so that a warp's stores are
+// whole lines: `per` threads lie along the units of a token (all of them, or 256 where there are more), 256 / per tokens side
+// by side.  blockIdx.y: sequence, blockIdx.z: K or V.
 template <typename T, int HD, bool VEC>
 __global__ void __launch_bounds__(256) kv4_load_kernel(Kv4 c, int n, const int32_t* __restrict__ lens, T* __restrict__ k,
-                                                       T* __restrict__ v) {
-  constexpr int LANES = HD / 8;
+                                                       T* __restrict__ v, int per) {
+  constexpr int E = 16 / sizeof(T), UNITS = HD / E, DEEP = 4;   // numbers per thread, units per head, tokens on their way
+  using Codes = std::conditional_t<E == 8, uint32_t, uint16_t>;
   pdl_wait();
   pdl_trigger();
-  const bool of_v = blockIdx.y != 0;
-  T* out = of_v ? v : k;
-  if (!out) return;
-  const uint32_t* codes = reinterpret_cast<const uint32_t*>(of_v ? c.v : c.k);
-  const uint32_t* pairs = of_v ? c.vp : c.kp;
-  const size_t words = (size_t)c.B * n * c.Hkv * LANES;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) {
-    const int lane = (int)(i % LANES);
-    const size_t head = i / LANES, token = head / c.Hkv;
-    const int h = (int)(head - token * c.Hkv), b = (int)(token / n), j = (int)(token - (size_t)b * n);
-    float x[8];
-    if (lens && j >= lens[b]) {
+  const bool of_v = blockIdx.z != 0;
+  T* const out = of_v ? v : k;
+  const int side = 256 / per, mine = (int)threadIdx.x / per, units = c.Hkv * UNITS, blocks = (units + per - 1) / per;
+  const int w = (int)(blockIdx.x % blocks) * per + (int)threadIdx.x - mine * per;
+  if (!out || mine >= side || w >= units) return;
+  const int b = blockIdx.y, len = lens ? lens[b] : n, j0 = (int)(blockIdx.x / blocks) * (DEEP * side) + mine;
+  const size_t plane = ((size_t)b * c.Hkv + w / UNITS) * c.cap;
+  const Codes* const src = reinterpret_cast<const Codes*>(of_v ? c.v : c.k) + plane * UNITS + w % UNITS;
+  const uint32_t* const par = (of_v ? c.vp : c.kp) + plane;
+  T* const dst = out + ((size_t)b * n * units + w) * E;
+  uint32_t u[DEEP], p[DEEP];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    } else {
-      const size_t row = ((size_t)b * c.Hkv + h) * c.cap + j;
-      const uint32_t w = codes[row * LANES + lane], p = pairs[row];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = fmaf((float)((w >> (4 * e)) & 15u), kv4_step(p), kv4_lo(p));
+  for (int i = 0; i < DEEP; ++i) {
+    const int j = j0 + i * side;
+    u[i] = p[i] = 0;     // code 0, step 0, lo 0
+    if (j < n && j < len) {
+      u[i] = src[(size_t)j * UNITS];
+      p[i] = par[j];
     }
-    if constexpr (VEC) {
-      Vec8<T>::store(out + i * 8, x);
-    } else {
+  }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) out[i * 8 + e] = from_f32<T>(x[e]);
+  for (int i = 0; i < DEEP; ++i) {
+    const int j = j0 + i * side;
+    if (j >= n) break;
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = fmaf((float)((u[i] >> (4 * e)) & 15u), kv4_step(p[i]), kv4_lo(p[i]));
+    T* const to = dst + (size_t)j * units * E;
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) to[e] = from_f32<T>(x[e]);
+    } else if constexpr (E == 4) {
+      *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+      Vec8<T>::store(to, x);
     }
   }
 }
 
 // ---------------------------------------------------------------- eviction
-constexpr int EV_THREADS = 1024, EV_PER = 8, EV_BINS = 2048;
+constexpr int EV_THREADS = 512, EV_PER = 8, EV_BINS = 2048, EV_CLUSTER = 8;
+constexpr int EV_SMEM_KEYS = 40 * 1024;   // ordered weights that one CTA keeps
 
 // Order of the weights as unsigned numbers; a NaN comes last, -0 and 0 are equal.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -172,100 +253,163 @@ __device__ __forceinline__ int block_scan(int v, int* warps, int& total) {   // 
   __syncthreads();
   if (lane == 31) warps[w] = s;
   __syncthreads();
-  int before = 0, all = 0;
-  {
-    int t = warps[lane];
+  int t = lane < EV_THREADS / 32 ? warps[lane] : 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, t, o);
-      if (lane >= o) t += u;
-    }
-    all = __shfl_sync(0xffffffffu, t, 31);
-    before = __shfl_sync(0xffffffffu, t, w == 0 ? 0 : w - 1);
-    if (w == 0) before = 0;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, t, o);
+    if (lane >= o) t += u;
   }
-  total = all;
-  return before + s - v;
+  total = __shfl_sync(0xffffffffu, t, 31);
+  const int before = __shfl_sync(0xffffffffu, t, max(w - 1, 0));
+  return (w == 0 ? 0 : before) + s - v;
+}
+// 16 bytes from the same place of shared memory in the cluster's CTA `rank`
+__device__ __forceinline__ int4 remote4(const int* p, uint32_t rank) {
+  int4 r;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "r"(cluster_addr(smem_u32(p), rank)));
+  return r;
 }
 
-// One CTA per (sequence, KV head).  The smallest weight that stays is found digit by digit (11, 11 and 10 bits of the
-// ordered weight, a histogram each), then one pass in order writes the places.
+// A cluster of one or eight CTAs per (sequence, KV head), each with its share of the keys (multiples of EV_PER, kept in
+// shared memory as ordered numbers where they fit).  The smallest weight that stays is found digit by digit (11, 11 and 10
+// bits, a histogram each; every CTA adds up all of the cluster's), then each CTA counts its share, and one pass in order
+// writes the places.  Every weight is read once; what is left is the latency of a dozen barriers.
 __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __restrict__ weight, int n, int cap, int Hkv,
                                                                 int keep, int first, int last,
-                                                                const int32_t* __restrict__ lens, int dst_cap,
-                                                                float* __restrict__ dst_weight, int32_t* __restrict__ index,
-                                                                int32_t* __restrict__ new_lens) {
-  __shared__ int hist[EV_BINS];
+                                                                const int32_t* __restrict__ lens, int share, int kept_in_smem,
+                                                                int dst_cap, float* __restrict__ dst_weight,
+                                                                int32_t* __restrict__ index, int32_t* __restrict__ new_lens) {
+  extern __shared__ __align__(16) uint32_t keys[];
+  __shared__ __align__(16) int hist[EV_BINS];
+  __shared__ __align__(16) int counts[4];
   __shared__ int warps[32];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
+  __shared__ int found[2];
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, bh = blockIdx.x, b = bh / Hkv;
+  const int tid = threadIdx.x, rank = (int)cluster_ctarank();
+  const bool alone = share >= cap;
+  const int bh = alone ? blockIdx.x : blockIdx.x / EV_CLUSTER, b = bh / Hkv;
   const float* w = weight + (size_t)bh * cap;
   const int len = lens ? min(max(lens[b], 0), n) : n, kept = min(len, keep);
   const bool choose = len > keep;                       // else every key stays
   const int lo = choose ? first : len, hi = choose ? len - last : len;   // keys lo .. hi - 1 compete
+  const int j_lo = min(rank * share, len), j_hi = min(j_lo + share, len);
   int need = choose ? keep - first - last : 0;          // for this many places
   uint32_t prefix = 0, mask = 0;                        // digits of the threshold found so far
+  auto sync_all = [&] {
+    if (alone) __syncthreads();
+    else cluster_sync();
+  };
+  auto four = [&](int j, uint32_t (&k)[4]) {            // the ordered weights of keys j .. j + 3 (j a multiple of 4)
+    if (kept_in_smem) {
+      const uint4 x = *reinterpret_cast<const uint4*>(keys + (j - j_lo));
+      k[0] = x.x; k[1] = x.y; k[2] = x.z; k[3] = x.w;
+    } else {
+      const float4 x = *reinterpret_cast<const float4*>(w + j);
+      k[0] = weight_key(x.x); k[1] = weight_key(x.y); k[2] = weight_key(x.z); k[3] = weight_key(x.w);
+    }
+  };
+  if (kept_in_smem && choose) {
+#pragma unroll 2
+    for (int j = j_lo + tid * 4; j < j_hi; j += EV_THREADS * 4) {
+      const float4 x = *reinterpret_cast<const float4*>(w + j);
+      *reinterpret_cast<uint4*>(keys + (j - j_lo)) =
+          make_uint4(weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w));
+    }
+  }
   if (need > 0) {
-    for (int shift = 21; ; ) {
+    for (int shift = 21;;) {
       for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
       __syncthreads();
       const int bins = shift == 0 ? 1024 : 2048;
-      for (int j0 = lo / 4 * 4 + tid * 4; j0 < hi; j0 += EV_THREADS * 4) {
-        const float4 x = *reinterpret_cast<const float4*>(w + j0);
-        const float e[4] = {x.x, x.y, x.z, x.w};
+      for (int j = j_lo + tid * 4; j < j_hi; j += EV_THREADS * 4) {
+        uint32_t k[4];
+        four(j, k);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t key = weight_key(e[q]);
-          if (j0 + q >= lo && j0 + q < hi && (key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1);
+        for (int q = 0; q < 4; ++q)
+          if (j + q >= lo && j + q < hi && (k[q] & mask) == prefix) atomicAdd(&hist[(k[q] >> shift) & (bins - 1)], 1);
+      }
+      sync_all();
+      // the bin, counted from the largest, in which the last place goes: four bins per thread
+      static_assert(EV_BINS == 4 * EV_THREADS, "four bins per thread");
+      const int at = EV_BINS - 4 - 4 * tid;
+      int4 c = alone ? *reinterpret_cast<const int4*>(&hist[at]) : make_int4(0, 0, 0, 0);
+      if (!alone) {
+#pragma unroll
+        for (int r = 0; r < EV_CLUSTER; ++r) {
+          const int4 x = remote4(&hist[at], r);
+          c.x += x.x; c.y += x.y; c.z += x.z; c.w += x.w;
         }
       }
-      __syncthreads();
-      // the bin, counted from the largest, in which the last place goes: bins in pairs per thread, largest first
-      const int top = EV_BINS - 1 - 2 * tid, c0 = hist[top], c1 = hist[top - 1];
-      int total;
-      const int before = block_scan(c0 + c1, warps, total);
-      if (before < need && need <= before + c0) {
-        s_prefix = (uint32_t)top;
-        s_need = need - before;
-      } else if (before + c0 < need && need <= before + c0 + c1) {
-        s_prefix = (uint32_t)(top - 1);
-        s_need = need - before - c0;
+      int total, before = block_scan(c.x + c.y + c.z + c.w, warps, total);
+      const int bin[4] = {c.w, c.z, c.y, c.x};   // largest first
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (before < need && need <= before + bin[i]) {
+          found[0] = at + 3 - i;
+          found[1] = need - before;
+        }
+        before += bin[i];
       }
-      __syncthreads();
-      prefix |= s_prefix << shift;
+      sync_all();   // and no CTA clears a histogram that another one still reads
+      prefix |= (uint32_t)found[0] << shift;
       mask |= (uint32_t)(bins - 1) << shift;
-      need = s_need;
-      __syncthreads();
+      need = found[1];
       if (shift == 0) break;
       shift = shift == 21 ? 10 : 0;
     }
   }
-  // `need` of the keys equal to `prefix` stay, the first ones
-  int32_t* idx = index + (size_t)bh * keep;
-  float* dw = dst_weight + (size_t)bh * dst_cap;
-  int sure_before = 0, ties_before = 0;
-  for (int base = 0; base < len; base += EV_THREADS * EV_PER) {
-    const int j0 = base + tid * EV_PER;
-    float e[EV_PER];
-    uint32_t sure = 0, tie = 0;
-#pragma unroll
-    for (int q = 0; q < EV_PER; q += 4) {
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (j0 + q < len) x = *reinterpret_cast<const float4*>(w + j0 + q);
-      e[q] = x.x; e[q + 1] = x.y; e[q + 2] = x.z; e[q + 3] = x.w;
+  __syncthreads();
+  // `need` of the keys equal to `prefix` stay, the first ones.  sure: stays whatever the ties do.
+  auto eight = [&](int j0, uint32_t& sure, uint32_t& tie) {
+    sure = tie = 0;
+    if (j0 >= j_hi) return;
+    uint32_t k[8];
+    if (choose) {
+      uint32_t (&k0)[4] = *reinterpret_cast<uint32_t(*)[4]>(&k[0]);
+      uint32_t (&k1)[4] = *reinterpret_cast<uint32_t(*)[4]>(&k[4]);
+      four(j0, k0);
+      four(j0 + 4, k1);
     }
 #pragma unroll
     for (int q = 0; q < EV_PER; ++q) {
       const int j = j0 + q;
-      if (j >= len) continue;
-      const uint32_t key = weight_key(e[q]);
+      if (j >= j_hi) continue;
       const bool forced = j < lo || j >= hi;
-      if (forced || (mask && key > prefix)) sure |= 1u << q;
-      else if (mask && key == prefix) tie |= 1u << q;
+      if (forced || (mask && k[q] > prefix)) sure |= 1u << q;
+      else if (mask && k[q] == prefix) tie |= 1u << q;
     }
+  };
+  int sure_before = 0, ties_before = 0;
+  if (!alone) {   // what the CTAs with earlier keys hold
+    int sures = 0, ties = 0;
+    for (int j0 = j_lo + tid * EV_PER; j0 < j_hi; j0 += EV_THREADS * EV_PER) {
+      uint32_t s, t;
+      eight(j0, s, t);
+      sures += __popc(s);
+      ties += __popc(t);
+    }
+    int total;
+    block_scan(sures, warps, total);
+    if (tid == 0) counts[0] = total;
+    block_scan(ties, warps, total);
+    if (tid == 0) counts[1] = total;
+    cluster_sync();
+    for (int r = 0; r < rank; ++r) {
+      const int4 x = remote4(counts, r);
+      sure_before += x.x;
+      ties_before += x.y;
+    }
+    cluster_sync();   // no CTA leaves while another one reads its counts
+  }
+  int32_t* idx = index + (size_t)bh * keep;
+  float* dw = dst_weight + (size_t)bh * dst_cap;
+  for (int base = j_lo; base < j_hi; base += EV_THREADS * EV_PER) {
+    const int j0 = base + tid * EV_PER;
+    uint32_t sure, tie;
+    eight(j0, sure, tie);
     int total;
     const int scan = block_scan((__popc(sure) << 16) | __popc(tie), warps, total);
     int s = sure_before + (scan >> 16), t = ties_before + (scan & 0xFFFF);
@@ -275,7 +419,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __r
       if (is_sure || (is_tie && t < need)) {
         const int slot = s + min(t, need);
         idx[slot] = j0 + q;
-        dw[slot] = e[q];
+        dw[slot] = w[j0 + q];
       }
       s += is_sure;
       t += is_tie;
@@ -283,11 +427,13 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __r
     sure_before += total >> 16;
     ties_before += total & 0xFFFF;
   }
-  for (int i = kept + tid; i < dst_cap; i += EV_THREADS) {
-    if (i < keep) idx[i] = -1;
-    dw[i] = 0.f;
+  if (rank == 0) {
+    for (int i = kept + tid; i < dst_cap; i += EV_THREADS) {
+      if (i < keep) idx[i] = -1;
+      dw[i] = 0.f;
+    }
+    if (tid == 0 && bh % Hkv == 0) new_lens[b] = kept;
   }
-  if (tid == 0 && bh % Hkv == 0) new_lens[b] = kept;
 }
 
 // The rows that stay, 16 bytes per thread: HD / 32 threads for K and as many for V, the first of each with the pair.
@@ -311,7 +457,8 @@ __global__ void __launch_bounds__(256) kv4_gather_kernel(Kv4 src, Kv4 dst, const
 template <typename T, int HD>
 cudaError_t store_as(const Launch& L, const Kv4& c, const T* k, const T* v, size_t ldk, size_t ldv, int a, const int32_t* pos,
                      int start) {
-  const int rows = c.B * a, per = std::max(1, std::min(ST_ROWS, rows / (4 * sm_count())));
+  // five CTAs to an SM; enough of them that a last round of a few costs little
+  const int rows = c.B * a, per = std::max(1, std::min(pos ? ST_ROWS : 4, rows / (16 * sm_count())));
   const bool vec = !(((uintptr_t)k | (uintptr_t)v) & 15) && !((ldk | ldv) * sizeof(T) & 15);
   const dim3 grid((rows + per - 1) / per);
   cudaError_t e = vec ? launch_k(L, kv4_store_kernel<T, HD, true>, grid, dim3(ST_THREADS), 0, c, k, v, ldk, ldv, a, rows, per,
@@ -324,11 +471,11 @@ cudaError_t store_as(const Launch& L, const Kv4& c, const T* k, const T* v, size
 
 template <typename T, int HD>
 cudaError_t load_as(const Launch& L, const Kv4& c, int n, const int32_t* lens, T* k, T* v) {
-  const size_t words = (size_t)c.B * n * c.Hkv * (HD / 8);
-  const dim3 grid((unsigned)std::min<size_t>((words + 255) / 256, (size_t)sm_count() * 16), 2);
+  const int units = c.Hkv * (HD / (16 / (int)sizeof(T))), per = std::min(units, 256), side = 256 / per;
+  const dim3 grid((unsigned)((n + 4 * side - 1) / (4 * side) * ((units + per - 1) / per)), c.B, 2);
   const bool vec = !(((uintptr_t)k | (uintptr_t)v) & 15);
-  cudaError_t e = vec ? launch_k(L, kv4_load_kernel<T, HD, true>, grid, dim3(256), 0, c, n, lens, k, v)
-                      : launch_k(L, kv4_load_kernel<T, HD, false>, grid, dim3(256), 0, c, n, lens, k, v);
+  cudaError_t e = vec ? launch_k(L, kv4_load_kernel<T, HD, true>, grid, dim3(256), 0, c, n, lens, k, v, per)
+                      : launch_k(L, kv4_load_kernel<T, HD, false>, grid, dim3(256), 0, c, n, lens, k, v, per);
   L.count();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -358,8 +505,21 @@ cudaError_t launch_kv4_load(const Launch& L, const Kv4& c, int n, const int32_t*
 cudaError_t launch_kv4_evict(const Launch& L, const Kv4& src, const float* weight, int n, int keep, int first, int last,
                              const int32_t* lens, const Kv4& dst, float* dst_weight, int32_t* index, int32_t* new_lens) {
   const int heads = src.B * src.Hkv;
-  cudaError_t e = launch_k(L, kv4_select_kernel, dim3(heads), dim3(EV_THREADS), 0, weight, n, src.cap, src.Hkv, keep, first,
-                           last, lens, dst.cap, dst_weight, index, new_lens);
+  static DeviceOnce once;
+  cudaError_t e = once.run([] {
+    return cudaFuncSetAttribute(kv4_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_SMEM_KEYS * 4);
+  });
+  if (e != cudaSuccess) return e;
+  // eight CTAs per head where one would make more than two trips over its keys, unless there are CTAs enough
+  const bool alone = n <= 2 * EV_THREADS * EV_PER || heads > 2 * sm_count();
+  const int share = alone ? src.cap : (n + EV_CLUSTER * EV_PER - 1) / (EV_CLUSTER * EV_PER) * EV_PER;
+  const int mine = alone ? (n + EV_PER - 1) / EV_PER * EV_PER : share, in_smem = mine <= EV_SMEM_KEYS;
+  const size_t smem = in_smem ? (size_t)mine * 4 : 0;
+  e = alone ? launch_k(L, kv4_select_kernel, dim3(heads), dim3(EV_THREADS), smem, weight, n, src.cap, src.Hkv, keep, first,
+                       last, lens, share, in_smem, dst.cap, dst_weight, index, new_lens)
+            : launch_k_cluster(L, kv4_select_kernel, dim3(heads * EV_CLUSTER), dim3(EV_THREADS), smem, dim3(EV_CLUSTER, 1, 1),
+                               weight, n, src.cap, src.Hkv, keep, first, last, lens, share, in_smem, dst.cap, dst_weight, index,
+                               new_lens);
   L.count();
   if (e != cudaSuccess) return e;
   const int per = src.hd / 16;

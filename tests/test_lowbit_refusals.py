@@ -37,11 +37,11 @@ def test_quantize_rows(dllm):
 
 
 def test_gemm(dllm):
-    need = dllm.lib.dllm_gemm_s8_scratch_bytes(3, 256, 4096)
-    assert need > 0 and dllm.lib.dllm_gemm_s8_scratch_bytes(0, 256, 4096) == 0
-    good = dict(A=P, lda=4096, sa=P, W=P, ldw=4096, sw=P, C=P, dt=0, M=3, N=256, K=4096, s=P, sb=need)
+    need = dllm.lib.dllm_gemm_s8_scratch_bytes(200, 3584, 18944)
+    assert need > 0 and dllm.lib.dllm_gemm_s8_scratch_bytes(0, 256, 4096) == 0 == dllm.lib.dllm_gemm_s8_scratch_bytes(3, 256, 4096)
+    good = dict(A=P, lda=18944, sa=P, W=P, ldw=18944, sw=P, C=P, dt=0, M=200, N=3584, K=18944, s=P, sb=need)
     for bad in (dict(A=None), dict(sa=None), dict(W=None), dict(sw=None), dict(C=None), dict(M=0), dict(N=0), dict(K=0),
-                dict(lda=4088), dict(lda=4080), dict(ldw=4088), dict(ldw=4080), dict(A=P + 8), dict(W=P + 4), dict(dt=3), dict(s=None),
+                dict(lda=18952), dict(lda=18928), dict(ldw=18952), dict(ldw=18928), dict(A=P + 8), dict(W=P + 4), dict(dt=3), dict(s=None),
                 dict(sb=need - 1), dict(s=P + 8), dict(C=P + 2)):
         a = {**good, **bad}
         refused(dllm, "dllm_gemm_s8", a["A"], a["lda"], a["sa"], a["W"], a["ldw"], a["sw"], a["C"], a["dt"], a["M"], a["N"], a["K"],
