@@ -88,45 +88,35 @@ __device__ __forceinline__ uint2 encode16(const float (&x)[16], float lo, float 
   __nv_bfloat16 step_b = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
   if (__bfloat162float(step_b) == 0.f) step_b = __float2bfloat16_rn(1.f);
   const float lo_f = __bfloat162float(lo_b), step = __bfloat162float(step_b);
-  // rint of the quotient by a product with the reciprocal, rounded by adding 1.5 * 2^23.  u is the quotient's nearest integer
-  // where what is left, e = d - u * step (exact: u * step has 12 bits, and d is at least half a step wherever u is not 0), is
-  // less than half a step; otherwise (a tie, or the product fell on a tie's other side) it is divided, and so are the rows
-  // whose quotients may leave 0..15 (fp32 rows whose offset was rounded up or down by more than a step's share).  The
-  // quotient's own rounding never makes a tie: half steps are exact, and the nearest other d is further off than half a unit
-  // of the quotient.  Four codes add up to 16 bits in fp32.  (Store of 16 x 1536 tokens of 32 heads, bf16: with a division per
-  // element and eight elements per lane 310 us; FIGURE.)
-  const float inv = __frcp_rn(step), half = 0.5f * step;
-  bool divide = !(lo >= lo_f) || !(__fsub_rn(hi, lo_f) <= 15.4f * step);
+  // The quotient by a product with the reciprocal and one correction, rounded by adding 1.5 * 2^23.  The corrected product is
+  // off by 2^-46 of itself before it is rounded, so it meets a tie exactly where the quotient does (half steps are exact, and
+  // the nearest other d is further off than half a unit of the quotient): this is rint of the IEEE quotient without its cost.
+  // Rows that it does not hold for are divided: tiny steps, and fp32 rows whose offset was rounded by so much that quotients
+  // leave 0..15.  Four codes add up to 16 bits in fp32.  (Store of 16 x 1536 tokens of 32 heads, bf16, 78 us of bytes: 310 us
+  // with a division per element, FIGURE now.)
+  const float inv = __frcp_rn(step);
+  float u[16];
+  if (lo >= lo_f && __fsub_rn(hi, lo_f) <= 15.4f * step && step > 1e-30f) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float d = __fsub_rn(x[i], lo_f), p = __fmul_rn(d, inv);
+      u[i] = __fsub_rn(__fadd_rn(__fmaf_rn(__fmaf_rn(-p, step, d), inv, p), 12582912.f), 12582912.f);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[i], lo_f), step)), 0.f), 15.f);
+  }
   uint32_t q[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 3; k >= 0; --k) {
-      const float d = __fsub_rn(x[4 * i + k], lo_f);
-      const float u = __fsub_rn(__fadd_rn(__fmul_rn(d, inv), 12582912.f), 12582912.f);
-      divide |= !(fabsf(__fmaf_rn(-u, step, d)) < half);
-      sum = k == 3 ? u : __fmaf_rn(sum, 16.f, u);
-    }
-    q[i] = (uint32_t)sum;
-  }
-  if (divide) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      q[i] = 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float u = fminf(fmaxf(rintf(__fdiv_rn(__fsub_rn(x[4 * i + k], lo_f), step)), 0.f), 15.f);
-        q[i] |= (uint32_t)u << (4 * k);
-      }
-    }
-  }
+  for (int i = 0; i < 4; ++i)
+    q[i] = __float_as_uint(__fadd_rn(__fmaf_rn(__fmaf_rn(__fmaf_rn(u[4 * i + 3], 16.f, u[4 * i + 2]), 16.f, u[4 * i + 1]), 16.f, u[4 * i]),
+                                     12582912.f));
   pair = (uint32_t)__bfloat16_as_ushort(step_b) | ((uint32_t)__bfloat16_as_ushort(lo_b) << 16);
   if (!(step < INFINITY) || !(fabsf(lo_f) < INFINITY)) {   // an infinity, a NaN, or a spread that no step stands for
     pair = 0x7FC07FC0u;
     return make_uint2(0, 0);
   }
-  return make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+  return make_uint2(__byte_perm(q[0], q[1], 0x5410), __byte_perm(q[2], q[3], 0x5410));
 }
 
 // A CTA takes `per` consecutive source rows (of all sequences together), LANES lanes per head of a row.  Rows whose

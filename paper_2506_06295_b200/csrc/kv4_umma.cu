@@ -44,6 +44,19 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
   return d;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// 16 columns; the caller waits for the stores (tcgen05.wait::st)
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
 // D fp32, A and B fp16, B MN-major
 __host__ __device__ constexpr uint32_t idesc_f16_mn(int m, int n) {
   return (1u << 4) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
@@ -313,18 +326,22 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
             s[16 + j] = make_float2(__uint_as_float(r1[2 * j]), __uint_as_float(r1[2 * j + 1]));
           }
         }
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int j = 0; j < KV4_KEYS / 2; ++j) {
           const float4 k = par[2 * j];
           s[j] = fma2(s[j], make_float2(k.x, k.y), mul2(make_float2(k.z, k.w), beta2));
-          if (valid < KV4_KEYS) {
+        }
+        if (valid < KV4_KEYS) {   // the last tile of the sequence
+#pragma unroll
+          for (int j = 0; j < KV4_KEYS / 2; ++j) {
             if (2 * j >= valid) s[j].x = -INFINITY;
             if (2 * j + 1 >= valid) s[j].y = -INFINITY;
           }
-          top[j & 3] = fmaxf(top[j & 3], fmaxf(s[j].x, s[j].y));
         }
-        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < KV4_KEYS / 2; ++j) top[j & 3] = max3(top[j & 3], s[j].x, s[j].y);
+        const float mx = max3(fmaxf(top[0], top[1]), top[2], top[3]);
         const bool grow = mx > m_ref + RESCALE_STEP;
         if (__any_sync(0xffffffffu, grow)) {
           const float corr = grow ? ex2(m_ref - mx) : 1.f;
@@ -344,18 +361,23 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         }
         const float ref = m_ref == -INFINITY ? 0.f : m_ref;
         const float2 ref2 = make_float2(-ref, -ref);
-        uint32_t pk[KV4_KEYS / 2];
 #pragma unroll
-        for (int j = 0; j < KV4_KEYS / 2; ++j) {
-          const float4 v = par[2 * j + 1];
-          const float2 e = add2(s[j], ref2), p = make_float2(ex2(e.x), ex2(e.y));
-          l2 = add2(l2, p);
-          z2 = fma2(p, make_float2(v.z, v.w), z2);
-          const float2 w = mul2(p, make_float2(v.x, v.y));
-          const __half2 h = __floats2half2_rn(w.x, w.y);
-          pk[j] = *reinterpret_cast<const uint32_t*>(&h);
+        for (int half = 0; half < 2; ++half) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int jj = 0; jj < 16; ++jj) {
+            const int j = half * 16 + jj;
+            const float4 v = par[2 * j + 1];
+            const float2 e = add2(s[j], ref2), p = make_float2(ex2(e.x), ex2(e.y));
+            l2 = add2(l2, p);
+            z2 = fma2(p, make_float2(v.z, v.w), z2);
+            const float2 w = mul2(p, make_float2(v.x, v.y));
+            const __half2 h = __floats2half2_rn(w.x, w.y);
+            pk[jj] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          tmem_st16(s_col + (uint32_t)(half * 16), pk);
         }
-        tmem_st32(s_col, pk);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&p_full[i]));
