@@ -1,18 +1,24 @@
-// The 4-bit cache's attention and weights on the 5th-generation tensor cores (tcgen05), for many rows.
+// Attention over the 4-bit cache on the 5th-generation tensor cores (tcgen05), for many rows.
 //
-// kv4_umma_kernel: two tiles of 128 rows ((query, head of the group) pairs of one KV head) x a range of keys, thirteen warps
+// kv4_umma_kernel: two tiles of 128 rows ((query, head of the group) pairs of one KV head) x a range of keys, sixteen warps
 // with fixed roles:
-//   warps 9-12       turn key tiles of 64 into operands: codes from global memory (a tile ahead in registers) to v = code - 8
-//                    in shared memory, K as bf16 and V as fp16 (both hold the integers exactly), and the keys' steps and
-//                    offsets to four numbers each
-//   warp 8           issues the tcgen05.mma: S_i = Q_i v_K^T (bf16), O_i += P~_i v_V (fp16), row tile i = 0, 1 in turn
-//   warps 0-3, 4-7   the softmax group of row tile 0 resp. 1, one row per thread: s = S * step_K + off_K * sum(q), maximum,
-//                    p = 2^(s - m), l += p, z += p off_V, P~ = p step_V 2^x as fp16 over its scores in tensor memory
-// x brings the largest step of the CTA's keys to [2^10, 2^11), and a row's reference follows its maximum when that has grown
-// by 2^4, so P~ stays below 2^15: fp16 rounds it by 2^-11 of itself down to 2^-24 of the largest weight.  The contraction's order
-// and O's columns are free, so the eight codes of a word stay in the order kv4_word gives, Q enters in it and O leaves it.
-// Each tile's conversion is shared by 256 rows; what a tile takes is the exponentials and the softmax's arithmetic.
+//   warps 9-11, 12-15  turn key tiles of 64 into fp16 operands in shared memory, codes from global memory a tile ahead in
+//                    registers: K' = step * (code - 8), V = lo + step * code, each times a power of two
+//   warp 8           issues the tcgen05.mma: S_i = Q_i K'^T + (sum of Q_i) (lo + 8 step)^T, O_i += P_i V, row tile i = 0, 1
+//                    in turn
+//   warps 0-3, 4-7   the softmax group of row tile 0 resp. 1, one row per thread: maximum, p = 2^(s - m + 10), l += p, P as
+//                    fp16 over its scores in tensor memory
+// K' is exact: a step has 8 bits and a code's distance from 8 three, fp16 holds eleven (down to 2^-21 of the largest number of
+// the CTA's keys).  The offsets' share of a score is a product of its own over sixteen elements: the row's sum in three fp16
+// parts (33 bits) times lo and times 8 step.  So scores are as good as fp32 sums, and the softmax needs nothing of a key but
+// its score -- the steps and offsets as four numbers per key cost 2048 of a tile's 3900 cycles in shared memory reads alone (a
+// uniform 16-byte read is four wavefronts).  V is rounded to fp16 once, and so is P (2^-11 of each term; bf16 outputs are
+// rounded by 2^-8); the powers of two keep the largest of either below 2^15.  A row's reference follows its maximum when that
+// has grown by 2^4.
+// The contraction's order and O's columns are free, so the eight codes of a word stay in the order kv4_word gives, Q enters in
+// it and O leaves it.
 #include <algorithm>
+#include <type_traits>
 
 #include "kv4.cuh"
 #include "tma.cuh"
@@ -22,27 +28,14 @@ namespace dllm {
 
 namespace {
 
-constexpr int UK_ROWS = 128, UK_STAGES = 4, UK_THREADS = 13 * 32, UK_MMA_WARP = 8, UK_CONV_WARP = 9;
+constexpr int UK_ROWS = 128, UK_STAGES = 4, UK_THREADS = 16 * 32, UK_MMA_WARP = 8, UK_K_WARP = 9, UK_V_WARP = 12;
+constexpr int UK_P_BITS = 10;   // P = p * 2^10: fp16's small numbers are further away
 
-// (128 + u) - 136 for the nibbles 0 and 4 of a word: bf16 pairs (128 is 0x4300, its last place is 1)
-__device__ __forceinline__ uint32_t kv4_bf16_lo(uint32_t w) {
-  uint32_t r;
-  asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(r) : "r"(w));
-  const __nv_bfloat162 h = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&r), __bfloat162bfloat162(__ushort_as_bfloat16(0x4308)));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmul.rn.f32x2 rd, ra, rb;\n\t"
-      "mov.b64 {%0, %1}, rd;\n\t}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
@@ -57,22 +50,30 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
-// D fp32, A and B fp16, B MN-major
-__host__ __device__ constexpr uint32_t idesc_f16_mn(int m, int n) {
-  return (1u << 4) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+// D fp32, A and B fp16; mn: B MN-major
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool mn) {
+  return (1u << 4) | ((mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
+__device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
 template <int HD>
 struct UkSmem {
-  static constexpr uint32_t TILE = KV4_KEYS * HD * 2, STAGE = 2 * TILE;              // K then V
-  // per stage two keys per entry: (step, step, off, off) of K times the softmax's scale, (w, w, off, off) of V
-  static constexpr uint32_t PAR = KV4_KEYS * 16, TOTAL = UK_STAGES * (STAGE + PAR) + 1024;
-  // tensor memory: Q_i as bf16 pairs, scores S_i (P~_i over their first half), outputs O_i
+  // per stage K', V, and the offsets' sixteen elements per key (32 of 128 swizzled bytes)
+  static constexpr uint32_t TILE = KV4_KEYS * HD * 2, OFF = KV4_KEYS * 128, STAGE = 2 * TILE + OFF;
+  static constexpr uint32_t SUM = UK_ROWS * 128;    // the rows' sums in parts, per row tile, laid out alike
+  static constexpr uint32_t TOTAL = UK_STAGES * STAGE + 2 * SUM + 1024;
+  // tensor memory: Q_i as fp16 pairs, scores S_i (P_i over their first half), outputs O_i
   static constexpr uint32_t Q_COL = 0, S_COL = HD, O_COL = S_COL + 2 * KV4_KEYS, COLS = 512;
   static_assert(O_COL + 2 * HD <= COLS, "tensor memory holds 512 columns");
+  static_assert(TOTAL <= 227 * 1024, "shared memory of a CTA");
 };
 
 template <int HD>
@@ -85,10 +86,10 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t kv_full[UK_STAGES], kv_empty[UK_STAGES], s_full[2], p_full[2], o_full[2], q_bar;
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_flag, v_top;
+  __shared__ int abort_flag, top[2];   // top: exponent fields of the largest numbers of K and V
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, par_s = base + UK_STAGES * SM::STAGE;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, sum_s = base + UK_STAGES * SM::STAGE;
   volatile int* abortp = &abort_flag;
   const int G = H / c.Hkv, kh = blockIdx.y, b = blockIdx.z / S, split = blockIdx.z - b * S;
   const int rows = a * G, row0 = blockIdx.x * (2 * UK_ROWS), live = row0 + UK_ROWS < rows ? 2 : 1;
@@ -117,9 +118,9 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
 
   if (tid == 0) {
     abort_flag = 0;
-    v_top = 0;
+    top[0] = top[1] = 0;
     for (int i = 0; i < UK_STAGES; ++i) {
-      mbar_init(smem_u32(&kv_full[i]), 4);      // one arrival per converting warp
+      mbar_init(smem_u32(&kv_full[i]), UK_THREADS / 32 - UK_K_WARP);      // one arrival per converting warp
       mbar_init(smem_u32(&kv_empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -141,29 +142,39 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
   const uint32_t tmem = tmem_slot;
   bool ok = true;
 
-  if (warp >= UK_CONV_WARP) {
-    // ---------------- conversion: 128 threads, per tile HD / 32 words of K and of V each, a quarter of a key's row at a time --
-    constexpr int V = HD / 64;                  // 16-byte vectors of K codes per thread and tile
-    constexpr int PER_ROW = HD / 32;            // such vectors per key
-    const int t = tid - UK_CONV_WARP * 32;
-    // the largest step of V among the CTA's keys, by its exponent
-    int ex = 0;
-    for (int j = tile_lo * KV4_KEYS + t; j < min(len, (tile_lo + n_tiles) * KV4_KEYS); j += 128)
-      ex = max(ex, (int)(c.vp[plane + j] >> 7) & 255);
-    ex = __reduce_max_sync(0xffffffffu, ex);
-    if (lane == 0) atomicMax(&v_top, ex);
-    asm volatile("bar.sync 3, 128;" ::: "memory");
-    const float up = __uint_as_float((uint32_t)(264 - max(v_top, 20)) << 23);   // 2^(137 - field): field f means 2^(f - 127)
-    uint4 kc[V], vc[V];
-    uint2 pc = make_uint2(0, 0);
+  // The largest |lo| and step of the CTA's keys, by exponent field (every warp of the calling group of T threads; fields
+  // outside of 30 .. 255 count as those).  A number's field f means less than 2^(f - 126).
+  auto largest = [&](const uint32_t* pairs, int t, int T, int more) {
+    int f = 30;
+    for (int j = t; j < n_tiles * KV4_KEYS; j += T) {
+      if (tile_lo * KV4_KEYS + j >= len) break;
+      const uint32_t p = pairs[j];
+      f = max(f, max((int)(p >> 23) & 255, ((int)(p >> 7) & 255) + more));
+    }
+    return min((int)__reduce_max_sync(0xffffffffu, f), 255);
+  };
+  // ---------------- conversion of K or of V: 32 elements of a key, 16 bytes of codes, at a time ----------------
+  auto convert = [&](auto of_v, auto warps) {
+    constexpr bool OF_V = decltype(of_v)::value;
+    constexpr int T = 32 * decltype(warps)::value, PER_ROW = HD / 32, UNITS = KV4_KEYS * PER_ROW, N = (UNITS + T - 1) / T;
+    const int t = tid - (OF_V ? UK_V_WARP : UK_K_WARP) * 32;
+    const uint8_t* const codes = (OF_V ? c.v : c.k) + (plane + (size_t)tile_lo * KV4_KEYS) * (HD / 2);
+    const uint32_t* const pairs = (OF_V ? c.vp : c.kp) + plane + (size_t)tile_lo * KV4_KEYS;
+    const int f = largest(pairs, t, T, OF_V ? 4 : 3);
+    if (lane == 0) atomicMax(&top[OF_V], f);
+    if constexpr (OF_V) asm volatile("bar.sync 3, %0;" ::"n"(T) : "memory");
+    else asm volatile("bar.sync 4, %0;" ::"n"(T) : "memory");
+    // V: |lo + step * code| < 2^(f - 125), to 2^15.  K: |lo|, 8 step < 2^(f - 126), to 2^7; 2^8 times that beside the sums
+    const float scale = pow2(OF_V ? 140 - top[1] : 133 - top[0]);
+    uint4 x[N];
+    uint32_t pr[N];
     auto fetch = [&](int tile) {
-      const size_t key = plane + (size_t)(tile_lo + tile) * KV4_KEYS;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        kc[i] = *reinterpret_cast<const uint4*>(c.k + key * (HD / 2) + (size_t)(i * 128 + t) * 16);
-        vc[i] = *reinterpret_cast<const uint4*>(c.v + key * (HD / 2) + (size_t)(i * 128 + t) * 16);
-      }
-      if (t < KV4_KEYS) pc = make_uint2(c.kp[key + t], c.vp[key + t]);
+      for (int i = 0; i < N; ++i)
+        if (i * T + t < UNITS) {
+          x[i] = *reinterpret_cast<const uint4*>(codes + (size_t)tile * (KV4_KEYS * HD / 2) + (size_t)(i * T + t) * 16);
+          pr[i] = pairs[tile * KV4_KEYS + (i * T + t) / PER_ROW];
+        }
     };
     fetch(0);
     for (int it = 0; it < n_tiles; ++it) {
@@ -172,51 +183,56 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         ok = false;
         break;
       }
-      const uint32_t ks = base + st * SM::STAGE, vs = ks + SM::TILE;
-      const uint4 kn[2] = {kc[0], kc[V - 1]}, vn[2] = {vc[0], vc[V - 1]};
-      const uint2 pn = pc;
-      if (it + 1 < n_tiles) fetch(it + 1);
+      const uint32_t stage = base + st * SM::STAGE, to = stage + (OF_V ? SM::TILE : 0u);
+      uint4 now[N];
+      uint32_t pair[N];
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int unit = i * 128 + t, r = unit / PER_ROW, qd = unit % PER_ROW;   // key; which 32 of its elements
+      for (int i = 0; i < N; ++i) {
+        now[i] = x[i];
+        pair[i] = pr[i];
+      }
+      if (it + 1 < n_tiles) fetch(it + 1);   // on its way while this one is converted
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int unit = i * T + t, r = unit / PER_ROW, qd = unit % PER_ROW;   // key; which 32 of its elements
+        if (unit >= UNITS) continue;
+        const bool out = (tile_lo + it) * KV4_KEYS + r >= len;   // keys behind the length count for nothing
+        const float step = out ? 0.f : kv4_step(pair[i]) * scale, lo = out ? 0.f : kv4_lo(pair[i]) * scale;
+        const __half2 step2 = __float2half2_rn(step), off2 = __float2half2_rn(fmaf(8.f, step, lo));
         // chunks of eight elements, in an order that puts the eight lanes that store together into eight banks
         const bool turn = HD == 128 && qd >= 2;
+        const uint4 y = now[i];
+        const uint32_t w[4] = {turn ? y.z : y.x, turn ? y.w : y.y, turn ? y.x : y.z, turn ? y.y : y.w};
 #pragma unroll
-        for (int of_v = 0; of_v < 2; ++of_v) {
-          const uint4 x = of_v ? vn[i] : kn[i];
-          const uint32_t w[4] = {turn ? x.z : x.x, turn ? x.w : x.y, turn ? x.x : x.z, turn ? x.y : x.w};
+        for (int k = 0; k < 4; ++k) {
+          const int chunk = qd * 4 + (turn ? k ^ 2 : k);
+          uint32_t p[4];
+          kv4_word(w[k], p);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int chunk = qd * 4 + (turn ? k ^ 2 : k);
-            uint32_t p[4];
-            if (of_v) {
-              kv4_word(w[k], p);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) p[e] = kv4_bf16_lo(w[k] >> (4 * e));
-            }
-            st_shared16((of_v ? vs : ks) + (chunk >> 3) * (KV4_KEYS * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4),
-                        make_uint4(p[0], p[1], p[2], p[3]));
-          }
+          for (int e = 0; e < 4; ++e)
+            p[e] = as_u32(OF_V ? __hfma2(as_half2(p[e]), step2, off2) : __hmul2(as_half2(p[e]), step2));
+          st_shared16(to + (chunk >> 3) * (KV4_KEYS * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4),
+                      make_uint4(p[0], p[1], p[2], p[3]));
         }
-      }
-      if (t < KV4_KEYS) {   // keys behind the length count for nothing, whatever stands there
-        const bool out = (tile_lo + it) * KV4_KEYS + t >= len;
-        const float ks_ = out ? 0.f : kv4_step(pn.x), ko = out ? 0.f : fmaf(8.f, ks_, kv4_lo(pn.x));
-        const float vs_ = out ? 0.f : kv4_step(pn.y), vo = out ? 0.f : fmaf(8.f, vs_, kv4_lo(pn.y));
-        float* par = reinterpret_cast<float*>(smem_raw + (par_s - smem_u32(smem_raw)) + st * SM::PAR) + (t >> 1) * 8 + (t & 1);
-        par[0] = ks_ * scale_log2;
-        par[2] = ko * scale_log2;
-        par[4] = vs_ * up;
-        par[6] = vo;
+        if (!OF_V && qd == 0) {   // beside the sum's parts (h, m, l, h, m, l, 0 ..): lo three times, 8 step three times
+          const uint32_t at = stage + 2 * SM::TILE + r * 128, lo1 = pack_half(lo * 256.f, lo * 256.f);
+          const float s8 = step * 2048.f;
+          st_shared16(at + ((r & 7) << 4), make_uint4(lo1, pack_half(lo * 256.f, s8), pack_half(s8, s8), 0u));
+          st_shared16(at + ((1 ^ (r & 7)) << 4), make_uint4(0u, 0u, 0u, 0u));
+        }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor cores read what these threads wrote
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&kv_full[st]));
     }
+  };
+  if (warp >= UK_V_WARP) {
+    convert(std::true_type{}, std::integral_constant<int, UK_THREADS / 32 - UK_V_WARP>{});
+  } else if (warp >= UK_K_WARP) {
+    convert(std::false_type{}, std::integral_constant<int, UK_V_WARP - UK_K_WARP>{});
   } else if (warp == UK_MMA_WARP) {
     // ---------------- MMA issuer ----------------
-    constexpr uint32_t idesc_s = make_idesc(UK_ROWS, KV4_KEYS), idesc_o = idesc_f16_mn(UK_ROWS, HD);
+    constexpr uint32_t idesc_s = idesc_f16(UK_ROWS, KV4_KEYS, false), idesc_o = idesc_f16(UK_ROWS, HD, true);
     auto ready = [&](int t) {
       const bool r = mbar_wait_warp(smem_u32(&kv_full[t % UK_STAGES]), (uint32_t)(t / UK_STAGES) & 1u, abortp);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -231,6 +247,8 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
           umma_bf16_ta(tmem + SM::S_COL + (uint32_t)(i * KV4_KEYS), tmem + SM::Q_COL + (uint32_t)(i * (HD / 2) + ks * 8),
                        dk + (uint64_t)(off >> 4), idesc_s, ks > 0 ? 1u : 0u);
         }
+        umma_bf16(tmem + SM::S_COL + (uint32_t)(i * KV4_KEYS), make_smem_desc(sum_s + i * SM::SUM),
+                  make_smem_desc(base + st * SM::STAGE + 2 * SM::TILE), idesc_s, 1u);   // (the operands' type is idesc's)
         umma_commit(smem_u32(&s_full[i]));
       }
       __syncwarp();
@@ -275,78 +293,92 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     const uint32_t s_col = tmem + row_lane + SM::S_COL + (uint32_t)(i * KV4_KEYS), o_col = tmem + row_lane + SM::O_COL + (uint32_t)(i * HD);
     const bool is_live = vr < rows;
     const int qi = is_live ? vr / G : 0, g = is_live ? vr - qi * G : 0;
-    float q_sum = 0.f;
+    float scale;    // what a score of this row has to be multiplied by
     {
+      // Q times the power of two that brings the row's largest to [2^13, 2^14), as fp16 (bf16's mantissas are exact in it)
       const uint4* src = reinterpret_cast<const uint4*>(q + ((size_t)b * a + qi) * ldq + (size_t)(kh * G + g) * HD);
+      uint4 x[HD / 8];
+#pragma unroll
+      for (int w = 0; w < HD / 8; ++w) x[w] = is_live ? src[w] : make_uint4(0, 0, 0, 0);
+      float sum = 0.f, most = 0.f;
+#pragma unroll
+      for (int w = 0; w < HD / 8; ++w) {
+        const uint32_t u[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float lo = __uint_as_float(u[k] << 16), hi = __uint_as_float(u[k] & 0xFFFF0000u);
+          sum += lo + hi;
+          most = max3(most, fabsf(lo), fabsf(hi));
+        }
+      }
+      const int f = max((int)(__float_as_uint(most) >> 23), 20);
+      const float up = pow2(140 - f);
 #pragma unroll
       for (int p = 0; p < PANELS; ++p) {
-        uint4 x[8];
-#pragma unroll
-        for (int w = 0; w < 8; ++w) x[w] = is_live ? src[p * 8 + w] : make_uint4(0, 0, 0, 0);
         uint32_t r[32];
 #pragma unroll
         for (int w = 0; w < 8; ++w) {   // elements (0, 4), (1, 5), (2, 6), (3, 7), as a word's codes come out
-          const uint32_t u[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
-          r[4 * w] = __byte_perm(u[0], u[2], 0x5410);
-          r[4 * w + 1] = __byte_perm(u[0], u[2], 0x7632);
-          r[4 * w + 2] = __byte_perm(u[1], u[3], 0x5410);
-          r[4 * w + 3] = __byte_perm(u[1], u[3], 0x7632);
+          const uint4 y = x[p * 8 + w];
+          const uint32_t u[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) q_sum += __uint_as_float(u[k] << 16) + __uint_as_float(u[k] & 0xFFFF0000u);
+          for (int k = 0; k < 2; ++k) {
+            r[4 * w + 2 * k] = pack_half(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k + 2] << 16) * up);
+            r[4 * w + 2 * k + 1] = pack_half(__uint_as_float(u[k] & 0xFFFF0000u) * up, __uint_as_float(u[k + 2] & 0xFFFF0000u) * up);
+          }
         }
         tmem_st32(tmem + row_lane + SM::Q_COL + (uint32_t)(i * (HD / 2) + p * 32), r);
       }
+      // the sum's three parts, 2^-8 of Q's scale (the offsets beside them have 2^8 of K's)
+      const float v = sum * up * 0.00390625f;
+      const float h = __half2float(__float2half_rn(v)), m = __half2float(__float2half_rn(v - h)), l = v - h - m;
+      const uint32_t at = sum_s + i * SM::SUM + row * 128;
+      st_shared16(at + ((row & 7) << 4), make_uint4(pack_half(h, m), pack_half(l, h), pack_half(m, l), 0u));
+      st_shared16(at + ((1 ^ (row & 7)) << 4), make_uint4(0u, 0u, 0u, 0u));
+      scale = scale_log2 * pow2(f - 140);   // K's part follows when it is known
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&q_bar));
     }
     constexpr float RESCALE_STEP = 4.f;
     float m_ref = -INFINITY;
-    float2 l2 = make_float2(0.f, 0.f), z2 = make_float2(0.f, 0.f);
-    const float2 beta2 = make_float2(q_sum, q_sum);
+    float2 l2 = make_float2(0.f, 0.f);
     if (i < live) {
-      for (int t = 0; t < n_tiles; ++t) {
-        ok = mbar_wait(smem_u32(&s_full[i]), (uint32_t)t & 1u, abortp);
-        // (the numbers below come from the converting warps, whose tile the scores have waited for)
-        if (ok) ok = mbar_wait(smem_u32(&kv_full[t % UK_STAGES]), (uint32_t)(t / UK_STAGES) & 1u, abortp);
-        ok = __all_sync(0xffffffffu, ok);
+      // (K's scale: what a converting warp wrote ahead of its first tile)
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&kv_full[0]), 0u, abortp));
+      scale *= pow2(top[0] - 133);
+      for (int t = 0; t < n_tiles && ok; ++t) {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[i]), (uint32_t)t & 1u, abortp));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const float4* par = reinterpret_cast<const float4*>(smem_raw + (par_s - smem_u32(smem_raw)) + (t % UK_STAGES) * SM::PAR);
         const int valid = len - (tile_lo + t) * KV4_KEYS;
-        float2 s[KV4_KEYS / 2];
+        float s[KV4_KEYS];
         {
           uint32_t r0[32], r1[32];
           tmem_ld32(s_col, r0);
           tmem_ld32(s_col + 32u, r1);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            s[j] = make_float2(__uint_as_float(r0[2 * j]), __uint_as_float(r0[2 * j + 1]));
-            s[16 + j] = make_float2(__uint_as_float(r1[2 * j]), __uint_as_float(r1[2 * j + 1]));
+          for (int j = 0; j < 32; ++j) {
+            s[j] = __uint_as_float(r0[j]);
+            s[32 + j] = __uint_as_float(r1[j]);
           }
-        }
-#pragma unroll
-        for (int j = 0; j < KV4_KEYS / 2; ++j) {
-          const float4 k = par[2 * j];
-          s[j] = fma2(s[j], make_float2(k.x, k.y), mul2(make_float2(k.z, k.w), beta2));
         }
         if (valid < KV4_KEYS) {   // the last tile of the sequence
 #pragma unroll
-          for (int j = 0; j < KV4_KEYS / 2; ++j) {
-            if (2 * j >= valid) s[j].x = -INFINITY;
-            if (2 * j + 1 >= valid) s[j].y = -INFINITY;
-          }
+          for (int j = 0; j < KV4_KEYS; ++j)
+            if (j >= valid) s[j] = -INFINITY;
         }
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < KV4_KEYS / 2; ++j) top[j & 3] = max3(top[j & 3], s[j].x, s[j].y);
-        const float mx = max3(fmaxf(top[0], top[1]), top[2], top[3]);
+        for (int j = 0; j < KV4_KEYS; j += 2) most[(j >> 1) & 3] = max3(most[(j >> 1) & 3], s[j], s[j + 1]);
+        const float mx = max3(fmaxf(most[0], most[1]), most[2], most[3]) * scale;   // scale > 0
         const bool grow = mx > m_ref + RESCALE_STEP;
         if (__any_sync(0xffffffffu, grow)) {
           const float corr = grow ? ex2(m_ref - mx) : 1.f;
           if (grow) m_ref = mx;
-          l2.x *= corr; l2.y *= corr; z2.x *= corr; z2.y *= corr;
+          l2.x *= corr;
+          l2.y *= corr;
           if (t > 0) {
 #pragma unroll
             for (int cc = 0; cc < HD; cc += 32) {
@@ -359,21 +391,17 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
             }
           }
         }
-        const float ref = m_ref == -INFINITY ? 0.f : m_ref;
-        const float2 ref2 = make_float2(-ref, -ref);
+        const float ref = (m_ref == -INFINITY ? 0.f : m_ref) - (float)UK_P_BITS;
+        const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t pk[16];
 #pragma unroll
           for (int jj = 0; jj < 16; ++jj) {
-            const int j = half * 16 + jj;
-            const float4 v = par[2 * j + 1];
-            const float2 e = add2(s[j], ref2), p = make_float2(ex2(e.x), ex2(e.y));
+            const int j = half * 32 + 2 * jj;
+            const float2 e = fma2(make_float2(s[j], s[j + 1]), scale2, ref2), p = make_float2(ex2(e.x), ex2(e.y));
             l2 = add2(l2, p);
-            z2 = fma2(p, make_float2(v.z, v.w), z2);
-            const float2 w = mul2(p, make_float2(v.x, v.y));
-            const __half2 h = __floats2half2_rn(w.x, w.y);
-            pk[jj] = *reinterpret_cast<const uint32_t*>(&h);
+            pk[jj] = pack_half(p.x, p.y);
           }
           tmem_st16(s_col + (uint32_t)(half * 16), pk);
         }
@@ -382,13 +410,11 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&p_full[i]));
       }
-      if (ok) ok = mbar_wait(smem_u32(&o_full[i]), 0u, abortp);
-      ok = __all_sync(0xffffffffu, ok);
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&o_full[i]), 0u, abortp));
       if (ok) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const float l = l2.x + l2.y, z = z2.x + z2.y, down = __uint_as_float((uint32_t)(max(v_top, 20) - 10) << 23);
-        const float inv = S > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-        const float f = down * inv, zf = z * inv;
+        const float l = (l2.x + l2.y) * pow2(-UK_P_BITS), down = pow2(top[1] - 140 - UK_P_BITS);
+        const float f = S > 1 ? down : l == 0.f ? 0.f : down / l;
         const size_t orow = ((size_t)b * a + qi) * H + kh * G + g;
 #pragma unroll
         for (int cc = 0; cc < HD; cc += 32) {
@@ -396,22 +422,14 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
           tmem_ld32(o_col + (uint32_t)cc, r);
           tmem_ld_wait();
           if (!is_live) continue;
-          float x[32];
 #pragma unroll
-          for (int k = 0; k < 32; ++k)   // column 8k + 2e + h of O is element 8k + e + 4h
-            x[(k & ~7) + ((k & 7) >> 1) + 4 * (k & 1)] = fmaf(__uint_as_float(r[k]), f, zf);
-          if (S > 1) {
-            float* dst = o_part + ((size_t)split * total + orow) * HD + cc;
+          for (int k = 0; k < 32; k += 8) {
+            float y[8];
 #pragma unroll
-            for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(x[k], x[k + 1], x[k + 2], x[k + 3]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; k += 8) {
-              float y[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) y[e] = x[k + e];
-              Vec8<__nv_bfloat16>::store(o + orow * HD + cc + k, y);
-            }
+            for (int e = 0; e < 8; ++e)   // column 2e + h of eight is element e + 4h
+              y[(e >> 1) + 4 * (e & 1)] = __uint_as_float(r[k + e]) * f;
+            if (S > 1) Vec8<float>::store(o_part + ((size_t)split * total + orow) * HD + cc + k, y);
+            else Vec8<__nv_bfloat16>::store(o + orow * HD + cc + k, y);
           }
         }
         if (is_live) {

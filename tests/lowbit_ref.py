@@ -83,7 +83,7 @@ def attention(q, cache, a, n, H, lens=None):
             ds = (hd / 16 + 4) * 2.0 ** -22 * mag.amax(-1) + 2.0 ** -21 * (1 + s.abs().amax(-1))
             s_err[b, :, h] = ds
             size = p @ ((v * vstep[b, h, :L, None]).abs() + voff[b, h, :L, None].abs())
-            o_err[b, :, h] = size * (2.0 ** -11 + 2 * ds[..., None] + L ** 0.5 * 2.0 ** -22)
+            o_err[b, :, h] = size * (3 * 2.0 ** -11 + 2 * ds[..., None] + L ** 0.5 * 2.0 ** -22)
     return [t.reshape(B, a, H, *t.shape[4:]) for t in (o, lse, o_err, s_err)]
 
 
