@@ -297,28 +297,34 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     {
       // Q times the power of two that brings the row's largest to [2^13, 2^14), as fp16 (bf16's mantissas are exact in it)
       const uint4* src = reinterpret_cast<const uint4*>(q + ((size_t)b * a + qi) * ldq + (size_t)(kh * G + g) * HD);
-      uint4 x[HD / 8];
-#pragma unroll
-      for (int w = 0; w < HD / 8; ++w) x[w] = is_live ? src[w] : make_uint4(0, 0, 0, 0);
       float sum = 0.f, most = 0.f;
+#pragma unroll 1
+      for (int p = 0; p < PANELS; ++p) {   // (read again below: a row's 64 registers at once are too many)
+        uint4 x[8];
 #pragma unroll
-      for (int w = 0; w < HD / 8; ++w) {
-        const uint32_t u[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+        for (int w = 0; w < 8; ++w) x[w] = is_live ? src[p * 8 + w] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float lo = __uint_as_float(u[k] << 16), hi = __uint_as_float(u[k] & 0xFFFF0000u);
-          sum += lo + hi;
-          most = max3(most, fabsf(lo), fabsf(hi));
+        for (int w = 0; w < 8; ++w) {
+          const uint32_t u[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float lo = __uint_as_float(u[k] << 16), hi = __uint_as_float(u[k] & 0xFFFF0000u);
+            sum += lo + hi;
+            most = max3(most, fabsf(lo), fabsf(hi));
+          }
         }
       }
       const int f = max((int)(__float_as_uint(most) >> 23), 20);
       const float up = pow2(140 - f);
-#pragma unroll
+#pragma unroll 1
       for (int p = 0; p < PANELS; ++p) {
         uint32_t r[32];
+        uint4 x[8];
+#pragma unroll
+        for (int w = 0; w < 8; ++w) x[w] = is_live ? src[p * 8 + w] : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int w = 0; w < 8; ++w) {   // elements (0, 4), (1, 5), (2, 6), (3, 7), as a word's codes come out
-          const uint4 y = x[p * 8 + w];
+          const uint4 y = x[w];
           const uint32_t u[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
@@ -352,26 +358,26 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const int valid = len - (tile_lo + t) * KV4_KEYS;
-        float s[KV4_KEYS];
-        {
-          uint32_t r0[32], r1[32];
-          tmem_ld32(s_col, r0);
-          tmem_ld32(s_col + 32u, r1);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            s[j] = __uint_as_float(r0[j]);
-            s[32 + j] = __uint_as_float(r1[j]);
-          }
-        }
-        if (valid < KV4_KEYS) {   // the last tile of the sequence
-#pragma unroll
-          for (int j = 0; j < KV4_KEYS; ++j)
-            if (j >= valid) s[j] = -INFINITY;
-        }
+        // 32 scores at a time, read from tensor memory twice (the maximum, the exponentials): 64 at once are more registers
+        // than a thread has, and what the compiler kept in local memory instead took FIGURE
         float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto scores = [&](int half, uint32_t (&r)[32]) {
+          tmem_ld32(s_col + (uint32_t)(half * 32), r);
+          tmem_ld_wait();
+          if (valid < KV4_KEYS) {   // the last tile of the sequence
 #pragma unroll
-        for (int j = 0; j < KV4_KEYS; j += 2) most[(j >> 1) & 3] = max3(most[(j >> 1) & 3], s[j], s[j + 1]);
+            for (int j = 0; j < 32; ++j)
+              if (half * 32 + j >= valid) r[j] = 0xFF800000u;
+          }
+        };
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t r[32];
+          scores(half, r);
+#pragma unroll
+          for (int j = 0; j < 32; j += 2)
+            most[(j >> 1) & 3] = max3(most[(j >> 1) & 3], __uint_as_float(r[j]), __uint_as_float(r[j + 1]));
+        }
         const float mx = max3(fmaxf(most[0], most[1]), most[2], most[3]) * scale;   // scale > 0
         const bool grow = mx > m_ref + RESCALE_STEP;
         if (__any_sync(0xffffffffu, grow)) {
@@ -395,11 +401,11 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          uint32_t pk[16];
+          uint32_t pk[16], r[32];
+          scores(half, r);
 #pragma unroll
           for (int jj = 0; jj < 16; ++jj) {
-            const int j = half * 32 + 2 * jj;
-            const float2 e = fma2(make_float2(s[j], s[j + 1]), scale2, ref2), p = make_float2(ex2(e.x), ex2(e.y));
+            const float2 e = fma2(make_float2(__uint_as_float(r[2 * jj]), __uint_as_float(r[2 * jj + 1])), scale2, ref2), p = make_float2(ex2(e.x), ex2(e.y));
             l2 = add2(l2, p);
             pk[jj] = pack_half(p.x, p.y);
           }
