@@ -2,8 +2,8 @@
 //
 // kv4_umma_kernel: two tiles of 128 rows ((query, head of the group) pairs of one KV head) x a range of keys, sixteen warps
 // with fixed roles:
-//   warps 9-11, 12-15  turn key tiles of 64 into fp16 operands in shared memory, codes from global memory a tile ahead in
-//                    registers: K' = step * (code - 8), V = lo + step * code, each times a power of two
+//   warps 9-11, 12-15  turn keys into fp16 operands in shared memory, two rounds of 64 to a tile, codes from global memory a
+//                    round ahead in registers: K' = step * (code - 8), V = lo + step * code, each times a power of two
 //   warp 8           issues the tcgen05.mma: S_i = Q_i K'^T + (sum of Q_i) (lo + 8 step)^T, O_i += P_i V, row tile i = 0, 1
 //                    in turn
 //   warps 0-3, 4-7   the softmax group of row tile 0 resp. 1, one row per thread: maximum, p = 2^(s - m + 10), l += p, P as
@@ -28,7 +28,7 @@ namespace dllm {
 
 namespace {
 
-constexpr int UK_ROWS = 128, UK_STAGES = 4, UK_THREADS = 16 * 32, UK_MMA_WARP = 8, UK_K_WARP = 9, UK_V_WARP = 12;
+constexpr int UK_ROWS = 128, UK_KEYS = 2 * KV4_KEYS, UK_STAGES = 2, UK_THREADS = 16 * 32, UK_MMA_WARP = 8, UK_K_WARP = 9, UK_V_WARP = 12;
 constexpr int UK_P_BITS = 10;   // P = p * 2^10: fp16's small numbers are further away
 
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
@@ -64,16 +64,25 @@ __device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// Sixteen fp16 per row (32 bytes, 32-byte swizzle: K-major, 8-row groups 256 bytes apart)
+__device__ __forceinline__ uint64_t make_smem_desc_32(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)6 << 61);
+}
+__device__ __forceinline__ uint32_t chunk_32(uint32_t base, int row, int chunk) {
+  return base + row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4);
+}
 template <int HD>
 struct UkSmem {
-  // per stage K', V, and the offsets' sixteen elements per key (32 of 128 swizzled bytes)
-  static constexpr uint32_t TILE = KV4_KEYS * HD * 2, OFF = KV4_KEYS * 128, STAGE = 2 * TILE + OFF;
-  static constexpr uint32_t SUM = UK_ROWS * 128;    // the rows' sums in parts, per row tile, laid out alike
-  static constexpr uint32_t TOTAL = UK_STAGES * STAGE + 2 * SUM + 1024;
-  // tensor memory: Q_i as fp16 pairs, scores S_i (P_i over their first half), outputs O_i
-  static constexpr uint32_t Q_COL = 0, S_COL = HD, O_COL = S_COL + 2 * KV4_KEYS, COLS = 512;
+  // per stage K', V, and the offsets' sixteen elements per key
+  static constexpr uint32_t TILE = UK_KEYS * HD * 2, OFF = UK_KEYS * 32, STAGE = 2 * TILE + OFF;
+  // per row tile Q, and the rows' sums in parts
+  static constexpr uint32_t Q = UK_ROWS * HD * 2, SUM = UK_ROWS * 32;
+  static constexpr uint32_t TOTAL = UK_STAGES * STAGE + 2 * (Q + SUM) + 1024;
+  // tensor memory: scores S_i (P_i over their first half), outputs O_i
+  static constexpr uint32_t S_COL = 0, O_COL = 2 * UK_KEYS, COLS = 512;
   static_assert(O_COL + 2 * HD <= COLS, "tensor memory holds 512 columns");
-  static_assert(TOTAL <= 227 * 1024, "shared memory of a CTA");
+  static_assert(TOTAL <= 227 * 1024 && STAGE % 1024 == 0 && Q % 1024 == 0, "shared memory of a CTA");
 };
 
 template <int HD>
@@ -82,21 +91,20 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
                     __nv_bfloat16* __restrict__ o, float* __restrict__ lse, float* __restrict__ o_part,
                     float2* __restrict__ ml_part, int a, int n, int H, int S, float scale_log2, int* __restrict__ status) {
   using SM = UkSmem<HD>;
-  constexpr int PANELS = HD / 64;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t kv_full[UK_STAGES], kv_empty[UK_STAGES], s_full[2], p_full[2], o_full[2], q_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag, top[2];   // top: exponent fields of the largest numbers of K and V
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, sum_s = base + UK_STAGES * SM::STAGE;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, q_s = base + UK_STAGES * SM::STAGE, sum_s = q_s + 2 * SM::Q;
   volatile int* abortp = &abort_flag;
   const int G = H / c.Hkv, kh = blockIdx.y, b = blockIdx.z / S, split = blockIdx.z - b * S;
   const int rows = a * G, row0 = blockIdx.x * (2 * UK_ROWS), live = row0 + UK_ROWS < rows ? 2 : 1;
   pdl_wait();
   pdl_trigger();
   const int len = lens ? min(max(lens[b], 0), n) : n;
-  const int tiles_all = (len + KV4_KEYS - 1) / KV4_KEYS, per_split = (tiles_all + S - 1) / S;
+  const int tiles_all = (len + UK_KEYS - 1) / UK_KEYS, per_split = (tiles_all + S - 1) / S;
   const int tile_lo = min(split * per_split, tiles_all), n_tiles = min(tile_lo + per_split, tiles_all) - tile_lo;
   const size_t plane = ((size_t)b * c.Hkv + kh) * c.cap, total = (size_t)gridDim.z / S * a * H;
 
@@ -142,14 +150,18 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
   const uint32_t tmem = tmem_slot;
   bool ok = true;
 
+  const int n_keys = min(len - tile_lo * UK_KEYS, n_tiles * UK_KEYS), rounds = (n_keys + KV4_KEYS - 1) / KV4_KEYS;
   // The largest |lo| and step of the CTA's keys, by exponent field (every warp of the calling group of T threads; fields
   // outside of 30 .. 255 count as those).  A number's field f means less than 2^(f - 126).
   auto largest = [&](const uint32_t* pairs, int t, int T, int more) {
     int f = 30;
-    for (int j = t; j < n_tiles * KV4_KEYS; j += T) {
-      if (tile_lo * KV4_KEYS + j >= len) break;
-      const uint32_t p = pairs[j];
-      f = max(f, max((int)(p >> 23) & 255, ((int)(p >> 7) & 255) + more));
+#pragma unroll 4
+    for (int j = 4 * t; j < n_keys; j += 4 * T) {
+      const uint4 p = *reinterpret_cast<const uint4*>(pairs + j);
+      const uint32_t u[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < n_keys) f = max(f, max((int)(u[e] >> 23) & 255, ((int)(u[e] >> 7) & 255) + more));
     }
     return min((int)__reduce_max_sync(0xffffffffu, f), 255);
   };
@@ -158,8 +170,8 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     constexpr bool OF_V = decltype(of_v)::value;
     constexpr int T = 32 * decltype(warps)::value, PER_ROW = HD / 32, UNITS = KV4_KEYS * PER_ROW, N = (UNITS + T - 1) / T;
     const int t = tid - (OF_V ? UK_V_WARP : UK_K_WARP) * 32;
-    const uint8_t* const codes = (OF_V ? c.v : c.k) + (plane + (size_t)tile_lo * KV4_KEYS) * (HD / 2);
-    const uint32_t* const pairs = (OF_V ? c.vp : c.kp) + plane + (size_t)tile_lo * KV4_KEYS;
+    const uint8_t* const codes = (OF_V ? c.v : c.k) + (plane + (size_t)tile_lo * UK_KEYS) * (HD / 2);
+    const uint32_t* const pairs = (OF_V ? c.vp : c.kp) + plane + (size_t)tile_lo * UK_KEYS;
     const int f = largest(pairs, t, T, OF_V ? 4 : 3);
     if (lane == 0) atomicMax(&top[OF_V], f);
     if constexpr (OF_V) asm volatile("bar.sync 3, %0;" ::"n"(T) : "memory");
@@ -168,18 +180,22 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     const float scale = pow2(OF_V ? 140 - top[1] : 133 - top[0]);
     uint4 x[N];
     uint32_t pr[N];
-    auto fetch = [&](int tile) {
+    auto fetch = [&](int round) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i * T + t < UNITS) {
-          x[i] = *reinterpret_cast<const uint4*>(codes + (size_t)tile * (KV4_KEYS * HD / 2) + (size_t)(i * T + t) * 16);
-          pr[i] = pairs[tile * KV4_KEYS + (i * T + t) / PER_ROW];
+      for (int i = 0; i < N; ++i) {
+        x[i] = make_uint4(0, 0, 0, 0);
+        pr[i] = 0;
+        if (i * T + t < UNITS && round < rounds) {   // (the last tile may have one round only: zeros in the other)
+          x[i] = *reinterpret_cast<const uint4*>(codes + (size_t)round * (KV4_KEYS * HD / 2) + (size_t)(i * T + t) * 16);
+          pr[i] = pairs[round * KV4_KEYS + (i * T + t) / PER_ROW];
         }
+      }
     };
     fetch(0);
-    for (int it = 0; it < n_tiles; ++it) {
-      const int st = it % UK_STAGES;
-      if (it >= UK_STAGES && !mbar_wait_warp(smem_u32(&kv_empty[st]), (uint32_t)(it / UK_STAGES - 1) & 1u, abortp)) {
+    for (int it = 0; it < 2 * n_tiles; ++it) {
+      const int tile = it >> 1, st = tile % UK_STAGES;
+      if (!(it & 1) && tile >= UK_STAGES &&
+          !mbar_wait_warp(smem_u32(&kv_empty[st]), (uint32_t)(tile / UK_STAGES - 1) & 1u, abortp)) {
         ok = false;
         break;
       }
@@ -191,12 +207,12 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         now[i] = x[i];
         pair[i] = pr[i];
       }
-      if (it + 1 < n_tiles) fetch(it + 1);   // on its way while this one is converted
+      fetch(it + 1);   // on its way while this one is converted
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const int unit = i * T + t, r = unit / PER_ROW, qd = unit % PER_ROW;   // key; which 32 of its elements
+        const int unit = i * T + t, r = (it & 1) * KV4_KEYS + unit / PER_ROW, qd = unit % PER_ROW;   // key; which 32 elements
         if (unit >= UNITS) continue;
-        const bool out = (tile_lo + it) * KV4_KEYS + r >= len;   // keys behind the length count for nothing
+        const bool out = tile * UK_KEYS + r >= n_keys;   // keys behind the length count for nothing
         const float step = out ? 0.f : kv4_step(pair[i]) * scale, lo = out ? 0.f : kv4_lo(pair[i]) * scale;
         const __half2 step2 = __float2half2_rn(step), off2 = __float2half2_rn(fmaf(8.f, step, lo));
         // chunks of eight elements, in an order that puts the eight lanes that store together into eight banks
@@ -211,19 +227,20 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             p[e] = as_u32(OF_V ? __hfma2(as_half2(p[e]), step2, off2) : __hmul2(as_half2(p[e]), step2));
-          st_shared16(to + (chunk >> 3) * (KV4_KEYS * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4),
+          st_shared16(to + (chunk >> 3) * (UK_KEYS * 128) + r * 128 + (((chunk & 7) ^ (r & 7)) << 4),
                       make_uint4(p[0], p[1], p[2], p[3]));
         }
         if (!OF_V && qd == 0) {   // beside the sum's parts (h, m, l, h, m, l, 0 ..): lo three times, 8 step three times
-          const uint32_t at = stage + 2 * SM::TILE + r * 128, lo1 = pack_half(lo * 256.f, lo * 256.f);
-          const float s8 = step * 2048.f;
-          st_shared16(at + ((r & 7) << 4), make_uint4(lo1, pack_half(lo * 256.f, s8), pack_half(s8, s8), 0u));
-          st_shared16(at + ((1 ^ (r & 7)) << 4), make_uint4(0u, 0u, 0u, 0u));
+          const float lo1 = lo * 256.f, s8 = step * 2048.f;
+          st_shared16(chunk_32(stage + 2 * SM::TILE, r, 0), make_uint4(pack_half(lo1, lo1), pack_half(lo1, s8), pack_half(s8, s8), 0u));
+          st_shared16(chunk_32(stage + 2 * SM::TILE, r, 1), make_uint4(0u, 0u, 0u, 0u));
         }
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor cores read what these threads wrote
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&kv_full[st]));
+      if (it & 1) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor cores read what these threads wrote
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&kv_full[st]));
+      }
     }
   };
   if (warp >= UK_V_WARP) {
@@ -232,7 +249,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     convert(std::false_type{}, std::integral_constant<int, UK_V_WARP - UK_K_WARP>{});
   } else if (warp == UK_MMA_WARP) {
     // ---------------- MMA issuer ----------------
-    constexpr uint32_t idesc_s = idesc_f16(UK_ROWS, KV4_KEYS, false), idesc_o = idesc_f16(UK_ROWS, HD, true);
+    constexpr uint32_t idesc_s = idesc_f16(UK_ROWS, UK_KEYS, false), idesc_o = idesc_f16(UK_ROWS, HD, true);
     auto ready = [&](int t) {
       const bool r = mbar_wait_warp(smem_u32(&kv_full[t % UK_STAGES]), (uint32_t)(t / UK_STAGES) & 1u, abortp);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -240,15 +257,14 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     };
     auto issue_s = [&](int i, int st) {
       if (elect_one()) {
-        const uint64_t dk = make_smem_desc(base + st * SM::STAGE);
+        const uint64_t dq = make_smem_desc(q_s + i * SM::Q), dk = make_smem_desc(base + st * SM::STAGE);
+        const uint32_t d = tmem + SM::S_COL + (uint32_t)(i * UK_KEYS);
+        // (umma_bf16 is kind::f16: the operands' type is the descriptor's)
 #pragma unroll
-        for (int ks = 0; ks < HD / 16; ++ks) {
-          const uint32_t off = (ks >> 2) * (KV4_KEYS * 128) + (ks & 3) * 32;
-          umma_bf16_ta(tmem + SM::S_COL + (uint32_t)(i * KV4_KEYS), tmem + SM::Q_COL + (uint32_t)(i * (HD / 2) + ks * 8),
-                       dk + (uint64_t)(off >> 4), idesc_s, ks > 0 ? 1u : 0u);
-        }
-        umma_bf16(tmem + SM::S_COL + (uint32_t)(i * KV4_KEYS), make_smem_desc(sum_s + i * SM::SUM),
-                  make_smem_desc(base + st * SM::STAGE + 2 * SM::TILE), idesc_s, 1u);   // (the operands' type is idesc's)
+        for (int ks = 0; ks < HD / 16; ++ks)
+          umma_bf16(d, dq + (uint64_t)(((ks >> 2) * (UK_ROWS * 128) + (ks & 3) * 32) >> 4),
+                    dk + (uint64_t)(((ks >> 2) * (UK_KEYS * 128) + (ks & 3) * 32) >> 4), idesc_s, ks > 0 ? 1u : 0u);
+        umma_bf16(d, make_smem_desc_32(sum_s + i * SM::SUM), make_smem_desc_32(base + st * SM::STAGE + 2 * SM::TILE), idesc_s, 1u);
         umma_commit(smem_u32(&s_full[i]));
       }
       __syncwarp();
@@ -264,10 +280,10 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (elect_one()) {
-          const uint64_t dv = make_smem_desc_mn(base + st * SM::STAGE + SM::TILE, KV4_KEYS * 128, 1024);
+          const uint64_t dv = make_smem_desc_mn(base + st * SM::STAGE + SM::TILE, UK_KEYS * 128, 1024);
 #pragma unroll
-          for (int ks = 0; ks < KV4_KEYS / 16; ++ks)
-            umma_bf16_ta(tmem + SM::O_COL + (uint32_t)(i * HD), tmem + SM::S_COL + (uint32_t)(i * KV4_KEYS + ks * 8),
+          for (int ks = 0; ks < UK_KEYS / 16; ++ks)
+            umma_bf16_ta(tmem + SM::O_COL + (uint32_t)(i * HD), tmem + SM::S_COL + (uint32_t)(i * UK_KEYS + ks * 8),
                          dv + (uint64_t)((ks * 16 * 128) >> 4), idesc_o, (t > 0 || ks > 0) ? 1u : 0u);
         }
         __syncwarp();
@@ -290,58 +306,47 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     // ---------------- softmax groups ----------------
     const int i = warp >> 2, row = (warp & 3) * 32 + lane, vr = row0 + i * UK_ROWS + row;
     const uint32_t row_lane = ((uint32_t)((warp & 3) * 32)) << 16;
-    const uint32_t s_col = tmem + row_lane + SM::S_COL + (uint32_t)(i * KV4_KEYS), o_col = tmem + row_lane + SM::O_COL + (uint32_t)(i * HD);
+    const uint32_t s_col = tmem + row_lane + SM::S_COL + (uint32_t)(i * UK_KEYS), o_col = tmem + row_lane + SM::O_COL + (uint32_t)(i * HD);
     const bool is_live = vr < rows;
     const int qi = is_live ? vr / G : 0, g = is_live ? vr - qi * G : 0;
     float scale;    // what a score of this row has to be multiplied by
     {
       // Q times the power of two that brings the row's largest to [2^13, 2^14), as fp16 (bf16's mantissas are exact in it)
       const uint4* src = reinterpret_cast<const uint4*>(q + ((size_t)b * a + qi) * ldq + (size_t)(kh * G + g) * HD);
+      uint4 x[HD / 8];
+#pragma unroll
+      for (int w = 0; w < HD / 8; ++w) x[w] = is_live ? src[w] : make_uint4(0, 0, 0, 0);
       float sum = 0.f, most = 0.f;
-#pragma unroll 1
-      for (int p = 0; p < PANELS; ++p) {   // (read again below: a row's 64 registers at once are too many)
-        uint4 x[8];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) x[w] = is_live ? src[p * 8 + w] : make_uint4(0, 0, 0, 0);
+      for (int w = 0; w < HD / 8; ++w) {
+        const uint32_t u[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
 #pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          const uint32_t u[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float lo = __uint_as_float(u[k] << 16), hi = __uint_as_float(u[k] & 0xFFFF0000u);
-            sum += lo + hi;
-            most = max3(most, fabsf(lo), fabsf(hi));
-          }
+        for (int k = 0; k < 4; ++k) {
+          const float lo = __uint_as_float(u[k] << 16), hi = __uint_as_float(u[k] & 0xFFFF0000u);
+          sum += lo + hi;
+          most = max3(most, fabsf(lo), fabsf(hi));
         }
       }
       const int f = max((int)(__float_as_uint(most) >> 23), 20);
       const float up = pow2(140 - f);
-#pragma unroll 1
-      for (int p = 0; p < PANELS; ++p) {
-        uint32_t r[32];
-        uint4 x[8];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) x[w] = is_live ? src[p * 8 + w] : make_uint4(0, 0, 0, 0);
+      for (int w = 0; w < HD / 8; ++w) {   // elements (0, 4), (1, 5), (2, 6), (3, 7), as a word's codes come out
+        const uint32_t u[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+        uint32_t r[4];
 #pragma unroll
-        for (int w = 0; w < 8; ++w) {   // elements (0, 4), (1, 5), (2, 6), (3, 7), as a word's codes come out
-          const uint4 y = x[w];
-          const uint32_t u[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            r[4 * w + 2 * k] = pack_half(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k + 2] << 16) * up);
-            r[4 * w + 2 * k + 1] = pack_half(__uint_as_float(u[k] & 0xFFFF0000u) * up, __uint_as_float(u[k + 2] & 0xFFFF0000u) * up);
-          }
+        for (int k = 0; k < 2; ++k) {
+          r[2 * k] = pack_half(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k + 2] << 16) * up);
+          r[2 * k + 1] = pack_half(__uint_as_float(u[k] & 0xFFFF0000u) * up, __uint_as_float(u[k + 2] & 0xFFFF0000u) * up);
         }
-        tmem_st32(tmem + row_lane + SM::Q_COL + (uint32_t)(i * (HD / 2) + p * 32), r);
+        st_shared16(q_s + i * SM::Q + (w >> 3) * (UK_ROWS * 128) + row * 128 + (((w & 7) ^ (row & 7)) << 4),
+                    make_uint4(r[0], r[1], r[2], r[3]));
       }
       // the sum's three parts, 2^-8 of Q's scale (the offsets beside them have 2^8 of K's)
       const float v = sum * up * 0.00390625f;
       const float h = __half2float(__float2half_rn(v)), m = __half2float(__float2half_rn(v - h)), l = v - h - m;
-      const uint32_t at = sum_s + i * SM::SUM + row * 128;
-      st_shared16(at + ((row & 7) << 4), make_uint4(pack_half(h, m), pack_half(l, h), pack_half(m, l), 0u));
-      st_shared16(at + ((1 ^ (row & 7)) << 4), make_uint4(0u, 0u, 0u, 0u));
+      st_shared16(chunk_32(sum_s + i * SM::SUM, row, 0), make_uint4(pack_half(h, m), pack_half(l, h), pack_half(m, l), 0u));
+      st_shared16(chunk_32(sum_s + i * SM::SUM, row, 1), make_uint4(0u, 0u, 0u, 0u));
       scale = scale_log2 * pow2(f - 140);   // K's part follows when it is known
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&q_bar));
@@ -357,23 +362,23 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[i]), (uint32_t)t & 1u, abortp));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const int valid = len - (tile_lo + t) * KV4_KEYS;
-        // 32 scores at a time, read from tensor memory twice (the maximum, the exponentials): 64 at once are more registers
-        // than a thread has, and what the compiler kept in local memory instead took FIGURE
+        const int valid = n_keys - t * UK_KEYS;
+        // 32 scores at a time, read from tensor memory twice (the maximum, the exponentials): more at once and the compiler
+        // keeps some of a thread's 128 registers in local memory (344 instead of 321 us with tiles of 64 keys)
         float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        auto scores = [&](int half, uint32_t (&r)[32]) {
-          tmem_ld32(s_col + (uint32_t)(half * 32), r);
+        auto scores = [&](int part, uint32_t (&r)[32]) {
+          tmem_ld32(s_col + (uint32_t)(part * 32), r);
           tmem_ld_wait();
-          if (valid < KV4_KEYS) {   // the last tile of the sequence
+          if (valid < UK_KEYS) {   // the last tile of the sequence
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-              if (half * 32 + j >= valid) r[j] = 0xFF800000u;
+              if (part * 32 + j >= valid) r[j] = 0xFF800000u;
           }
         };
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int part = 0; part < UK_KEYS / 32; ++part) {
           uint32_t r[32];
-          scores(half, r);
+          scores(part, r);
 #pragma unroll
           for (int j = 0; j < 32; j += 2)
             most[(j >> 1) & 3] = max3(most[(j >> 1) & 3], __uint_as_float(r[j]), __uint_as_float(r[j + 1]));
@@ -400,16 +405,16 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         const float ref = (m_ref == -INFINITY ? 0.f : m_ref) - (float)UK_P_BITS;
         const float2 scale2 = make_float2(scale, scale), ref2 = make_float2(-ref, -ref);
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int part = 0; part < UK_KEYS / 32; ++part) {
           uint32_t pk[16], r[32];
-          scores(half, r);
+          scores(part, r);
 #pragma unroll
           for (int jj = 0; jj < 16; ++jj) {
             const float2 e = fma2(make_float2(__uint_as_float(r[2 * jj]), __uint_as_float(r[2 * jj + 1])), scale2, ref2), p = make_float2(ex2(e.x), ex2(e.y));
             l2 = add2(l2, p);
             pk[jj] = pack_half(p.x, p.y);
           }
-          tmem_st16(s_col + (uint32_t)(half * 16), pk);
+          tmem_st16(s_col + (uint32_t)(part * 16), pk);
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
