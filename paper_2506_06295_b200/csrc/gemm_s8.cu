@@ -20,31 +20,53 @@ namespace {
 
 constexpr int S8_K = 128;    // integers of k per stage: one 128-byte swizzle row
 
-// W columns (rows of A) of a finished tile, TMEM lane = weight row: 128 threads, tl = 0..127 = lane.  split: the integers go
-// to the slab, for the sum over the slabs.
+// W columns (rows of A) of a finished tile, TMEM lane = weight row: 128 threads, tl = 0..127 = lane, all in step.  split: the
+// integers go to the slab, for the sum over the slabs.  The rows' scales of a trip are requested together, ahead of the
+// accumulator's columns (one by one between the stores, which the compiler must assume to change them, they took 1700 cycles
+// per trip of 16 rows: 8192 x 24576 x 4096 757 us, 505 now).  bf16: two lanes put their columns of two rows together, four
+// bytes a store.
 template <int W, typename T>
 __device__ __forceinline__ void s8_epilogue(uint32_t tmem_d, int tl, int m0, int n0, int M, int N, const float* __restrict__ sa,
                                             const float* __restrict__ sw, T* __restrict__ out, int* __restrict__ slab) {
   const uint32_t tmem_w = tmem_d + ((uint32_t)(tl >> 5) << 21);
   const int n = n0 + tl;
-  const float w = n < N ? sw[n] : 0.f;
+  const float w = n < N ? __ldg(sw + n) : 0.f;
+  const bool pairs = sizeof(T) == 2 && !(N & 1) && !((uintptr_t)out & 3);
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
   for (int c0 = 0; c0 < W; c0 += 16) {
     if (m0 + c0 >= M) break;  // uniform across the warp
     uint32_t r[16];
     tmem_ld16(tmem_w + (uint32_t)c0, r);
-    tmem_ld16_wait(r);
-    if (n < N) {
-      const size_t first = (size_t)(m0 + c0) * N + n;
+    float a[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        if (m0 + c0 + j >= M) continue;
-        if (slab)
-          slab[first + (size_t)j * N] = (int)r[j];
-        else
-          out[first + (size_t)j * N] = from_f32<T>(__int2float_rn((int)r[j]) * sa[m0 + c0 + j] * w);
+    for (int j = 0; j < 16; ++j) a[j] = slab ? 0.f : __ldg(sa + min(m0 + c0 + j, M - 1));
+    tmem_ld16_wait(r);
+    const size_t first = (size_t)(m0 + c0) * N;
+    if (slab) {
+      if (n < N) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (m0 + c0 + j < M) slab[first + (size_t)j * N + n] = (int)r[j];
       }
+      continue;
+    }
+    float v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = __int2float_rn((int)r[j]) * a[j] * w;
+    if (pairs) {
+      const int odd = tl & 1;
+      T* const dst = out + first + (size_t)odd * N + (n & ~1);
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) {
+        const float other = __shfl_xor_sync(0xffffffffu, odd ? v[j] : v[j + 1], 1);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(odd ? other : v[j], odd ? v[j + 1] : other);
+        if (n < N && m0 + c0 + j + odd < M) *reinterpret_cast<__nv_bfloat162*>(dst + (size_t)j * N) = h;
+      }
+    } else if (n < N) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (m0 + c0 + j < M) out[first + (size_t)j * N + n] = from_f32<T>(v[j]);
     }
   }
 }
@@ -63,7 +85,7 @@ struct S8Layout {
 // eight drain the accumulator, half of the columns per group of four.  The CTAs of a split tile are a cluster: each leaves its
 // integers in its own shared memory (the drained ring), and each adds up every S-th row of the tile over all of them, scales it
 // and writes it.  (3 x 4096 x 4096 in five splits with slabs in global memory and a launch that adds them: 10.5 us with the
-// row quantisation, and a third launch for the host; so: FIGURE.)
+// row quantisation, and a third launch for the host; so: 8.5.)
 constexpr int S8_THREADS = 256, S8_MOST_SPLITS = 8;
 __device__ __forceinline__ int4 remote4(uint32_t addr) {
   int4 r;
@@ -244,7 +266,7 @@ struct S8Form {
   const float *sa, *sw;
   T* out;
   int split;
-  static constexpr int GROUPS = 1;
+  static constexpr int GROUPS = 2;
   template <int W>
   static constexpr uint32_t ex_bytes() { return 0; }
   template <int W>
@@ -424,18 +446,43 @@ cudaError_t launch_as(const Launch& L, const CUtensorMap& tmW, const CUtensorMap
 
 }  // namespace
 
-// Tile, ring and split as for the bf16 products of as many bytes (plan_gemm_bf16, whose figures hold per stage: a stage has
-// the same bytes and takes the same cycles): up to 128 rows, and for more rows of small weights, one CTA per tile; CTA pairs
-// otherwise, their tile and split by the same estimate.
+// Tile, ring and split, from sweeps on B200 (products alone, bf16 out, weights not in L2, us).
+//   up to 32 rows   one CTA per 128 weight rows, k split until there is one per SM: 3 x 4096 x 4096 in 3 / 4 / 5 ranges 8.3 /
+//                   8.0 / 7.8
+//   up to 64        tiles of 64 rows; ranges by powers of two (clusters of five or six leave SMs idle): 64 x 4096 x 4096 in 4
+//                   9.5, in 5 9.7; a ring of eight stages where a CTA has its SM for itself (64 x 12288 x 4096 15.8 -> 14.6)
+//   up to 128       two tiles of 64 rows where the weight tiles are few (128 x 4608 x 3584 10.5 against 11.8), one of 128
+//                   otherwise (128 x 37888 x 3584 31.2 against 34.6); CTAs, two to an SM, at most nine tenths of the places:
+//                   72 tiles in 2 ranges 10.5, in 4 15.3
+//   up to 256       tiles of 128 rows in 2 or 4 ranges where they fit so (256 x 4096 x 4096 12.9 against 14.9 on pairs), else
+//   and above       CTA pairs, by what a unit's stages take (issue or bytes, as for bf16: a stage is the same bytes and cycles)
+//                   and a split's slabs with the launch that adds them: 256 x 24576 x 4096 33 against 38 in tiles of one CTA,
+//                   768 x 4096 x 12288 33 against 42, 8192 x 24576 x 4096 505 against 980
 GemmPlan plan_gemm_s8(int M, int N, int K) {
   GemmPlan p;
   const int sms = sm_count(), pairs = sms / 2;
-  const long n_tiles = (N + TILE_W - 1) / TILE_W, n_pairs = (N + 2 * TILE_W - 1) / (2 * TILE_W);
+  const long n_tiles = (N + TILE_W - 1) / TILE_W, n_pairs = (N + 2 * TILE_W - 1) / (2 * TILE_W), places = 2L * sms * 9 / 10;
   p.num_kb = (K + S8_K - 1) / S8_K;
   p.w_stream = (long)N * K >= 16L << 20;
-  int S = 0;
-  const bool many_rows = ((M + 255) / 256) * n_tiles > sms || (M >= 768 && K >= 2048);
-  if (M > 128 && ((long)N * K >= 1L << 22 || many_rows)) {
+  int S = 1;
+  auto ranges = [&](long tiles, long room) {   // the largest power of two that fits, four stages each at least
+    int s = 1;
+    while (2 * s <= S8_MOST_SPLITS && tiles * 2 * s <= room && p.num_kb >= 8 * s) s *= 2;
+    return s;
+  };
+  if (M <= 32) {
+    p.BN = 32;
+    S = std::max(1, std::min({(int)((sms + n_tiles - 1) / n_tiles), p.num_kb / 4, S8_MOST_SPLITS}));
+  } else if (M <= 64) {
+    p.BN = 64;
+    S = ranges(n_tiles, sms);
+  } else if (M <= 128) {
+    p.BN = 2 * n_tiles <= sms ? 64 : 128;
+    S = ranges(n_tiles * ((M + p.BN - 1) / p.BN), places);
+  } else if (M <= 256 && 4 * n_tiles <= places) {
+    p.BN = 128;
+    S = ranges(2 * n_tiles, places);
+  } else {
     p.pair = 1;
     double best = -1.0;
     for (int BN : {256, 192, 128}) {
@@ -445,7 +492,7 @@ GemmPlan plan_gemm_s8(int M, int N, int K) {
         const long units = tiles * s, rounds = (units + pairs - 1) / pairs;
         const double ctas = 2.0 * (units < pairs ? units : pairs), fabric = bytes * ctas / 12.0e6;
         const double us = (double)rounds * ((p.num_kb + s - 1) / s) * (issue > fabric ? issue : fabric) +
-                          (s > 1 ? s * (double)M * N * 8.0 / 10.0e6 : 0.0);
+                          (s > 1 ? 3.0 + s * (double)M * N * 8.0 / 10.0e6 : 0.0);
         if (best < 0.0 || us < best) {
           best = us;
           p.BN = BN;
@@ -453,18 +500,9 @@ GemmPlan plan_gemm_s8(int M, int N, int K) {
         }
       }
     }
-  } else {
-    p.BN = M <= 32 ? 32 : M <= 64 ? 64 : 128;
-    if (M > 64 && n_tiles * ((M + 63) / 64) <= sms) p.BN = 64;
   }
-  p.stages = p.pair ? MAX_STAGES : p.BN == 128 ? 3 : 4;
   p.m_tiles = (M + p.BN - 1) / p.BN;
-  if (S == 0) {
-    const long tiles = (long)p.m_tiles * n_tiles;
-    const bool two_per_sm = p.BN == 128 || (p.BN == 64 && p.m_tiles > 1);
-    S = two_per_sm ? (int)(2L * sms / tiles) : (int)((sms + tiles - 1) / tiles);
-    S = std::max(1, std::min({S, p.num_kb / 4, S8_MOST_SPLITS}));
-  }
+  p.stages = p.pair ? MAX_STAGES : p.BN == 128 ? 3 : n_tiles * p.m_tiles * S <= sms && p.BN == 64 ? 8 : 4;
   p.upc = (p.num_kb + S - 1) / S;
   p.S_max = (p.num_kb + p.upc - 1) / p.upc;
   return p;

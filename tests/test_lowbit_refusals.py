@@ -37,9 +37,9 @@ def test_quantize_rows(dllm):
 
 
 def test_gemm(dllm):
-    need = dllm.lib.dllm_gemm_s8_scratch_bytes(200, 3584, 18944)
+    need = dllm.lib.dllm_gemm_s8_scratch_bytes(384, 1024, 18944)
     assert need > 0 and dllm.lib.dllm_gemm_s8_scratch_bytes(0, 256, 4096) == 0 == dllm.lib.dllm_gemm_s8_scratch_bytes(3, 256, 4096)
-    good = dict(A=P, lda=18944, sa=P, W=P, ldw=18944, sw=P, C=P, dt=0, M=200, N=3584, K=18944, s=P, sb=need)
+    good = dict(A=P, lda=18944, sa=P, W=P, ldw=18944, sw=P, C=P, dt=0, M=384, N=1024, K=18944, s=P, sb=need)
     for bad in (dict(A=None), dict(sa=None), dict(W=None), dict(sw=None), dict(C=None), dict(M=0), dict(N=0), dict(K=0),
                 dict(lda=18952), dict(lda=18928), dict(ldw=18952), dict(ldw=18928), dict(A=P + 8), dict(W=P + 4), dict(dt=3), dict(s=None),
                 dict(sb=need - 1), dict(s=P + 8), dict(C=P + 2)):
