@@ -307,17 +307,71 @@ __global__ void __launch_bounds__(256) s8_finish_kernel(const int* __restrict__ 
 }
 
 // ---------------------------------------------------------------- rows of 8-bit integers
-// A CTA per row; VECS vectors of eight elements per thread stay in registers between the row's maximum and its codes, what
-// is beyond them is read twice.  VEC: rows start on 16-byte boundaries.
+// A CTA per row; QS_VECS vectors of eight elements per thread stay in registers as they were loaded between the row's maximum
+// and its codes, what is beyond them is read twice.  VEC: rows start on 16-byte boundaries.
 constexpr int QS_VECS = 4;
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const float4*>(p);
+    b = *reinterpret_cast<const float4*>(p + 4);
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    a = make_float4(v[0], v[1], v[2], v[3]);
+    b = make_float4(v[4], v[5], v[6], v[7]);
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  // largest |x| as its bits: an infinity above every number, a NaN above that
+  __device__ __forceinline__ uint32_t top() const {
+    float v[8];
+    get(v);
+    uint32_t t = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t = max(t, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+    return t;
+  }
+};
+template <>
+struct Raw8<__nv_bfloat16> {
+  uint4 a;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void set(const float (&v)[8]) {   // (numbers that were bf16)
+    a = make_uint4(__byte_perm(__float_as_uint(v[0]), __float_as_uint(v[1]), 0x7632),
+                   __byte_perm(__float_as_uint(v[2]), __float_as_uint(v[3]), 0x7632),
+                   __byte_perm(__float_as_uint(v[4]), __float_as_uint(v[5]), 0x7632),
+                   __byte_perm(__float_as_uint(v[6]), __float_as_uint(v[7]), 0x7632));
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  __device__ __forceinline__ uint32_t top() const {   // two 16-bit magnitudes per instruction
+    const uint32_t t = __vmaxu2(__vmaxu2(a.x & 0x7FFF7FFFu, a.y & 0x7FFF7FFFu), __vmaxu2(a.z & 0x7FFF7FFFu, a.w & 0x7FFF7FFFu));
+    return max(t << 16, t & 0xFFFF0000u);
+  }
+};
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_upto8(const T* p, int left, float (&v)[8]) {
+__device__ __forceinline__ Raw8<T> load_upto8(const T* p, int left) {
+  Raw8<T> r;
   if (VEC && left >= 8) {
-    Vec8<T>::load(p, v);
+    r.load(p);
   } else {
+    float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < left ? to_f32<T>(p[i]) : 0.f;
+    r.set(v);
   }
+  return r;
 }
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(1024) quantize_rows_s8_kernel(const T* __restrict__ x, size_t ldx, int8_t* __restrict__ q,
@@ -328,20 +382,13 @@ __global__ void __launch_bounds__(1024) quantize_rows_s8_kernel(const T* __restr
   const int tid = threadIdx.x, step = blockDim.x * 8;
   const T* row = x + (size_t)blockIdx.x * ldx;
   int8_t* dst = q + (size_t)blockIdx.x * ldq;
-  float v[QS_VECS][8];
-  uint32_t top = 0;   // largest |x| as its bits: an infinity above every number, a NaN above that
+  Raw8<T> v[QS_VECS];
+  uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < QS_VECS; ++i) load_upto8<T, VEC>(row + tid * 8 + i * step, cols - (tid * 8 + i * step), v[i]);
+  for (int i = 0; i < QS_VECS; ++i) v[i] = load_upto8<T, VEC>(row + tid * 8 + i * step, cols - (tid * 8 + i * step));
 #pragma unroll
-  for (int i = 0; i < QS_VECS; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[i][e]) & 0x7FFFFFFFu);
-  for (int c = tid * 8 + QS_VECS * step; c < cols; c += step) {
-    float u[8];
-    load_upto8<T, VEC>(row + c, cols - c, u);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(u[e]) & 0x7FFFFFFFu);
-  }
+  for (int i = 0; i < QS_VECS; ++i) top = max(top, v[i].top());
+  for (int c = tid * 8 + QS_VECS * step; c < cols; c += step) top = max(top, load_upto8<T, VEC>(row + c, cols - c).top());
   top = __reduce_max_sync(0xffffffffu, top);
   if ((tid & 31) == 0) red[tid >> 5] = top;
   __syncthreads();
@@ -349,28 +396,34 @@ __global__ void __launch_bounds__(1024) quantize_rows_s8_kernel(const T* __restr
   const float s = __fdiv_rn(__uint_as_float(top), 127.f);
   const bool zero = s == 0.f || top >= 0x7F800000u;   // codes 0; the scale then shows an infinity or a NaN
   if (tid == 0) scale[blockIdx.x] = s;
-  // The quotient by a product with the reciprocal (off by 2^-22 of at most 127), rounded by adding 1.5 * 2^23; divided where it
-  // lies within 2^-13 of a tie, or where the scale is so small that its reciprocal is not one.
-  const bool tiny = s < 1e-37f;
-  const float inv = tiny ? 0.f : __frcp_rn(s);
-  auto put = [&](int c, const float (&u)[8]) {
+  // The IEEE quotient by a product with the reciprocal and two corrections: behind the first it is within a unit of its last
+  // place, and with a correctly rounded reciprocal the second is then the correctly rounded quotient (Markstein, 1990; not for
+  // a divisor of ones alone, nor where a remainder leaves fp32's range: those are divided).  Rounded to an integer by adding
+  // 1.5 * 2^23.  (A test for near ties with divisions behind it: bf16 rows, whose maximum is a bf16 number, meet one in nearly
+  // every warp; 8192 x 12288 148 us, 112 so, 62 with rows kept as they were loaded.)
+  const bool divide = s < 1e-28f || !(s < INFINITY) || (__float_as_uint(s) & 0x7FFFFFu) == 0x7FFFFFu;
+  const float inv = __frcp_rn(s);
+  auto put = [&](int c, const Raw8<T>& raw) {
+    float u[8];
+    raw.get(u);
     uint32_t code[8];
-    bool divide = tiny;
+    if (!divide) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float p = __fmul_rn(u[e], inv), t = __fadd_rn(p, 12582912.f);
-      divide |= !(fabsf(__fsub_rn(p, __fsub_rn(t, 12582912.f))) < 0.5f - 1.f / 8192.f);
-      code[e] = __float_as_uint(t) & 255u;
-    }
-    if (divide) {
+      for (int e = 0; e < 8; ++e) {
+        float p = __fmul_rn(u[e], inv);
+        p = __fmaf_rn(__fmaf_rn(-p, s, u[e]), inv, p);
+        p = __fmaf_rn(__fmaf_rn(-p, s, u[e]), inv, p);
+        code[e] = __float_as_uint(__fadd_rn(p, 12582912.f));
+      }
+    } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        code[e] = zero ? 0u : (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(u[e], s)), -127.f), 127.f) & 255u;
+        code[e] = zero ? 0u : (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(u[e], s)), -127.f), 127.f);
     }
     if (c + 8 <= cols) {
       uint2 w;
-      w.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-      w.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+      w.x = __byte_perm(__byte_perm(code[0], code[1], 0x0040), __byte_perm(code[2], code[3], 0x0040), 0x5410);
+      w.y = __byte_perm(__byte_perm(code[4], code[5], 0x0040), __byte_perm(code[6], code[7], 0x0040), 0x5410);
       *reinterpret_cast<uint2*>(dst + c) = w;
     } else {
 #pragma unroll
@@ -381,11 +434,7 @@ __global__ void __launch_bounds__(1024) quantize_rows_s8_kernel(const T* __restr
 #pragma unroll
   for (int i = 0; i < QS_VECS; ++i)
     if (tid * 8 + i * step < cols) put(tid * 8 + i * step, v[i]);
-  for (int c = tid * 8 + QS_VECS * step; c < cols; c += step) {
-    float u[8];
-    load_upto8<T, VEC>(row + c, cols - c, u);
-    put(c, u);
-  }
+  for (int c = tid * 8 + QS_VECS * step; c < cols; c += step) put(c, load_upto8<T, VEC>(row + c, cols - c));
 }
 
 template <int BN, bool ONCE, typename T>

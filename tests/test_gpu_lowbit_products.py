@@ -51,6 +51,22 @@ def test_quantize_rows(dllm, rows, cols, pitch, dtype):
     assert q.stride(0) % 16 == 0
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_quantize_rows_at_ties(dllm, dtype):
+    """Rows whose maximum is a short number meet ties, and quotients next to ties, in every other element."""
+    g = gen(3)
+    top = torch.cat([torch.arange(128, 256, device="cuda"), torch.tensor([127.0, 254.0, 1.0], device="cuda")]).float()
+    top = top * 2.0 ** torch.randint(-60, 60, top.shape, generator=g, device="cuda").float()
+    half = (torch.randint(-253, 254, (top.numel(), 4096), generator=g, device="cuda").float() * 0.5)
+    x = (half.double() * (top.double() / 127)[:, None]).float()
+    x = x * (1 + torch.randint(-2, 3, x.shape, generator=g, device="cuda").float() * 2.0 ** -23)
+    x[:, 0] = top
+    x = x.to(dtype)
+    q, s = dllm.quantize_rows_s8(x)
+    codes, scale = ref.quantize_rows_s8(x)
+    assert torch.equal(q.double(), codes) and torch.equal(s.double(), scale)
+
+
 def test_quantize_rows_special_values(dllm):
     x = torch.randn((6, 64), generator=gen(2), device="cuda")
     x[0, 3], x[1, 5], x[2, 63] = float("nan"), float("inf"), -float("inf")
