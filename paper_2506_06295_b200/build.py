@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdllm_b200.so")
 SOURCES = ["api.cu", "elementwise.cu", "gemm_simt.cu", "gemm_tcgen05.cu", "gemm_rows.cu", "attention.cu", "attention_umma.cu",
-           "gemm_s8.cu", "kv4_rows.cu", "kv4_attention.cu", "kv4_umma.cu", "lowbit.cu"]
+           "gemm_s8.cu", "kv4_rows.cu", "kv4_attention.cu", "kv4_umma.cu", "kv4_weights.cu",
+           "lowbit.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-DNDEBUG"]
 

@@ -1358,6 +1358,7 @@ dllm_status dllm_debug_set_wait_limit_ns(uint64_t ns) {
   CU_TRY(nullptr, set_wait_limit_attention_umma(ns));
   CU_TRY(nullptr, set_wait_limit_gemm_s8(ns));
   CU_TRY(nullptr, set_wait_limit_kv4_umma(ns));
+  CU_TRY(nullptr, set_wait_limit_kv4_weights(ns));
   CU_TRY(nullptr, cudaDeviceSynchronize());
   return DLLM_OK;
 }

@@ -77,5 +77,9 @@ cudaError_t launch_kv4_umma(const Launch& L, const void* q, size_t ldq, const Kv
 cudaError_t set_wait_limit_kv4_umma(unsigned long long ns);
 cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                int a, int n, int H, const int32_t* lens);
+// kv4_weights.cu
+cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
+                                    int a, int n, int H, const int32_t* lens);
+cudaError_t set_wait_limit_kv4_weights(unsigned long long ns);
 
 }  // namespace dllm

@@ -18,7 +18,7 @@ namespace dllm {
 namespace {
 
 // rows per KV head above which the tcgen05 kernel is taken
-constexpr int KV4_UMMA_ROWS = 64;
+constexpr int KV4_UMMA_ROWS = 64, KV4_WEIGHTS_ROWS = 64;
 constexpr int KA_THREADS = 128, KA_ROWS = 16, KA_STAGES = 3;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -566,6 +566,7 @@ cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, con
 
 cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                int a, int n, int H, const int32_t* lens) {
+  if ((long)a * (H / c.Hkv) > KV4_WEIGHTS_ROWS) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens);
   const dim3 grid((n + KW_KEYS - 1) / KW_KEYS, c.Hkv, c.B);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)c.hd);
   cudaError_t e = c.hd == 64 ? launch_k(L, kv4_weights_kernel<64>, grid, dim3(128), 0, (const __nv_bfloat16*)q, ldq, c, lse,

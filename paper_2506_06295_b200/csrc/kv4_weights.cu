@@ -1,0 +1,344 @@
+// What every key of the 4-bit cache gets of many rows' attention, on the 5th-generation tensor cores (tcgen05).
+//
+// kv4_weights_umma_kernel: two tiles of 128 keys of one KV head x all rows ((query, head of the group) pairs), or a share of
+// them per CTA of a cluster; thirteen warps with fixed roles:
+//   warps 0-3, 4-7  a thread per key of tile 0 resp. 1: turns its key's codes into an operand row once, then adds up
+//                   2^(s - lse) over the rows, which are the columns of its lane of the accumulator
+//   warp 8          issues the tcgen05.mma: S^T = K Q^T for 128 rows at a time, into one of two accumulators per key tile
+//   warps 9-12      bring the rows in, as they are, and their sums and lse in parts
+// With the keys along the lanes a key's numbers are its thread's registers, and what remains is made part of the product.  With
+// step = m 2^e (1 <= m < 2), v = code - 8, off = lo + 8 step and c = m log2(e) / sqrt(hd)
+//     (s - lse) log2(e) = c * ( q . (v 2^e) + (off / m) sum(q) + (1 / c) (-lse log2(e)) )
+// v 2^e is exact in bf16, so are the rows; the other two products are taken over sixteen more elements, both factors in three
+// bf16 parts (24 bits), the six larger partial products of each.  The thread multiplies by c: a multiplication, an exponential
+// and an addition per score, and the special-function unit's four results per scheduler and cycle are what it takes.
+// Every key is added to by one thread, the rows in their order, the shares of a cluster in theirs.
+#include <algorithm>
+
+#include "kv4.cuh"
+#include "tma.cuh"
+#include "umma.cuh"
+
+namespace dllm {
+
+namespace {
+
+constexpr int WK_TILE = 128, WK_KEYS = 2 * WK_TILE, WK_ROWS = 128, WK_STAGES = 3, WK_THREADS = 13 * 32, WK_MMA_WARP = 8,
+              WK_Q_WARP = 9, WK_CLUSTER = 8;
+
+__device__ __forceinline__ float exp2_sfu(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void put16(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// x as three bf16 (their sum is x)
+__device__ __forceinline__ void parts3(float x, float (&p)[3]) {
+  p[0] = __bfloat162float(__float2bfloat16_rn(x));
+  p[1] = __bfloat162float(__float2bfloat16_rn(x - p[0]));
+  p[2] = x - p[0] - p[1];
+}
+// Sixteen bf16 per row: 32 bytes with the 32-byte swizzle, 8-row groups 256 bytes apart.
+__device__ __forceinline__ uint64_t desc_rows32(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)6 << 61);
+}
+__device__ __forceinline__ void put_rows32(uint32_t base, int row, uint4 lo, uint4 hi) {
+  const uint32_t turn = (uint32_t)((row >> 2) & 1) << 4;
+  put16(base + row * 32 + turn, lo);
+  put16(base + row * 32 + (16u ^ turn), hi);
+}
+
+template <int HD>
+struct WkSmem {
+  static constexpr uint32_t OPERAND = WK_TILE * HD * 2, MORE = WK_TILE * 32;   // 128 rows; their sixteen more elements
+  static constexpr uint32_t KEYS = 2 * (OPERAND + MORE), STAGE = OPERAND + MORE;
+  static constexpr uint32_t TOTAL = KEYS + WK_STAGES * STAGE + 1024;
+};
+
+template <int HD>
+__global__ void __launch_bounds__(WK_THREADS, 1)
+    kv4_weights_umma_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c, const float* __restrict__ lse,
+                            const int32_t* __restrict__ lens, float* __restrict__ weight, int a, int n, int H, int shares,
+                            float scale_log2, int* __restrict__ status) {
+  using SM = WkSmem<HD>;
+  constexpr int CHUNKS = HD / 8;                 // 16-byte chunks of a row
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t k_bar, q_full[WK_STAGES], q_empty[WK_STAGES], d_full[2][2], d_empty[2][2];
+  __shared__ float sums[2][WK_ROWS];
+  __shared__ __align__(16) float total[WK_KEYS];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + SM::KEYS;
+  volatile int* abortp = &abort_flag;
+  const int G = H / c.Hkv, kh = blockIdx.y, b = blockIdx.z, rows = a * G;
+  const int rank = shares > 1 ? (int)cluster_ctarank() : 0, block = blockIdx.x / shares;
+  pdl_wait();
+  pdl_trigger();
+  const int len = lens ? min(max(lens[b], 0), n) : n;
+  if (block * WK_KEYS >= len) return;            // the whole cluster
+  const size_t plane = ((size_t)b * c.Hkv + kh) * c.cap;
+  const int tiles_all = (rows + WK_ROWS - 1) / WK_ROWS, per_share = (tiles_all + shares - 1) / shares;
+  const int tile_lo = min(rank * per_share, tiles_all), n_tiles = min(tile_lo + per_share, tiles_all) - tile_lo;
+  const int key_tiles = block * WK_KEYS + WK_TILE < len ? 2 : 1;
+
+  if (tid == 0) {
+    abort_flag = 0;
+    mbar_init(smem_u32(&k_bar), 8);              // one arrival per warp of the keys' threads
+    for (int i = 0; i < WK_STAGES; ++i) {
+      mbar_init(smem_u32(&q_full[i]), 4);
+      mbar_init(smem_u32(&q_empty[i]), 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&d_full[i >> 1][i & 1]), 1);
+      mbar_init(smem_u32(&d_empty[i >> 1][i & 1]), 4);
+    }
+    mbar_fence_init();
+  }
+  if (warp == WK_MMA_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+  bool ok = true;
+  float got = 0.f;
+
+  if (warp >= WK_Q_WARP) {
+    // ---------------- the rows: 16 (heads of 64: 8) threads per row, all of a batch's loads on their way together ----------------
+    constexpr int SIDE = 128 / CHUNKS, BATCH = 8, PASSES = WK_ROWS / SIDE;
+    const int t = tid - WK_Q_WARP * 32, ch = t % CHUNKS, r0 = t / CHUNKS;
+    const int di = SIDE / G, dg = SIDE - di * G;   // SIDE rows further on
+    int qi = (tile_lo * WK_ROWS + r0) / G, g = tile_lo * WK_ROWS + r0 - qi * G;
+    const __nv_bfloat16* const qb = q + (size_t)b * a * ldq + (size_t)kh * G * HD + ch * 8;
+    for (int u = 0; u < n_tiles; ++u) {
+      const int st = u % WK_STAGES;
+      if (u >= WK_STAGES && !mbar_wait_warp(smem_u32(&q_empty[st]), (uint32_t)(u / WK_STAGES - 1) & 1u, abortp)) {
+        ok = false;
+        break;
+      }
+      const uint32_t to = ring + st * SM::STAGE;
+#pragma unroll
+      for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
+        uint4 x[BATCH];
+#pragma unroll
+        for (int p = 0; p < BATCH; ++p) {
+          x[p] = qi < a ? *reinterpret_cast<const uint4*>(qb + (size_t)qi * ldq + g * HD) : make_uint4(0, 0, 0, 0);
+          qi += di;
+          g += dg;
+          if (g >= G) {
+            g -= G;
+            ++qi;
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < BATCH; ++p) {
+          const int r = (p0 + p) * SIDE + r0;
+          put16(to + (ch >> 3) * (WK_ROWS * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4), x[p]);
+          const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+          float sum = 0.f;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum += __uint_as_float(w[k] << 16) + __uint_as_float(w[k] & 0xFFFF0000u);
+#pragma unroll
+          for (int o = CHUNKS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          if (ch == 0) sums[u & 1][r] = sum;
+        }
+      }
+      asm volatile("bar.sync 3, 128;" ::: "memory");
+      {
+        // a row's sum and its lse in parts; rows past the last one and rows that saw no key: so large that nothing is left
+        const int vr = (tile_lo + u) * WK_ROWS + t;
+        float x = INFINITY;
+        if (vr < rows) {
+          const int i = vr / G;
+          x = lse[((size_t)b * a + i) * H + kh * G + (vr - i * G)];
+          if (x == -INFINITY) x = INFINITY;
+        }
+        x = x > 1e30f ? 1e30f : x < -1e30f ? -1e30f : x;   // (a NaN stays one)
+        float s[3], l[3];
+        parts3(sums[u & 1][t], s);
+        parts3(-1.4426950408889634f * x, l);
+        put_rows32(to + SM::OPERAND, t, make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[0]), bf16_pair(s[1], s[0]), bf16_pair(l[0], l[1])),
+                   make_uint4(bf16_pair(l[2], l[0]), bf16_pair(l[1], l[0]), 0u, 0u));
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&q_full[st]));
+    }
+  } else if (warp == WK_MMA_WARP) {
+    // ---------------- MMA issuer ----------------
+    constexpr uint32_t idesc = make_idesc(WK_TILE, WK_ROWS);
+    ok = mbar_wait_warp(smem_u32(&k_bar), 0u, abortp);
+    for (int u = 0; u < n_tiles && ok; ++u) {
+      const int st = u % WK_STAGES, buf = u & 1;
+      ok = mbar_wait_warp(smem_u32(&q_full[st]), (uint32_t)(u / WK_STAGES) & 1u, abortp);
+      for (int i = 0; i < key_tiles && ok; ++i) {
+        if (u >= 2) ok = mbar_wait_warp(smem_u32(&d_empty[i][buf]), (uint32_t)(u / 2 - 1) & 1u, abortp);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (elect_one()) {
+          const uint32_t keys = base + i * (SM::OPERAND + SM::MORE), row = ring + st * SM::STAGE;
+          const uint32_t d = tmem + (uint32_t)((2 * i + buf) * WK_ROWS);
+          const uint64_t dk = make_smem_desc(keys), dq = make_smem_desc(row);
+#pragma unroll
+          for (int ks = 0; ks < HD / 16; ++ks) {
+            const uint64_t off = (uint64_t)(((ks >> 2) * (128 * 128) + (ks & 3) * 32) >> 4);
+            umma_bf16(d, dk + off, dq + off, idesc, ks > 0 ? 1u : 0u);
+          }
+          umma_bf16(d, desc_rows32(keys + SM::OPERAND), desc_rows32(row + SM::OPERAND), idesc, 1u);
+          umma_commit(smem_u32(&d_full[i][buf]));
+        }
+        __syncwarp();
+      }
+      if (ok && elect_one()) umma_commit(smem_u32(&q_empty[st]));
+      __syncwarp();
+    }
+  } else {
+    // ---------------- the keys ----------------
+    const int i = warp >> 2, row = (warp & 3) * 32 + lane, key = block * WK_KEYS + i * WK_TILE + row;
+    const uint32_t to = base + i * (SM::OPERAND + SM::MORE), d_lane = tmem + (((uint32_t)((warp & 3) * 32)) << 16) + (uint32_t)(2 * i * WK_ROWS);
+    float mul;
+    {
+      const size_t at = plane + min(key, len - 1);
+      uint4 x[HD / 32];
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k) x[k] = *reinterpret_cast<const uint4*>(c.k + at * (HD / 2) + k * 16);
+      const uint32_t pair = c.kp[at];
+      const float step = kv4_step(pair), off = fmaf(8.f, step, kv4_lo(pair));
+      // step = m 2^e; a step of 0 (or too small for a normal bf16): no codes
+      const bool none = fabsf(step) < 1.17549435e-38f;
+      const uint32_t bits = __float_as_uint(step);
+      const float m = none ? 1.f : !(fabsf(step) < INFINITY) ? step : __uint_as_float((bits & 0x807FFFFFu) | 0x3F800000u);
+      const float unit = none || !(fabsf(step) < INFINITY) ? 0.f : __uint_as_float(bits & 0x7F800000u);
+      mul = scale_log2 * m;
+      const __nv_bfloat162 unit2 = __float2bfloat162_rn(unit);
+#pragma unroll
+      for (int k = 0; k < HD / 32; ++k) {
+        const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t p[4];   // elements (0, 1), (2, 3), (4, 5), (6, 7)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = (w[j] >> (8 * e)) & 15u, hi = (w[j] >> (8 * e + 4)) & 15u;
+            const uint32_t v = 0x43004300u | lo | hi << 16;                      // 128 + code, twice
+            const __nv_bfloat162 h = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v),
+                                                     __bfloat162bfloat162(__ushort_as_bfloat16(0x4308))), unit2);
+            p[e] = *reinterpret_cast<const uint32_t*>(&h);
+          }
+          const int chunk = k * 4 + j;
+          put16(to + (chunk >> 3) * (WK_TILE * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), make_uint4(p[0], p[1], p[2], p[3]));
+        }
+      }
+      float o[3], z[3];
+      parts3(off / m, o);
+      parts3(1.f / mul, z);
+      // beside the row's (s0, s1, s2, s0, s1, s0, l0, l1, l2, l0, l1, l0, 0 ..)
+      put_rows32(to + SM::OPERAND, row, make_uint4(bf16_pair(o[0], o[0]), bf16_pair(o[0], o[1]), bf16_pair(o[1], o[2]), bf16_pair(z[0], z[0])),
+                 make_uint4(bf16_pair(z[0], z[1]), bf16_pair(z[1], z[2]), 0u, 0u));
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&k_bar));
+    }
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    for (int u = 0; u < n_tiles && i < key_tiles; ++u) {
+      const int buf = u & 1;
+      ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&d_full[i][buf]), (uint32_t)(u >> 1) & 1u, abortp));
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t d = d_lane + (uint32_t)(buf * WK_ROWS);
+      const int parts = (min(rows - (tile_lo + u) * WK_ROWS, WK_ROWS) + 31) / 32;   // of 32 rows
+      auto add = [&](const uint32_t (&r)[32]) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          const float2 p = make_float2(exp2_sfu(__uint_as_float(r[j]) * mul), exp2_sfu(__uint_as_float(r[j + 1]) * mul));
+          sum[(j >> 1) & 1] = add2(sum[(j >> 1) & 1], p);
+        }
+      };
+      // 32 scores at a time, the next ones on their way out of tensor memory meanwhile
+      uint32_t x[32], y[32];
+      tmem_ld32(d, x);
+      tmem_ld_wait();
+      for (int p = 0; p < parts; p += 2) {
+        if (p + 1 < parts) tmem_ld32(d + (uint32_t)((p + 1) * 32), y);
+        add(x);
+        tmem_ld_wait();
+        if (p + 1 < parts) {
+          if (p + 2 < parts) tmem_ld32(d + (uint32_t)((p + 2) * 32), x);
+          add(y);
+          tmem_ld_wait();
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&d_empty[i][buf]));
+    }
+    got = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+    if (shares > 1) total[i * WK_TILE + row] = got;
+  }
+  ok = __syncthreads_and(ok);
+  if (!ok && tid == 0 && status) atomicCAS(status, ST_OK, ST_TIMEOUT_ATTN_UMMA);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == WK_MMA_WARP)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  const int key = block * WK_KEYS + tid;
+  if (shares > 1) {
+    cluster_sync();
+    if (rank == 0 && tid < WK_KEYS && key < len) {
+      for (int s = 1; s < shares; ++s) {
+        float x;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(cluster_addr(smem_u32(&total[tid]), s)));
+        got += x;
+      }
+    }
+    cluster_sync();   // no CTA leaves while another one reads its sums
+  }
+  if (rank == 0 && tid < WK_KEYS && key < len) weight[plane + key] += got;
+}
+
+template <int HD>
+cudaError_t weights_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, const Kv4& c, const float* lse, float* weight, int a,
+                       int n, int H, const int32_t* lens) {
+  constexpr int SMEM = (int)WkSmem<HD>::TOTAL;
+  static DeviceOnce once;
+  cudaError_t e = once.run(
+      [] { return cudaFuncSetAttribute(kv4_weights_umma_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); });
+  if (e != cudaSuccess) return e;
+  // fewer CTAs than multiprocessors: the rows in shares, a power of two of them
+  const long blocks = (n + WK_KEYS - 1) / WK_KEYS, ctas = blocks * c.Hkv * c.B;
+  const int tiles = (int)(((long)a * (H / c.Hkv) + WK_ROWS - 1) / WK_ROWS);
+  int shares = 1;
+  while (2 * shares <= WK_CLUSTER && 2 * shares <= tiles && ctas * 2 * shares <= sm_count()) shares *= 2;
+  const dim3 grid((unsigned)(blocks * shares), c.Hkv, c.B);
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
+  e = shares == 1 ? launch_k(L, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, q, ldq, c, lse, lens, weight, a, n, H,
+                             shares, scale_log2, L.d_status)
+                  : launch_k_cluster(L, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, dim3(shares, 1, 1), q, ldq, c,
+                                     lse, lens, weight, a, n, H, shares, scale_log2, L.d_status);
+  L.count();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
+                                    int a, int n, int H, const int32_t* lens) {
+  return c.hd == 64 ? weights_as<64>(L, (const __nv_bfloat16*)q, ldq, c, lse, weight, a, n, H, lens)
+                    : weights_as<128>(L, (const __nv_bfloat16*)q, ldq, c, lse, weight, a, n, H, lens);
+}
+
+}  // namespace dllm
+
+DLLM_WAIT_LIMIT_HOOK(kv4_weights)
