@@ -494,9 +494,13 @@ dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache
  * capacity]) += the sum over the a queries and the query heads of KV head h of
  * exp(q . k_j / sqrt(head_dim) - lse), for j below the sequence's length; the other
  * weights stay as they are.  d_lse as dllm_attention_kv4 leaves it; a row whose lse is
- * -infinity gives nothing.  Sums are taken in a fixed order. */
+ * -infinity gives nothing.  Sums are taken in a fixed order.  d_scratch: as many bytes as
+ * the query asks for (NULL where that is 0), 16-byte aligned; calls that may overlap on
+ * the GPU need one each. */
+size_t dllm_attention_weights_kv4_scratch_bytes(int B, int a, int n_heads, int n_kv_heads);
 dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, const float* d_lse,
-                                       float* d_weight, int a, int n, int n_heads, const int32_t* d_lens, void* stream);
+                                       float* d_weight, int a, int n, int n_heads, const int32_t* d_lens, void* d_scratch,
+                                       size_t scratch_bytes, void* stream);
 /* Keeps, per sequence and KV head, min(length, keep) keys: the first `first` and the
  * last `last` of them (response rows, say) and, of the others, those with the largest
  * weights (equal ones: the lowest index; a NaN counts as lowest), in their order; where

@@ -75,11 +75,13 @@ cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, con
 cudaError_t launch_kv4_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n, int H,
                             const int32_t* lens, float* o_part, float2* ml_part, int S);
 cudaError_t set_wait_limit_kv4_umma(unsigned long long ns);
+size_t kv4_weights_scratch_bytes(int B, int a, int H, int Hkv);
 cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
-                               int a, int n, int H, const int32_t* lens);
+                               int a, int n, int H, const int32_t* lens, void* scratch);
 // kv4_weights.cu
+size_t kv4_weights_umma_scratch_bytes(int B, int a, int H, int Hkv);
 cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
-                                    int a, int n, int H, const int32_t* lens);
+                                    int a, int n, int H, const int32_t* lens, void* scratch);
 cudaError_t set_wait_limit_kv4_weights(unsigned long long ns);
 
 }  // namespace dllm

@@ -564,9 +564,13 @@ cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, con
                     : attention_as<128>(L, qb, ldq, c, ob, lse, a, n, H, lens, scratch, scratch_floats);
 }
 
+size_t kv4_weights_scratch_bytes(int B, int a, int H, int Hkv) {
+  return (long)a * (H / Hkv) > KV4_WEIGHTS_ROWS ? kv4_weights_umma_scratch_bytes(B, a, H, Hkv) : 0;
+}
+
 cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
-                               int a, int n, int H, const int32_t* lens) {
-  if ((long)a * (H / c.Hkv) > KV4_WEIGHTS_ROWS) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens);
+                               int a, int n, int H, const int32_t* lens, void* scratch) {
+  if ((long)a * (H / c.Hkv) > KV4_WEIGHTS_ROWS) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens, scratch);
   const dim3 grid((n + KW_KEYS - 1) / KW_KEYS, c.Hkv, c.B);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)c.hd);
   cudaError_t e = c.hd == 64 ? launch_k(L, kv4_weights_kernel<64>, grid, dim3(128), 0, (const __nv_bfloat16*)q, ldq, c, lse,

@@ -5,7 +5,8 @@
 //   warps 0-3, 4-7  a thread per key of tile 0 resp. 1: turns its key's codes into an operand row once, then adds up
 //                   2^(s - lse) over the rows, which are the columns of its lane of the accumulator
 //   warp 8          issues the tcgen05.mma: S^T = K Q^T for 128 rows at a time, into one of two accumulators per key tile
-//   warps 9-12      bring the rows in, as they are, and their sums and lse in parts
+//   warps 9-12      bring the rows in, as they are, and their sums and lse in parts (which kv4_row_parts_kernel has left: made
+//                   here, by every CTA again, they took 4500 cycles per 128 rows instead of the exponentials' 2048)
 // With the keys along the lanes a key's numbers are its thread's registers, and what remains is made part of the product.  With
 // step = m 2^e (1 <= m < 2), v = code - 8, off = lo + 8 step and c = m log2(e) / sqrt(hd)
 //     (s - lse) log2(e) = c * ( q . (v 2^e) + (off / m) sum(q) + (1 / c) (-lse log2(e)) )
@@ -55,6 +56,46 @@ __device__ __forceinline__ void put_rows32(uint32_t base, int row, uint4 lo, uin
   put16(base + row * 32 + (16u ^ turn), hi);
 }
 
+// A row's sum and its lse in parts, 32 bytes per row: [B, Hkv, rows up to a multiple of 128].  Rows past the last one and rows
+// that saw no key: so large an lse that nothing is left.  HD / 8 threads per row.
+template <int HD>
+__global__ void __launch_bounds__(256) kv4_row_parts_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq,
+                                                            const float* __restrict__ lse, uint4* __restrict__ parts, int B, int a,
+                                                            int H, int Hkv, int padded) {
+  constexpr int CHUNKS = HD / 8;
+  pdl_wait();
+  pdl_trigger();
+  const int G = H / Hkv;
+  const size_t unit = (size_t)blockIdx.x * 256 + threadIdx.x, record = unit / CHUNKS;
+  const int ch = (int)(unit % CHUNKS), vr = (int)(record % padded);
+  const size_t head = record / padded;
+  const int kh = (int)(head % Hkv), b = (int)(head / Hkv), i = vr / G, g = vr - i * G;
+  const bool live = b < B && vr < a * G;
+  float sum = 0.f;
+  if (live) {
+    const uint4 x = *reinterpret_cast<const uint4*>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + g) * HD + ch * 8);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum += __uint_as_float(w[k] << 16) + __uint_as_float(w[k] & 0xFFFF0000u);
+  }
+#pragma unroll
+  for (int o = CHUNKS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (ch != 0 || b >= B) return;
+  float x = live ? lse[((size_t)b * a + i) * H + kh * G + g] : INFINITY;
+  if (x == -INFINITY) x = INFINITY;
+  x = x > 1e30f ? 1e30f : x < -1e30f ? -1e30f : x;   // (a NaN stays one)
+  float s[3], l[3];
+  parts3(sum, s);
+  parts3(-1.4426950408889634f * x, l);
+  parts[2 * record] = make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[0]), bf16_pair(s[1], s[0]), bf16_pair(l[0], l[1]));
+  parts[2 * record + 1] = make_uint4(bf16_pair(l[2], l[0]), bf16_pair(l[1], l[0]), 0u, 0u);
+}
+
+// 16 bytes to shared memory; live == false: zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+
 template <int HD>
 struct WkSmem {
   static constexpr uint32_t OPERAND = WK_TILE * HD * 2, MORE = WK_TILE * 32;   // 128 rows; their sixteen more elements
@@ -64,14 +105,13 @@ struct WkSmem {
 
 template <int HD>
 __global__ void __launch_bounds__(WK_THREADS, 1)
-    kv4_weights_umma_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c, const float* __restrict__ lse,
+    kv4_weights_umma_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c, const uint4* __restrict__ parts,
                             const int32_t* __restrict__ lens, float* __restrict__ weight, int a, int n, int H, int shares,
                             float scale_log2, int* __restrict__ status) {
   using SM = WkSmem<HD>;
   constexpr int CHUNKS = HD / 8;                 // 16-byte chunks of a row
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t k_bar, q_full[WK_STAGES], q_empty[WK_STAGES], d_full[2][2], d_empty[2][2];
-  __shared__ float sums[2][WK_ROWS];
   __shared__ __align__(16) float total[WK_KEYS];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
@@ -116,25 +156,25 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
   float got = 0.f;
 
   if (warp >= WK_Q_WARP) {
-    // ---------------- the rows: 16 (heads of 64: 8) threads per row, all of a batch's loads on their way together ----------------
-    constexpr int SIDE = 128 / CHUNKS, BATCH = 8, PASSES = WK_ROWS / SIDE;
+    // ---------------- the rows: 16 (heads of 64: 8) threads per row, two tiles on their way ----------------
+    constexpr int SIDE = 128 / CHUNKS;
     const int t = tid - WK_Q_WARP * 32, ch = t % CHUNKS, r0 = t / CHUNKS;
     const int di = SIDE / G, dg = SIDE - di * G;   // SIDE rows further on
     int qi = (tile_lo * WK_ROWS + r0) / G, g = tile_lo * WK_ROWS + r0 - qi * G;
     const __nv_bfloat16* const qb = q + (size_t)b * a * ldq + (size_t)kh * G * HD + ch * 8;
-    for (int u = 0; u < n_tiles; ++u) {
-      const int st = u % WK_STAGES;
-      if (u >= WK_STAGES && !mbar_wait_warp(smem_u32(&q_empty[st]), (uint32_t)(u / WK_STAGES - 1) & 1u, abortp)) {
-        ok = false;
-        break;
-      }
-      const uint32_t to = ring + st * SM::STAGE;
+    const uint4* const pb = parts + 2 * (((size_t)b * c.Hkv + kh) * tiles_all + tile_lo) * WK_ROWS;
+    for (int u = 0; u <= n_tiles; ++u) {
+      if (u < n_tiles) {
+        const int st = u % WK_STAGES;
+        if (u >= WK_STAGES && !mbar_wait_warp(smem_u32(&q_empty[st]), (uint32_t)(u / WK_STAGES - 1) & 1u, abortp)) {
+          ok = false;
+          break;
+        }
+        const uint32_t to = ring + st * SM::STAGE;
 #pragma unroll
-      for (int p0 = 0; p0 < PASSES; p0 += BATCH) {
-        uint4 x[BATCH];
-#pragma unroll
-        for (int p = 0; p < BATCH; ++p) {
-          x[p] = qi < a ? *reinterpret_cast<const uint4*>(qb + (size_t)qi * ldq + g * HD) : make_uint4(0, 0, 0, 0);
+        for (int p = 0; p < WK_ROWS / SIDE; ++p) {
+          const int r = p * SIDE + r0;
+          copy16(to + (ch >> 3) * (WK_ROWS * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4), qi < a ? qb + (size_t)qi * ldq + g * HD : qb, qi < a);
           qi += di;
           g += dg;
           if (g >= G) {
@@ -142,40 +182,18 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
             ++qi;
           }
         }
-#pragma unroll
-        for (int p = 0; p < BATCH; ++p) {
-          const int r = (p0 + p) * SIDE + r0;
-          put16(to + (ch >> 3) * (WK_ROWS * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4), x[p]);
-          const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-          float sum = 0.f;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) sum += __uint_as_float(w[k] << 16) + __uint_as_float(w[k] & 0xFFFF0000u);
-#pragma unroll
-          for (int o = CHUNKS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-          if (ch == 0) sums[u & 1][r] = sum;
-        }
+        const uint32_t turn = (uint32_t)((t >> 2) & 1) << 4;
+        copy16(to + SM::OPERAND + t * 32 + turn, pb + 2 * ((size_t)u * WK_ROWS + t), true);
+        copy16(to + SM::OPERAND + t * 32 + (16u ^ turn), pb + 2 * ((size_t)u * WK_ROWS + t) + 1, true);
       }
-      asm volatile("bar.sync 3, 128;" ::: "memory");
-      {
-        // a row's sum and its lse in parts; rows past the last one and rows that saw no key: so large that nothing is left
-        const int vr = (tile_lo + u) * WK_ROWS + t;
-        float x = INFINITY;
-        if (vr < rows) {
-          const int i = vr / G;
-          x = lse[((size_t)b * a + i) * H + kh * G + (vr - i * G)];
-          if (x == -INFINITY) x = INFINITY;
-        }
-        x = x > 1e30f ? 1e30f : x < -1e30f ? -1e30f : x;   // (a NaN stays one)
-        float s[3], l[3];
-        parts3(sums[u & 1][t], s);
-        parts3(-1.4426950408889634f * x, l);
-        put_rows32(to + SM::OPERAND, t, make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[0]), bf16_pair(s[1], s[0]), bf16_pair(l[0], l[1])),
-                   make_uint4(bf16_pair(l[2], l[0]), bf16_pair(l[1], l[0]), 0u, 0u));
-      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (u == 0) continue;
+      asm volatile("cp.async.wait_group 1;" ::: "memory");   // the tile before this one
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&q_full[st]));
+      if (lane == 0) mbar_arrive(smem_u32(&q_full[(u - 1) % WK_STAGES]));
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == WK_MMA_WARP) {
     // ---------------- MMA issuer ----------------
     constexpr uint32_t idesc = make_idesc(WK_TILE, WK_ROWS);
@@ -310,7 +328,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
 
 template <int HD>
 cudaError_t weights_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, const Kv4& c, const float* lse, float* weight, int a,
-                       int n, int H, const int32_t* lens) {
+                       int n, int H, const int32_t* lens, uint4* parts) {
   constexpr int SMEM = (int)WkSmem<HD>::TOTAL;
   static DeviceOnce once;
   cudaError_t e = once.run(
@@ -323,20 +341,31 @@ cudaError_t weights_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, cons
   while (2 * shares <= WK_CLUSTER && 2 * shares <= tiles && ctas * 2 * shares <= sm_count()) shares *= 2;
   const dim3 grid((unsigned)(blocks * shares), c.Hkv, c.B);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
-  e = shares == 1 ? launch_k(L, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, q, ldq, c, lse, lens, weight, a, n, H,
-                             shares, scale_log2, L.d_status)
-                  : launch_k_cluster(L, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, dim3(shares, 1, 1), q, ldq, c,
-                                     lse, lens, weight, a, n, H, shares, scale_log2, L.d_status);
+  const size_t threads = (size_t)c.B * c.Hkv * tiles * WK_ROWS * (HD / 8);
+  e = launch_k(L, kv4_row_parts_kernel<HD>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, q, ldq, lse, parts, c.B, a, H,
+               c.Hkv, tiles * WK_ROWS);
+  L.count();
+  if (e != cudaSuccess) return e;
+  Launch behind = L;
+  behind.pdl = true;
+  e = shares == 1 ? launch_k(behind, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, q, ldq, c,
+                             (const uint4*)parts, lens, weight, a, n, H, shares, scale_log2, L.d_status)
+                  : launch_k_cluster(behind, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, dim3(shares, 1, 1), q, ldq, c,
+                                     (const uint4*)parts, lens, weight, a, n, H, shares, scale_log2, L.d_status);
   L.count();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
+size_t kv4_weights_umma_scratch_bytes(int B, int a, int H, int Hkv) {
+  return (size_t)B * Hkv * (((size_t)a * (H / Hkv) + WK_ROWS - 1) / WK_ROWS) * WK_ROWS * 32;
+}
+
 cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
-                                    int a, int n, int H, const int32_t* lens) {
-  return c.hd == 64 ? weights_as<64>(L, (const __nv_bfloat16*)q, ldq, c, lse, weight, a, n, H, lens)
-                    : weights_as<128>(L, (const __nv_bfloat16*)q, ldq, c, lse, weight, a, n, H, lens);
+                                    int a, int n, int H, const int32_t* lens, void* scratch) {
+  return c.hd == 64 ? weights_as<64>(L, (const __nv_bfloat16*)q, ldq, c, lse, weight, a, n, H, lens, (uint4*)scratch)
+                    : weights_as<128>(L, (const __nv_bfloat16*)q, ldq, c, lse, weight, a, n, H, lens, (uint4*)scratch);
 }
 
 }  // namespace dllm

@@ -178,13 +178,22 @@ dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache
               "attention over the 4-bit cache");
 }
 
+size_t dllm_attention_weights_kv4_scratch_bytes(int B, int a, int n_heads, int n_kv_heads) {
+  if (B <= 0 || a <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || (long)a * n_heads > (1L << 30) / B) return 0;
+  return kv4_weights_scratch_bytes(B, a, n_heads, n_kv_heads);
+}
+
 dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, const float* d_lse,
-                                       float* d_weight, int a, int n, int n_heads, const int32_t* d_lens, void* stream) {
+                                       float* d_weight, int a, int n, int n_heads, const int32_t* d_lens, void* d_scratch,
+                                       size_t scratch_bytes, void* stream) {
   Kv4 c;
   TRY(check_cache(cache, &c));
   TRY(check_queries(d_q, ldq, c, a, n, n_heads));
   if (!d_lse || !d_weight) return fail(DLLM_INVALID_ARG, "lse or weight is NULL");
-  return done(launch_kv4_weights(on(stream), d_q, ldq, c, d_lse, d_weight, a, n, n_heads, d_lens), "attention weights");
+  const size_t need = kv4_weights_scratch_bytes(c.B, a, n_heads, c.Hkv);
+  if (need && (!d_scratch || !aligned16(d_scratch) || scratch_bytes < need))
+    return fail(DLLM_INVALID_ARG, "these weights need %zu bytes of 16-byte aligned scratch", need);
+  return done(launch_kv4_weights(on(stream), d_q, ldq, c, d_lse, d_weight, a, n, n_heads, d_lens, d_scratch), "attention weights");
 }
 
 dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, int n, int keep, int first, int last,

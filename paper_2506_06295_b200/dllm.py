@@ -116,7 +116,8 @@ SIGNATURES = {
     "dllm_kv4_load": (_I, [_KV4, _I, _P, _P, _P, _I, _P]),
     "dllm_attention_kv4_scratch_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
     "dllm_attention_kv4": (_I, [_P, _SZ, _KV4, _P, _P, _I, _I, _I, _P, _P, _SZ, _P]),
-    "dllm_attention_weights_kv4": (_I, [_P, _SZ, _KV4, _P, _P, _I, _I, _I, _P, _P]),
+    "dllm_attention_weights_kv4_scratch_bytes": (_SZ, [_I, _I, _I, _I]),
+    "dllm_attention_weights_kv4": (_I, [_P, _SZ, _KV4, _P, _P, _I, _I, _I, _P, _P, _SZ, _P]),
     "dllm_kv4_evict": (_I, [_KV4, _P, _I, _I, _I, _I, _P, _KV4, _P, _P, _P, _P]),
 }
 for _name, (_res, _args) in SIGNATURES.items():
@@ -810,18 +811,21 @@ def attention_kv4(q, cache: KV4Cache, a: int, n: int, H: int, lens=None, scratch
     return o, lse
 
 
-def attention_weights_kv4(q, cache: KV4Cache, lse, weight, a: int, n: int, H: int, lens=None, stream=None) -> None:
+def attention_weights_kv4(q, cache: KV4Cache, lse, weight, a: int, n: int, H: int, lens=None, scratch=None,
+                          stream=None) -> None:
     """Adds to weight (float32 [B, Hkv, capacity]) what every key gets of the rows' attention, summed over the a queries and
     the query heads of its KV head; lse as attention_kv4 returns it."""
     import torch
     if _elsewhere(q, stream):
-        with _Placed(stream, q, *cache.tensors(), lse, weight, lens):
-            return attention_weights_kv4(q, cache, lse, weight, a, n, H, lens)
+        with _Placed(stream, q, *cache.tensors(), lse, weight, lens, scratch):
+            return attention_weights_kv4(q, cache, lse, weight, a, n, H, lens, scratch)
     ldq = _queries(q, cache, a, H)
     _like(lse, torch.float32, (cache.B * a, H), "lse")
     _like(weight, torch.float32, (cache.B, cache.Hkv, cache.capacity), "weight")
+    at, size, keep = _space(q, lib.dllm_attention_weights_kv4_scratch_bytes(cache.B, a, H, cache.Hkv), scratch)
     _check(lib.dllm_attention_weights_kv4(q.data_ptr(), ldq, cache.ref, lse.data_ptr(), weight.data_ptr(), a, n, H,
-                                          _lens(lens, cache), _stream_of(q, cache.k_codes, lse, weight, lens)))
+                                          _lens(lens, cache), at, size,
+                                          _stream_of(q, cache.k_codes, lse, weight, lens, keep)))
 
 
 def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: int = 0, lens=None, to=None, stream=None):

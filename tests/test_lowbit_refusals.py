@@ -85,11 +85,15 @@ def test_attention_and_weights(dllm):
     for bad in (dict(q=None), dict(q=P + 8), dict(ldq=1023), dict(ldq=1016), dict(a=0), dict(n=0), dict(n=129), dict(H=6), dict(H=0)):
         a = {**good, **bad}
         refused(dllm, "dllm_attention_kv4", a["q"], a["ldq"], c, a["o"], a["lse"], a["a"], a["n"], a["H"], None, a["s"], a["sb"], None)
-        refused(dllm, "dllm_attention_weights_kv4", a["q"], a["ldq"], c, P, P, a["a"], a["n"], a["H"], None, None)
+        refused(dllm, "dllm_attention_weights_kv4", a["q"], a["ldq"], c, P, P, a["a"], a["n"], a["H"], None, P, 1 << 40, None)
     for o in (None, P + 8):
         refused(dllm, "dllm_attention_kv4", P, 1024, c, o, P, 3, 128, 8, None, P, need, None)
     for lse, w in ((None, P), (P, None)):
-        refused(dllm, "dllm_attention_weights_kv4", P, 1024, c, lse, w, 3, 128, 8, None, None)
+        refused(dllm, "dllm_attention_weights_kv4", P, 1024, c, lse, w, 3, 128, 8, None, P, 1 << 40, None)
+    need = dllm.lib.dllm_attention_weights_kv4_scratch_bytes(2, 100, 8, 4)
+    assert need > 0
+    for s, sb in ((None, need), (P, need - 1), (P + 8, need)):
+        refused(dllm, "dllm_attention_weights_kv4", P, 1024, c, P, P, 100, 128, 8, None, s, sb, None)
     big = cache(dllm, B=1, Hkv=1, cap=8192)
     need = dllm.lib.dllm_attention_kv4_scratch_bytes(1, 1, 8192, 1, 1, 128)
     assert need > 0
