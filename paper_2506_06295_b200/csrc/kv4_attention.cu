@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "kv4.cuh"
+#include "umma.cuh"
 
 namespace dllm {
 
@@ -32,6 +33,19 @@ __device__ __forceinline__ float exp2_fast(float x) {
 __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmul.rn.f32x2 rd, ra, rb;\n\t"
+      "mov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 // Power of two that brings a number with exponent field `ex` to [2^13, 2^14), and its inverse.  Fields below 20 count as 20.
 __device__ __forceinline__ float kv4_up(int ex) { return __uint_as_float((uint32_t)(267 - max(ex, 20)) << 23); }
@@ -85,7 +99,8 @@ template <int HD>
 struct KaSmem {
   static constexpr int ROW = HD / 2;                                    // bytes of a key's codes
   static constexpr int K = 0, V = KV4_KEYS * ROW, KP = 2 * V, VP = KP + KV4_KEYS * 4, STAGE = VP + KV4_KEYS * 4;
-  static constexpr int WARP = KA_STAGES * STAGE, TOTAL = 4 * WARP;
+  // a warp's ring, and what it makes of a tile's pairs: (step, step, off, off) of two keys of K, the same of V
+  static constexpr int PAR = KA_STAGES * STAGE, WARP = PAR + KV4_KEYS * 16, TOTAL = 4 * WARP;
   static constexpr int XS = HD + 4;                                     // floats per exchanged row
   static_assert(KA_ROWS * XS * 4 <= WARP, "a warp's outputs replace its ring");
   // place of the 16-byte chunk c of a key's V codes: eight keys' same chunks lie in eight different banks
@@ -156,7 +171,8 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
   for (int i = 0; i < HD / 8; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[i][e] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};
+  float m[2] = {-INFINITY, -INFINITY};
+  float2 l[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)}, z[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
   int v_ex = 20;   // exponent field of the largest step of V so far
 
   int stage = 0;
@@ -167,6 +183,19 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
     const uint8_t* kt = ring_g + stage * SM::STAGE;
     const uint32_t vt = ring + stage * SM::STAGE + SM::V;
     const int valid = len - tile * KV4_KEYS;   // >= 1
+
+    // the pairs of two keys per lane as the four numbers that scores and weights take; keys behind the length: no V
+    const uint2 kp = *reinterpret_cast<const uint2*>(kt + SM::KP + lane * 8);
+    uint2 vp = *reinterpret_cast<const uint2*>(kt + SM::VP + lane * 8);
+    if (2 * lane >= valid) vp.x = 0u;
+    if (2 * lane + 1 >= valid) vp.y = 0u;
+    const int ex = max(v_ex, (int)__reduce_max_sync(0xffffffffu, max((vp.x >> 7) & 255u, (vp.y >> 7) & 255u)));
+    const float up = kv4_up(ex);
+    float4* const par = reinterpret_cast<float4*>(ring_g + SM::PAR);
+    par[2 * lane] = make_float4(kv4_step(kp.x), kv4_step(kp.y), fmaf(8.f, kv4_step(kp.x), kv4_lo(kp.x)),
+                                fmaf(8.f, kv4_step(kp.y), kv4_lo(kp.y)));
+    par[2 * lane + 1] = make_float4(kv4_step(vp.x) * up, kv4_step(vp.y) * up, fmaf(8.f, kv4_step(vp.x), kv4_lo(vp.x)),
+                                    fmaf(8.f, kv4_step(vp.y), kv4_lo(vp.y)));
 
     float s[8][4];
 #pragma unroll
@@ -190,28 +219,31 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
         mma_f16_16816(s[nt], aq[2 * i + 1], p[2], p[3]);
       }
     }
-    // scores in log2 units; their maxima
+    __syncwarp();
+    // scores in log2 units; their maxima (two keys of a row per instruction)
     float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) {
-      const uint2 kp = *reinterpret_cast<const uint2*>(kt + SM::KP + (nt * 8 + 2 * t) * 4);
-      const uint32_t pr[2] = {kp.x, kp.y};
+      const float4 k = par[2 * (nt * 4 + t)];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float step = kv4_step(pr[e]), off = fmaf(8.f, step, kv4_lo(pr[e]));
-        const bool out = nt * 8 + 2 * t + e >= valid;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float& x = s[nt][2 * h + e];
-          x = out ? -INFINITY : fmaf(x * step, alpha[h], off * beta[h]);
-          top[h] = fmaxf(top[h], x);
-        }
+      for (int h = 0; h < 2; ++h) {
+        const float2 x = fma2(mul2(make_float2(s[nt][2 * h], s[nt][2 * h + 1]), make_float2(k.x, k.y)), make_float2(alpha[h], alpha[h]),
+                              mul2(make_float2(k.z, k.w), make_float2(beta[h], beta[h])));
+        s[nt][2 * h] = x.x;
+        s[nt][2 * h + 1] = x.y;
       }
     }
-    // the steps of V: two keys per lane
-    const uint2 vp_mine = *reinterpret_cast<const uint2*>(kt + SM::VP + lane * 8);
-    const uint32_t e0 = 2 * lane < valid ? (vp_mine.x >> 7) & 255u : 0u, e1 = 2 * lane + 1 < valid ? (vp_mine.y >> 7) & 255u : 0u;
-    const int ex = max(v_ex, (int)__reduce_max_sync(0xffffffffu, max(e0, e1)));
+    if (valid < KV4_KEYS) {   // the last tile of the sequence
+#pragma unroll
+      for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (nt * 8 + 2 * t + (e & 1) >= valid) s[nt][e] = -INFINITY;
+    }
+#pragma unroll
+    for (int nt = 0; nt < 8; ++nt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) top[h] = max3(top[h], s[nt][2 * h], s[nt][2 * h + 1]);
     float corr[2];
     bool same = ex == v_ex;
 #pragma unroll
@@ -224,11 +256,11 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
       m[h] = now;
     }
     if (!__all_sync(0xffffffffu, same)) {
-      const float shrink = kv4_up(ex) * kv4_down(v_ex);   // 2^(v_ex - ex)
+      const float shrink = up * kv4_down(v_ex);   // 2^(v_ex - ex)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        l[h] *= corr[h];
-        z[h] *= corr[h];
+        l[h].x *= corr[h]; l[h].y *= corr[h];
+        z[h].x *= corr[h]; z[h].y *= corr[h];
         corr[h] *= shrink;
       }
 #pragma unroll
@@ -237,29 +269,24 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
         for (int e = 0; e < 4; ++e) acc[i][e] *= corr[e >> 1];
       v_ex = ex;
     }
-    const float up = kv4_up(v_ex);
-    const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+    const float2 ref[2] = {make_float2(m[0] == -INFINITY ? 0.f : -m[0], m[0] == -INFINITY ? 0.f : -m[0]),
+                           make_float2(m[1] == -INFINITY ? 0.f : -m[1], m[1] == -INFINITY ? 0.f : -m[1])};
+    uint32_t pw[8][2];
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) {
-      const uint2 vp = *reinterpret_cast<const uint2*>(kt + SM::VP + (nt * 8 + 2 * t) * 4);
-      const uint32_t pr[2] = {vp.x, vp.y};
+      const float4 v = par[2 * (nt * 4 + t) + 1];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const bool out = nt * 8 + 2 * t + e >= valid;   // whatever stands there counts for nothing
-        const float step = out ? 0.f : kv4_step(pr[e]), off = out ? 0.f : fmaf(8.f, step, kv4_lo(pr[e])), w = step * up;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float p = exp2_fast(s[nt][2 * h + e] - ref[h]);
-          l[h] += p;
-          z[h] = fmaf(p, off, z[h]);
-          s[nt][2 * h + e] = p * w;
-        }
+      for (int h = 0; h < 2; ++h) {
+        const float2 e = add2(make_float2(s[nt][2 * h], s[nt][2 * h + 1]), ref[h]), p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+        l[h] = add2(l[h], p);
+        z[h] = fma2(p, make_float2(v.z, v.w), z[h]);
+        const float2 w = mul2(p, make_float2(v.x, v.y));
+        pw[nt][h] = half_pair(w.x, w.y);
       }
     }
 #pragma unroll
     for (int ks = 0; ks < KV4_KEYS / 16; ++ks) {
-      const uint32_t ap[4] = {half_pair(s[2 * ks][0], s[2 * ks][1]), half_pair(s[2 * ks][2], s[2 * ks][3]),
-                              half_pair(s[2 * ks + 1][0], s[2 * ks + 1][1]), half_pair(s[2 * ks + 1][2], s[2 * ks + 1][3])};
+      const uint32_t ap[4] = {pw[2 * ks][0], pw[2 * ks][1], pw[2 * ks + 1][0], pw[2 * ks + 1][1]};
 #pragma unroll
       for (int cb = 0; cb < CH / 2; ++cb) {
         const int key = ks * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
@@ -289,14 +316,15 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
   const float down = kv4_down(v_ex);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
+    float lh = l[h].x + l[h].y, zh = z[h].x + z[h].y;
 #pragma unroll
     for (int x = 1; x <= 2; x <<= 1) {
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
-      z[h] += __shfl_xor_sync(0xffffffffu, z[h], x);
+      lh += __shfl_xor_sync(0xffffffffu, lh, x);
+      zh += __shfl_xor_sync(0xffffffffu, zh, x);
     }
     if (t == 0) {
       x_m[warp][g + 8 * h] = m[h];
-      x_l[warp][g + 8 * h] = l[h];
+      x_l[warp][g + 8 * h] = lh;
     }
     // columns 2t and 2t + 1 of block (ch, e) are elements 32 ch + 8t + e and 32 ch + 8t + 4 + e
 #pragma unroll
@@ -306,7 +334,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
         float4 v;
         float* f = &v.x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = fmaf(acc[ch * 4 + e][2 * h + half], down, z[h]);
+        for (int e = 0; e < 4; ++e) f[e] = fmaf(acc[ch * 4 + e][2 * h + half], down, zh);
         *reinterpret_cast<float4*>(xo + (g + 8 * h) * SM::XS + ch * 32 + t * 8 + half * 4) = v;
       }
   }
@@ -361,29 +389,38 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const float* __restric
   const int lane = threadIdx.x & 31;
   const size_t row = (size_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= total) return;
-  float top = -INFINITY;
-  for (int s = lane; s < S; s += 32) top = fmaxf(top, __ldcg(&ml_part[s * total + row].x));
-  top = warp_max(top);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, out[PER];
+  // lane s has split s (and s + 32): all of a row's numbers are on their way at once
+  float2 ml[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+    ml[k] = lane + 32 * k < S ? __ldcg(&ml_part[(size_t)(lane + 32 * k) * total + row]) : make_float2(-INFINITY, 0.f);
+  const float top = warp_max(fmaxf(ml[0].x, ml[1].x));
+  const float ref = top == -INFINITY ? 0.f : top, f0 = exp2_fast(ml[0].x - ref), f1 = exp2_fast(ml[1].x - ref);
+  const float sum = warp_sum(fmaf(f0, ml[0].y, f1 * ml[1].y));
+  float out[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) out[e] = 0.f;
-#pragma unroll 4
-  for (int s = 0; s < S; ++s) {
-    const float2 ml = __ldcg(&ml_part[s * total + row]);
-    const float f = exp2_fast(ml.x - ref);
-    sum = fmaf(f, ml.y, sum);
-    const float* p = o_part + (s * total + row) * HD + lane * PER;
-    float x[PER];
-    if constexpr (PER == 4) {
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
-      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-    } else {
-      const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
-      x[0] = v.x; x[1] = v.y;
+  for (int s0 = 0; s0 < S; s0 += 8) {
+    float x[8][PER];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float* p = o_part + ((size_t)min(s0 + k, S - 1) * total + row) * HD + lane * PER;
+      if constexpr (PER == 4) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+        x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
+      } else {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
+        x[k][0] = v.x; x[k][1] = v.y;
+      }
     }
 #pragma unroll
-    for (int e = 0; e < PER; ++e) out[e] = fmaf(f, x[e], out[e]);
+    for (int k = 0; k < 8; ++k) {
+      const int s = s0 + k;
+      const float f = __shfl_sync(0xffffffffu, s < 32 ? f0 : f1, s & 31);
+      if (s < S)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) out[e] = fmaf(f, x[k][e], out[e]);
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   __nv_bfloat16* dst = o + row * HD + lane * PER;
