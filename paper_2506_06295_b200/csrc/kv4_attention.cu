@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "kv4.cuh"
+#include "tma.cuh"
 #include "umma.cuh"
 
 namespace dllm {
@@ -20,7 +21,7 @@ namespace {
 
 // rows per KV head above which the tcgen05 kernel is taken
 constexpr int KV4_UMMA_ROWS = 64, KV4_WEIGHTS_ROWS = 64;
-constexpr int KA_THREADS = 128, KA_ROWS = 16, KA_STAGES = 3;
+constexpr int KA_THREADS = 128, KA_ROWS = 16, KA_STAGES = 3, KA_CLUSTER = 8;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
                                                               const int32_t* __restrict__ lens,
                                                               __nv_bfloat16* __restrict__ o, float* __restrict__ lse,
                                                               float* __restrict__ o_part, float2* __restrict__ ml_part, int a,
-                                                              int n, int H, int S, float scale_log2) {
+                                                              int n, int H, int S, int clustered, float scale_log2) {
   using SM = KaSmem<HD>;
   constexpr int KS = HD / 16, CH = HD / 32;    // k-steps of Q K^T; 16-byte chunks of a row
   extern __shared__ __align__(128) uint8_t smem[];
@@ -341,22 +342,72 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
   __syncthreads();
   constexpr int PER = HD * KA_ROWS / KA_THREADS;   // consecutive elements per thread
   const int r = tid / (HD / PER), col = tid % (HD / PER) * PER, vr = row0 + r;
-  if (vr >= rows) return;
   float top = x_m[0][r];
 #pragma unroll
   for (int w = 1; w < 4; ++w) top = fmaxf(top, x_m[w][r]);
-  const float ref = top == -INFINITY ? 0.f : top;
   float sum = 0.f, out[PER];
+  {
+    const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-  for (int e = 0; e < PER; ++e) out[e] = 0.f;
+    for (int e = 0; e < PER; ++e) out[e] = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const float f = exp2_fast(x_m[w][r] - ref);
-    const float* x = reinterpret_cast<const float*>(smem + w * SM::WARP) + r * SM::XS + col;
-    sum = fmaf(f, x_l[w][r], sum);
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2_fast(x_m[w][r] - ref);
+      const float* x = reinterpret_cast<const float*>(smem + w * SM::WARP) + r * SM::XS + col;
+      sum = fmaf(f, x_l[w][r], sum);
 #pragma unroll
-    for (int e = 0; e < PER; ++e) out[e] = fmaf(f, x[e], out[e]);
+      for (int e = 0; e < PER; ++e) out[e] = fmaf(f, x[e], out[e]);
+    }
   }
+  if (S > 1 && clustered) {
+    // the splits are a cluster: every CTA's rows in its shared memory, each CTA finishes every S-th one
+    __syncthreads();   // the warps' rows have been read
+    float* const mine = reinterpret_cast<float*>(smem);
+    float2* const my_ml = reinterpret_cast<float2*>(smem + KA_ROWS * SM::XS * 4);
+#pragma unroll
+    for (int e = 0; e < PER; e += 4)
+      *reinterpret_cast<float4*>(mine + r * SM::XS + col + e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
+    if (col == 0) my_ml[r] = make_float2(top, sum);
+    cluster_sync();
+    for (int u = tid; u < KA_ROWS * (HD / 4); u += KA_THREADS) {
+      const int r2 = u / (HD / 4), c4 = u % (HD / 4) * 4, vr2 = row0 + r2;
+      if (r2 % S != split || vr2 >= rows) continue;
+      float2 ml[KA_CLUSTER];
+      float4 x[KA_CLUSTER];
+#pragma unroll
+      for (int k = 0; k < KA_CLUSTER; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k < S) {
+          asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ml[k].x), "=f"(ml[k].y) : "r"(cluster_addr(smem_u32(my_ml + r2), k)));
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(x[k].x), "=f"(x[k].y), "=f"(x[k].z), "=f"(x[k].w)
+                       : "r"(cluster_addr(smem_u32(mine + r2 * SM::XS + c4), k)));
+        }
+      }
+      float t2 = ml[0].x;
+#pragma unroll
+      for (int k = 1; k < KA_CLUSTER; ++k) t2 = fmaxf(t2, ml[k].x);
+      const float ref = t2 == -INFINITY ? 0.f : t2;
+      float l2 = 0.f;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < KA_CLUSTER; ++k) {
+        const float f = exp2_fast(ml[k].x - ref);
+        l2 = fmaf(f, ml[k].y, l2);
+        y.x = fmaf(f, x[k].x, y.x); y.y = fmaf(f, x[k].y, y.y); y.z = fmaf(f, x[k].z, y.z); y.w = fmaf(f, x[k].w, y.w);
+      }
+      const float inv = l2 == 0.f ? 0.f : 1.f / l2;
+      const int i2 = vr2 / G;
+      const size_t orow = ((size_t)b * a + i2) * H + kh * G + (vr2 - i2 * G);
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(y.x * inv, y.y * inv), hi = __floats2bfloat162_rn(y.z * inv, y.w * inv);
+      *reinterpret_cast<uint2*>(o + orow * HD + c4) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      if (lse && c4 == 0) lse[orow] = l2 == 0.f ? -INFINITY : (t2 + log2f(l2)) * 0.69314718055994531f;
+    }
+    cluster_sync();   // no CTA leaves while another one reads its rows
+    return;
+  }
+  if (vr >= rows) return;
   const int i = vr / G;
   const size_t orow = ((size_t)b * a + i) * H + kh * G + (vr - i * G);
   if (S > 1) {
@@ -431,10 +482,11 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const float* __restric
 }
 
 // ---------------------------------------------------------------- weights
-// S^T = v_K Q^T with the keys along the rows: a warp holds 32 keys in registers and goes over all rows of its KV head, 64 at
-// a time in shared memory; a key's probabilities add up in its threads' registers (fp32, in the order of the rows), the four
+// At most KW_ROWS rows per KV head: S^T = v_K Q^T with the keys along the rows.  A CTA makes fp16 operands of the rows once, in
+// shared memory; its warps hold 32 keys each in registers and go over the rows, then take the next keys, whose codes are on
+// their way meanwhile.  A key's probabilities add up in its threads' registers (fp32, in the order of the rows), the four
 // threads of a key at the end.  No two CTAs add to the same key.
-constexpr int KW_KEYS = 128, KW_ROWS = 64;
+constexpr int KW_KEYS = 128, KW_ROWS = KV4_WEIGHTS_ROWS;
 template <int HD>
 __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c,
                                                           const float* __restrict__ lse, const int32_t* __restrict__ lens,
@@ -449,59 +501,66 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
   const int len = lens ? min(max(lens[b], 0), n) : n;
   if (blockIdx.x * KW_KEYS >= len) return;
   const size_t plane = ((size_t)b * c.Hkv + kh) * c.cap;
-  const int key0 = blockIdx.x * KW_KEYS + warp * 32 + g;       // keys key0 + 8 i, i = 0..3
-  uint32_t ak[2][KS][4];
-  float step[4], off[4], got[4];
+  uint32_t w[4][CH], pr[4];      // keys of lane group g: first + 8 i
+  auto fetch = [&](int first) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int key = min(key0 + 8 * i, len - 1);
-    const uint8_t* src = c.k + (plane + key) * (HD / 2) + t * (HD / 8);
-    uint32_t w[CH];
-    if constexpr (HD == 128) {
-      const uint4 x = *reinterpret_cast<const uint4*>(src);
-      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
-    } else {
-      const uint2 x = *reinterpret_cast<const uint2*>(src);
-      w[0] = x.x; w[1] = x.y;
-    }
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      uint32_t p[4];
-      kv4_word(w[k], p);
-      ak[i >> 1][2 * k][i & 1] = p[0];
-      ak[i >> 1][2 * k][2 + (i & 1)] = p[1];
-      ak[i >> 1][2 * k + 1][i & 1] = p[2];
-      ak[i >> 1][2 * k + 1][2 + (i & 1)] = p[3];
-    }
-    const uint32_t pr = c.kp[plane + key];
-    step[i] = kv4_step(pr);
-    off[i] = fmaf(8.f, step[i], kv4_lo(pr));
-    got[i] = 0.f;
-  }
-  for (int base = 0; base < rows; base += KW_ROWS) {
-    __syncthreads();
-#pragma unroll
-    for (int pass = 0; pass < KW_ROWS / 32; ++pass) {
-      const int r = pass * 32 + tid / 4, vr = base + r, i = vr / G, share = tid & 3;
-      const bool live = vr < rows;
-      uint32_t w[HD / 8];
-      float alpha, beta;
-      q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + vr - i * G) * HD, live, share, scale_log2, w, alpha, beta);
-#pragma unroll
-      for (int u = 0; u < UNITS; ++u) qs[u][r][share] = make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]);
-      if (share == 0) {
-        float x = INFINITY;      // rows past the last one and rows that saw no key give nothing
-        if (live) {
-          const float e = lse[((size_t)b * a + i) * H + kh * G + (vr - i * G)];
-          if (e != -INFINITY) x = e * 1.4426950408889634f;
-        }
-        par[r] = make_float4(alpha, beta, x, 0.f);
+    for (int i = 0; i < 4; ++i) {
+      const size_t key = plane + min(first + 8 * i, len - 1);
+      const uint8_t* src = c.k + key * (HD / 2) + t * (HD / 8);
+      if constexpr (HD == 128) {
+        const uint4 x = *reinterpret_cast<const uint4*>(src);
+        w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(src);
+        w[i][0] = x.x; w[i][1] = x.y;
       }
+      pr[i] = c.kp[key];
     }
-    __syncthreads();
+  };
+  int key0 = blockIdx.x * KW_KEYS + warp * 32 + g;
+  fetch(key0);
+#pragma unroll
+  for (int pass = 0; pass < KW_ROWS / 32; ++pass) {
+    const int r = pass * 32 + tid / 4, i = r / G, share = tid & 3;
+    if (pass * 32 >= rows) break;
+    const bool live = r < rows;
+    uint32_t x[HD / 8];
+    float alpha, beta;
+    q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + r - i * G) * HD, live, share, scale_log2, x, alpha, beta);
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) qs[u][r][share] = make_uint4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
+    if (share == 0) {
+      float y = INFINITY;      // rows past the last one and rows that saw no key give nothing
+      if (live) {
+        const float e = lse[((size_t)b * a + i) * H + kh * G + (r - i * G)];
+        if (e != -INFINITY) y = e * 1.4426950408889634f;
+      }
+      par[r] = make_float4(alpha, beta, y, 0.f);
+    }
+  }
+  __syncthreads();
+  for (; key0 - warp * 32 - g < len; key0 += gridDim.x * KW_KEYS) {
+    uint32_t ak[2][KS][4];
+    float step[4], off[4], got[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        uint32_t p[4];
+        kv4_word(w[i][k], p);
+        ak[i >> 1][2 * k][i & 1] = p[0];
+        ak[i >> 1][2 * k][2 + (i & 1)] = p[1];
+        ak[i >> 1][2 * k + 1][i & 1] = p[2];
+        ak[i >> 1][2 * k + 1][2 + (i & 1)] = p[3];
+      }
+      step[i] = kv4_step(pr[i]);
+      off[i] = fmaf(8.f, step[i], kv4_lo(pr[i]));
+      got[i] = 0.f;
+    }
+    fetch(key0 + (int)gridDim.x * KW_KEYS);
 #pragma unroll 2
     for (int nt = 0; nt < KW_ROWS / 8; ++nt) {
-      if (base + nt * 8 >= rows) break;
+      if (nt * 8 >= rows) break;
       float s[2][4];
 #pragma unroll
       for (int i = 0; i < 2; ++i)
@@ -524,12 +583,12 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
           got[i] += exp2_fast(fmaf(s[i >> 1][2 * (i & 1) + e] * step[i], p.x, fmaf(off[i], p.y, -p.z)));
       }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 4; ++i) {
 #pragma unroll
-    for (int x = 1; x <= 2; x <<= 1) got[i] += __shfl_xor_sync(0xffffffffu, got[i], x);
-    if (t == 0 && key0 + 8 * i < len) weight[plane + key0 + 8 * i] += got[i];
+      for (int x = 1; x <= 2; x <<= 1) got[i] += __shfl_xor_sync(0xffffffffu, got[i], x);
+      if (t == 0 && key0 + 8 * i < len) weight[plane + key0 + 8 * i] += got[i];
+    }
   }
 }
 
@@ -537,20 +596,34 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
 struct Kv4Plan {
   bool umma;
   int S;
+  bool clustered;   // the splits merge inside a cluster, without scratch
 };
 Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
   const long rows = (long)a * (H / Hkv), tiles = (n + KV4_KEYS - 1) / KV4_KEYS;
   Kv4Plan p;
   p.umma = rows > KV4_UMMA_ROWS;
-  long S;
+  p.clustered = false;
   if (p.umma) {
     const long base = (rows + 255) / 256 * Hkv * B;    // one CTA per SM
-    S = std::min(sm_count() / base, (tiles + 3) / 4);
-  } else {
-    const long base = (rows + KA_ROWS - 1) / KA_ROWS * Hkv * B;
-    S = std::min(2L * sm_count() / base, (tiles + 3) / 4);   // two CTAs per SM; a tile per warp at least
+    p.S = (int)std::max(1L, std::min({(long)sm_count() / base, (tiles + 3) / 4, 64L}));
+    return p;
   }
-  p.S = (int)std::max(1L, std::min(S, 64L));
+  // What a CTA takes, us (B200): 4.5 at its ends, 1.5 for a tile of each of its four warps, two CTAs to an SM at a time; 4.5 more
+  // where splits are merged, by a cluster of up to eight as by a launch (which a call's host side and scratch make the
+  // dearer one).  Measured / by this: 64 x 768 x 32 heads in 1 / 2 ranges 8.7 / 13.0 (9 / 12), 3 x 4128 x 32 in 1 / 4 / 8 30.0 /
+  // 13.9 / 13.0 (30 / 16.5 / 13.5), 32 x 4128 x 32 in 2 / 4 / 8 21.7 / 20.0 / 27.0 (22.5 / 16.5 / 22.5).
+  const long base = (rows + KA_ROWS - 1) / KA_ROWS * Hkv * B, places = 2L * sm_count();
+  double best = -1.0;
+  for (int S = 1; S <= 64 && S <= tiles; ++S) {
+    if (S > 1 && S < KA_CLUSTER && (S & (S - 1))) continue;   // clusters of a power of two
+    const long per_warp = ((tiles + S - 1) / S + 3) / 4, waves = (base * S + places - 1) / places;
+    const double us = (double)waves * (4.5 + 1.5 * (double)per_warp) + (S > 1 ? 4.5 : 0.0);
+    if (best < 0.0 || us < best) {
+      best = us;
+      p.S = S;
+    }
+  }
+  p.clustered = p.S > 1 && p.S <= KA_CLUSTER;
   return p;
 }
 
@@ -565,19 +638,21 @@ cudaError_t attention_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, co
   const size_t total = (size_t)c.B * a * H, part = total * (HD + 2);
   const Kv4Plan plan = plan_kv4(c.B, a, n, H, c.Hkv);
   int S = plan.S;
-  if (S > 1) S = std::max(1, (int)std::min<size_t>(S, scratch ? scratch_floats / part : 0));
+  if (S > 1 && !plan.clustered) S = std::max(1, (int)std::min<size_t>(S, scratch ? scratch_floats / part : 0));
   float* const o_part = scratch;
-  float2* const ml_part = reinterpret_cast<float2*>(scratch + (S > 1 ? (size_t)S * total * HD : 0));
+  float2* const ml_part = reinterpret_cast<float2*>(scratch + (S > 1 && !plan.clustered ? (size_t)S * total * HD : 0));
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
   const dim3 grid((a * (H / c.Hkv) + KA_ROWS - 1) / KA_ROWS, c.Hkv, c.B * S);
   if (plan.umma) {
     e = launch_kv4_umma(L, q, ldq, c, o, lse, a, n, H, lens, o_part, ml_part, S);
   } else {
-    e = launch_k(L, kv4_attn_kernel<HD>, grid, dim3(KA_THREADS), KaSmem<HD>::TOTAL, q, ldq, c, lens, o, lse, o_part, ml_part, a,
-                 n, H, S, scale_log2);
+    e = plan.clustered ? launch_k_cluster(L, kv4_attn_kernel<HD>, grid, dim3(KA_THREADS), KaSmem<HD>::TOTAL, dim3(1, 1, S), q, ldq,
+                                          c, lens, o, lse, o_part, ml_part, a, n, H, S, 1, scale_log2)
+                       : launch_k(L, kv4_attn_kernel<HD>, grid, dim3(KA_THREADS), KaSmem<HD>::TOTAL, q, ldq, c, lens, o, lse,
+                                  o_part, ml_part, a, n, H, S, 0, scale_log2);
     L.count();
   }
-  if (e != cudaSuccess || S == 1) return e != cudaSuccess ? e : cudaGetLastError();
+  if (e != cudaSuccess || S == 1 || plan.clustered) return e != cudaSuccess ? e : cudaGetLastError();
   Launch behind = L;
   behind.pdl = true;
   e = launch_k(behind, kv4_combine_kernel<HD>, dim3((unsigned)((total + 7) / 8)), dim3(256), 0, (const float*)o_part,
@@ -589,8 +664,9 @@ cudaError_t attention_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, co
 }  // namespace
 
 size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd) {
-  const int S = plan_kv4(B, a, n, H, Hkv).S;
-  return S > 1 ? (size_t)S * B * a * H * (hd + 2) : 0;
+  const Kv4Plan plan = plan_kv4(B, a, n, H, Hkv);
+  const int S = plan.S;
+  return S > 1 && !plan.clustered ? (size_t)S * B * a * H * (hd + 2) : 0;
 }
 
 cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n,
@@ -608,7 +684,9 @@ size_t kv4_weights_scratch_bytes(int B, int a, int H, int Hkv) {
 cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                int a, int n, int H, const int32_t* lens, void* scratch) {
   if ((long)a * (H / c.Hkv) > KV4_WEIGHTS_ROWS) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens, scratch);
-  const dim3 grid((n + KW_KEYS - 1) / KW_KEYS, c.Hkv, c.B);
+  // three CTAs to an SM, each over its share of the keys
+  const long blocks = (n + KW_KEYS - 1) / KW_KEYS, heads = (long)c.Hkv * c.B;
+  const dim3 grid((unsigned)std::max(1L, std::min(blocks, (3L * sm_count() + heads - 1) / heads)), c.Hkv, c.B);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)c.hd);
   cudaError_t e = c.hd == 64 ? launch_k(L, kv4_weights_kernel<64>, grid, dim3(128), 0, (const __nv_bfloat16*)q, ldq, c, lse,
                                         lens, weight, a, n, H, scale_log2)
