@@ -490,6 +490,12 @@ size_t dllm_attention_kv4_scratch_bytes(int B, int a, int n, int n_heads, int n_
 dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, void* d_o, float* d_lse, int a,
                                int n, int n_heads, const int32_t* d_lens, void* d_scratch, size_t scratch_bytes,
                                void* stream);
+/* Tuning / test hook, for every later call in this process: the kernel of the two
+ * calls below and above (0 automatic; 1 the few-rows kernel, the weights' for at most
+ * 64 rows per KV head; 2 the tcgen05 kernel) and the number of key ranges the attention
+ * is cut into (0 automatic).  Scratch sizes follow it.  Results stay within the same
+ * bounds. */
+dllm_status dllm_debug_kv4_plan(int kernel, int splits);
 /* What every key gets of the rows' attention: d_weight[b, h, j] (float [B, n_kv_heads,
  * capacity]) += the sum over the a queries and the query heads of KV head h of
  * exp(q . k_j / sqrt(head_dim) - lse), for j below the sequence's length; the other

@@ -68,6 +68,7 @@ cudaError_t launch_kv4_load(const Launch& L, const Kv4& c, int n, const int32_t*
 cudaError_t launch_kv4_evict(const Launch& L, const Kv4& src, const float* weight, int n, int keep, int first, int last,
                              const int32_t* lens, const Kv4& dst, float* dst_weight, int32_t* index, int32_t* new_lens);
 // kv4_attention.cu
+void set_kv4_plan(int kernel, int splits);   // dllm_debug_kv4_plan
 size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd);
 cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n,
                                  int H, const int32_t* lens, float* scratch, size_t scratch_floats);

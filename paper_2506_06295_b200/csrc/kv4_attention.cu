@@ -19,8 +19,7 @@ namespace dllm {
 
 namespace {
 
-// rows per KV head above which the tcgen05 kernel is taken
-constexpr int KV4_UMMA_ROWS = 64, KV4_WEIGHTS_ROWS = 64;
+constexpr int KV4_WEIGHTS_ROWS = 64;   // rows per KV head above which the weights take the tcgen05 kernel
 constexpr int KA_THREADS = 128, KA_ROWS = 16, KA_STAGES = 3, KA_CLUSTER = 8;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -592,38 +591,48 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
   }
 }
 
-// Which kernel, and how many ranges the keys are cut into.
+// Which kernel, and how many ranges the keys are cut into, by what they take (us, B200):
+//   few rows   16 rows a CTA, two CTAs to an SM: 4.5 at its ends, and for a tile of 64 keys of each of its four warps 1.5, 2.1
+//              beside a second CTA; 4.5 more where ranges are merged, by a cluster of up to eight as by a launch (which a call's
+//              host side and scratch make the dearer one)
+//   tcgen05    256 rows a CTA, one to an SM: 12 at its ends, 2.3 for a tile of 128 keys, 5 for a merge and its bytes
+// Measured / by this, few rows then tcgen05, each in its best number of ranges:  64 x 768 x 32 heads 8.7 / 9, 17 / 18;
+// 128 x 768 x 32 12.7 / 10.8, 17.8 / 18;  256 x 768 x 32 23 / 22, 24.7 / 26;  512 x 1024 x 32 47 / 52, 33 / 30;  128 x 512 x 28 on 4
+// 10.1 / 8.7, 21 / 21;  100 x 16384 x 8 48 / 43, 32 / 36;  16 sequences of 80 x 1536 x 32 158 / 154, 132 / 158;  8 of 16 x 32768 x
+// 28 on 4 270 / 273, 155 / 164.
 struct Kv4Plan {
-  bool umma;
-  int S;
-  bool clustered;   // the splits merge inside a cluster, without scratch
+  bool umma = false;
+  int S = 1;
+  bool clustered = false;   // the splits merge inside a cluster, without scratch
 };
+int g_kernel = 0, g_splits = 0;   // dllm_debug_kv4_plan
+
 Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
-  const long rows = (long)a * (H / Hkv), tiles = (n + KV4_KEYS - 1) / KV4_KEYS;
+  const long rows = (long)a * (H / Hkv), heads = (long)Hkv * B, tiles = (n + KV4_KEYS - 1) / KV4_KEYS, sms = sm_count();
   Kv4Plan p;
-  p.umma = rows > KV4_UMMA_ROWS;
-  p.clustered = false;
-  if (p.umma) {
-    const long base = (rows + 255) / 256 * Hkv * B;    // one CTA per SM
-    p.S = (int)std::max(1L, std::min({(long)sm_count() / base, (tiles + 3) / 4, 64L}));
-    return p;
-  }
-  // What a CTA takes, us (B200): 4.5 at its ends, 1.5 for a tile of each of its four warps, two CTAs to an SM at a time; 4.5 more
-  // where splits are merged, by a cluster of up to eight as by a launch (which a call's host side and scratch make the
-  // dearer one).  Measured / by this: 64 x 768 x 32 heads in 1 / 2 ranges 8.7 / 13.0 (9 / 12), 3 x 4128 x 32 in 1 / 4 / 8 30.0 /
-  // 13.9 / 13.0 (30 / 16.5 / 13.5), 32 x 4128 x 32 in 2 / 4 / 8 21.7 / 20.0 / 27.0 (22.5 / 16.5 / 22.5).
-  const long base = (rows + KA_ROWS - 1) / KA_ROWS * Hkv * B, places = 2L * sm_count();
   double best = -1.0;
-  for (int S = 1; S <= 64 && S <= tiles; ++S) {
+  const long few = (rows + KA_ROWS - 1) / KA_ROWS * heads;
+  for (int S = 1; S <= 64 && S <= tiles && g_kernel != 2; ++S) {
     if (S > 1 && S < KA_CLUSTER && (S & (S - 1))) continue;   // clusters of a power of two
-    const long per_warp = ((tiles + S - 1) / S + 3) / 4, waves = (base * S + places - 1) / places;
-    const double us = (double)waves * (4.5 + 1.5 * (double)per_warp) + (S > 1 ? 4.5 : 0.0);
+    const long per_warp = ((tiles + S - 1) / S + 3) / 4, waves = (few * S + 2 * sms - 1) / (2 * sms);
+    const double us = (double)waves * (4.5 + (few * S > sms ? 2.1 : 1.5) * (double)per_warp) + (S > 1 ? 4.5 : 0.0);
     if (best < 0.0 || us < best) {
       best = us;
       p.S = S;
     }
   }
-  p.clustered = p.S > 1 && p.S <= KA_CLUSTER;
+  const long many = (rows + 255) / 256 * heads, wide = (tiles + 1) / 2;
+  for (int S = 1; (rows > KA_ROWS || g_kernel == 2) && g_kernel != 1 && S <= 64 && S <= wide; ++S) {
+    const long waves = (many * S + sms - 1) / sms;
+    const double us = (double)waves * (12.0 + 2.3 * (double)((wide + S - 1) / S)) + (S > 1 ? 5.0 + S * (double)B * a * H * 1040.0 / 10.0e6 : 0.0);
+    if (best < 0.0 || us < best) {
+      best = us;
+      p.S = S;
+      p.umma = true;
+    }
+  }
+  if (g_splits > 0) p.S = (int)std::min<long>(g_splits, p.umma ? wide : tiles);
+  p.clustered = !p.umma && p.S > 1 && p.S <= KA_CLUSTER && !(p.S & (p.S - 1));
   return p;
 }
 
@@ -677,13 +686,20 @@ cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, con
                     : attention_as<128>(L, qb, ldq, c, ob, lse, a, n, H, lens, scratch, scratch_floats);
 }
 
+void set_kv4_plan(int kernel, int splits) {
+  g_kernel = kernel;
+  g_splits = splits;
+}
+
+static bool weights_on_umma(int a, int H, int Hkv) { return g_kernel == 2 || (long)a * (H / Hkv) > KV4_WEIGHTS_ROWS; }
+
 size_t kv4_weights_scratch_bytes(int B, int a, int H, int Hkv) {
-  return (long)a * (H / Hkv) > KV4_WEIGHTS_ROWS ? kv4_weights_umma_scratch_bytes(B, a, H, Hkv) : 0;
+  return weights_on_umma(a, H, Hkv) ? kv4_weights_umma_scratch_bytes(B, a, H, Hkv) : 0;
 }
 
 cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                int a, int n, int H, const int32_t* lens, void* scratch) {
-  if ((long)a * (H / c.Hkv) > KV4_WEIGHTS_ROWS) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens, scratch);
+  if (weights_on_umma(a, H, c.Hkv)) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens, scratch);
   // three CTAs to an SM, each over its share of the keys
   const long blocks = (n + KW_KEYS - 1) / KW_KEYS, heads = (long)c.Hkv * c.B;
   const dim3 grid((unsigned)std::max(1L, std::min(blocks, (3L * sm_count() + heads - 1) / heads)), c.Hkv, c.B);

@@ -157,6 +157,13 @@ dllm_status dllm_kv4_load(const dllm_kv4_cache* cache, int n, const int32_t* d_l
   return done(launch_kv4_load(on(stream), c, n, d_lens, d_k, d_v, dtype), "4-bit load");
 }
 
+dllm_status dllm_debug_kv4_plan(int kernel, int splits) {
+  if (kernel < 0 || kernel > 2 || splits < 0 || splits > 64)
+    return fail(DLLM_INVALID_ARG, "dllm_debug_kv4_plan: kernel 0, 1 or 2, splits 0 to 64");
+  set_kv4_plan(kernel, splits);
+  return DLLM_OK;
+}
+
 size_t dllm_attention_kv4_scratch_bytes(int B, int a, int n, int n_heads, int n_kv_heads, int head_dim) {
   if (B <= 0 || a <= 0 || n <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128) ||
       (long)a * n_heads > (1L << 30) / B)

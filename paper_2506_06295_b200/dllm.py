@@ -116,6 +116,7 @@ SIGNATURES = {
     "dllm_kv4_load": (_I, [_KV4, _I, _P, _P, _P, _I, _P]),
     "dllm_attention_kv4_scratch_bytes": (_SZ, [_I, _I, _I, _I, _I, _I]),
     "dllm_attention_kv4": (_I, [_P, _SZ, _KV4, _P, _P, _I, _I, _I, _P, _P, _SZ, _P]),
+    "dllm_debug_kv4_plan": (_I, [_I, _I]),
     "dllm_attention_weights_kv4_scratch_bytes": (_SZ, [_I, _I, _I, _I]),
     "dllm_attention_weights_kv4": (_I, [_P, _SZ, _KV4, _P, _P, _I, _I, _I, _P, _P, _SZ, _P]),
     "dllm_kv4_evict": (_I, [_KV4, _P, _I, _I, _I, _I, _P, _KV4, _P, _P, _P, _P]),
@@ -850,3 +851,8 @@ def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: 
                               new_weight.data_ptr(), index.data_ptr(), new_lens.data_ptr(),
                               _stream_of(cache.k_codes, weight, lens, to.k_codes)))
     return to, new_weight, index, new_lens
+
+
+def debug_kv4_plan(kernel: int = 0, splits: int = 0) -> None:
+    """Tuning / test hook: kernel (1 few rows, 2 tcgen05) and key ranges of the 4-bit cache's attention (0: automatic)."""
+    _check(lib.dllm_debug_kv4_plan(kernel, splits))

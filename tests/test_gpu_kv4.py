@@ -113,6 +113,14 @@ def test_rows_without_a_spread_and_without_numbers(dllm):
 
 
 # ---------------------------------------------------------------- attention
+@pytest.fixture(params=[(0, 0), (1, 1), (1, 4), (1, 11), (2, 1), (2, 3)], ids=lambda p: f"kernel{p[0]}-ranges{p[1]}")
+def plan(request, dllm):
+    """The plan's own choice, and both kernels with one range of keys, merged in a cluster and by a launch."""
+    dllm.debug_kv4_plan(*request.param)
+    yield request.param
+    dllm.debug_kv4_plan()
+
+
 SHAPES = [  # B, a, n, H, Hkv, hd, lens
     (1, 1, 1, 1, 1, 64, None),
     (1, 1, 1, 7, 1, 128, None),
@@ -147,7 +155,7 @@ def check_attention(q, cache, a, n, H, lens, o, lse):
 
 
 @pytest.mark.parametrize("B,a,n,H,Hkv,hd,lens", SHAPES)
-def test_attention(dllm, B, a, n, H, Hkv, hd, lens):
+def test_attention(dllm, plan, B, a, n, H, Hkv, hd, lens):
     g = gen(n + a)
     cache = ref.random_cache(dllm, g, B, Hkv, -(-n // 64) * 64, hd)
     q, lens = queries(g, B, a, H, hd), lens_of(lens)
@@ -160,7 +168,7 @@ def test_attention(dllm, B, a, n, H, Hkv, hd, lens):
 
 @pytest.mark.parametrize("a,H,Hkv,n", [(2, 8, 2, 150), (90, 8, 2, 700)])
 @pytest.mark.parametrize("hd", [64, 128])
-def test_attention_ignores_what_lies_behind_a_length(dllm, hd, a, H, Hkv, n):
+def test_attention_ignores_what_lies_behind_a_length(dllm, plan, hd, a, H, Hkv, n):
     """NaN, infinities and the largest numbers behind every length, inside of a tile and behind n; rows of Q inside of wider rows."""
     g = gen(5)
     cap = -(-n // 64) * 64
@@ -186,7 +194,7 @@ def test_attention_ignores_what_lies_behind_a_length(dllm, hd, a, H, Hkv, n):
 
 
 @pytest.mark.parametrize("a", [3, 80])
-def test_attention_of_a_row_with_a_nan(dllm, a):
+def test_attention_of_a_row_with_a_nan(dllm, plan, a):
     """A NaN among the keys or values of one head shows in that head's rows and in no other's; so does one in a query."""
     g = gen(6)
     cache = ref.random_cache(dllm, g, 1, 2, 192, 128)
@@ -209,7 +217,7 @@ def test_attention_of_a_row_with_a_nan(dllm, a):
 
 @pytest.mark.parametrize("a,qs,cs", [(4, 40.0, 1.0), (100, 40.0, 1.0), (4, 1e-30, 1.0), (4, 1e30, 1e-30), (100, 1e30, 1e-30), (4, 1.0, 1e-20),
                                      (100, 1.0, 1e-20), (4, 1e-4, 1e4), (100, 1e-4, 1e4)])
-def test_attention_of_very_large_and_very_small_numbers(dllm, a, qs, cs):
+def test_attention_of_very_large_and_very_small_numbers(dllm, plan, a, qs, cs):
     """One key ahead of all others, scores of zero, numbers near the ends of bf16's range."""
     g = gen(7)
     cache = ref.random_cache(dllm, g, 1, 2, 320, 128, scale=cs)
@@ -219,7 +227,7 @@ def test_attention_of_very_large_and_very_small_numbers(dllm, a, qs, cs):
 
 
 @pytest.mark.parametrize("a", [4, 100])
-def test_attention_over_values_of_very_different_steps(dllm, a):
+def test_attention_over_values_of_very_different_steps(dllm, plan, a):
     g = gen(8)
     cache = ref.random_cache(dllm, g, 1, 1, 640, 128)
     cache.v_params.mul_(2.0 ** torch.randint(-12, 13, (1, 1, 640, 1), generator=g, device="cuda").float())
@@ -235,8 +243,10 @@ def test_attention_over_values_of_very_different_steps(dllm, a):
     assert bool(((lse.double().reshape(wl.shape) - wl).abs() <= se + 2.0 ** -23 * wl.abs()).all())
 
 
-def test_attention_past_four_gigabytes(dllm):
+def test_attention_past_four_gigabytes(dllm, plan):
     """The last plane of a cache whose codes take 4.3 GB a tensor."""
+    if plan[1] == 1 or plan == (1, 4):
+        pytest.skip("eight million keys in few ranges: enough in the others")
     B, Hkv, cap, hd = 1, 8, 64 * 131200, 128
     cache = dllm.KV4Cache(B, Hkv, cap, hd)
     assert cache.k_codes.numel() > 2 ** 32
@@ -288,7 +298,7 @@ def test_attention_on_another_stream_and_in_a_graph(dllm, n):
 
 # ---------------------------------------------------------------- weights
 @pytest.mark.parametrize("B,a,n,H,Hkv,hd,lens", SHAPES)
-def test_weights(dllm, B, a, n, H, Hkv, hd, lens):
+def test_weights(dllm, plan, B, a, n, H, Hkv, hd, lens):
     g = gen(n + 2 * a)
     cap = -(-n // 64) * 64
     cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
