@@ -607,6 +607,8 @@ def _stream_of(*tensors) -> int:
 def _row_pitch(t, cols: int, name: str) -> int:
     """Elements between the rows of [..., rows, cols] whose rows are evenly spaced through all leading dimensions."""
     shape, strides = t.shape, t.stride()
+    if len(shape) == 2 and shape[1] == cols and strides[1] == 1 and shape[0] > 1:
+        return strides[0]
     if len(shape) < 2 or shape[-1] != cols or (strides[-1] != 1 and cols > 1):
         _refuse(f"{name}: rows of {cols} adjacent elements are needed")
     rows, pitch = 1, 0
@@ -627,7 +629,7 @@ def _space(x, need: int, scratch):
     if scratch is None:
         if not need:
             return None, 0, None
-        t = torch.empty(need, dtype=torch.uint8, device=x.device)
+        t = x.new_empty(need, dtype=torch.uint8)
         return t.data_ptr(), need, t
     if not scratch.is_contiguous():
         _refuse("scratch must be contiguous")
@@ -645,8 +647,8 @@ def quantize_rows_s8(x, stream=None):
         _refuse("x must be a matrix")
     rows, cols = x.shape
     ldq = -(-cols // 16) * 16
-    q = torch.empty((rows, ldq), dtype=torch.int8, device=x.device)
-    scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    q = x.new_empty((rows, ldq), dtype=torch.int8)
+    scale = x.new_empty((rows,), dtype=torch.float32)
     _check(lib.dllm_quantize_rows_s8(x.data_ptr(), _row_pitch(x, cols, "x"), _dtype(x), q.data_ptr(), ldq, scale.data_ptr(),
                                      rows, cols, _stream_of(x)))
     return q[:, :cols], scale
@@ -663,7 +665,7 @@ def _product(x, W, w_scale, out_dtype, out):
     if out is not None:
         _like(out, out.dtype if out_dtype is None else out_dtype, (M, N), "out")
     else:
-        out = torch.empty((M, N), dtype=torch.float32 if out_dtype is None else out_dtype, device=x.device)
+        out = x.new_empty((M, N), dtype=torch.float32 if out_dtype is None else out_dtype)
     return M, N, K, out
 
 
@@ -707,15 +709,9 @@ class KV4Cache:
 
     def __init__(self, B: int, Hkv: int, capacity: int, hd: int, device="cuda:0"):
         import torch
-        self._bind(*self._tensors(torch.zeros, B, Hkv, capacity, hd, device))
-
-    @staticmethod
-    def _tensors(make, B, Hkv, capacity, hd, device):
-        import torch
         cap = -(-capacity // 64) * 64
-        codes, pairs = (B, Hkv, cap, hd // 2), (B, Hkv, cap, 2)
-        return (make(codes, dtype=torch.uint8, device=device), make(pairs, dtype=torch.bfloat16, device=device),
-                make(codes, dtype=torch.uint8, device=device), make(pairs, dtype=torch.bfloat16, device=device))
+        self._bind(*(torch.zeros((B, Hkv, cap, w), dtype=dt, device=device)
+                     for w, dt in ((hd // 2, torch.uint8), (2, torch.bfloat16)) * 2))
 
     @classmethod
     def from_tensors(cls, k_codes, k_params, v_codes, v_params) -> "KV4Cache":
@@ -723,6 +719,15 @@ class KV4Cache:
         self = cls.__new__(cls)
         self._bind(k_codes, k_params, v_codes, v_params)
         return self
+
+    def _new_like(self, capacity: int) -> "KV4Cache":
+        """A cache of the same sequences, heads and head size whose rows hold nothing yet."""
+        B, Hkv, cap, half = self.B, self.Hkv, -(-capacity // 64) * 64, self.hd // 2
+        codes, pairs = self.k_codes.new_empty, self.k_params.new_empty
+        new = KV4Cache.__new__(KV4Cache)
+        new._hold(codes((B, Hkv, cap, half)), pairs((B, Hkv, cap, 2)), codes((B, Hkv, cap, half)), pairs((B, Hkv, cap, 2)),
+                  B, Hkv, cap, half)
+        return new
 
     def _bind(self, k_codes, k_params, v_codes, v_params) -> None:
         import torch
@@ -735,6 +740,9 @@ class KV4Cache:
         _like(v_params, torch.bfloat16, (B, Hkv, cap, 2), "v_params")
         if not k_codes.device == k_params.device == v_codes.device == v_params.device:
             _refuse("a cache's tensors must be on one device")
+        self._hold(k_codes, k_params, v_codes, v_params, B, Hkv, cap, half)
+
+    def _hold(self, k_codes, k_params, v_codes, v_params, B, Hkv, cap, half) -> None:
         self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
         self.B, self.Hkv, self.capacity, self.hd, self.device = B, Hkv, cap, 2 * half, k_codes.device
         self.c = Kv4CacheStruct(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(), v_params.data_ptr(),
@@ -782,8 +790,8 @@ def kv4_load(cache: KV4Cache, n: int, lens=None, dtype=None, stream=None):
     if not 0 < n <= cache.capacity:
         _refuse("n must lie within the capacity")
     shape, dtype = (cache.B, n, cache.Hkv * cache.hd), torch.float32 if dtype is None else dtype
-    k = torch.empty(shape, dtype=dtype, device=cache.device)
-    v = torch.empty(shape, dtype=dtype, device=cache.device)
+    k = cache.k_codes.new_empty(shape, dtype=dtype)
+    v = k.new_empty(shape)
     _check(lib.dllm_kv4_load(cache.ref, n, _lens(lens, cache), k.data_ptr(), v.data_ptr(), _dtype(k),
                              _stream_of(cache.k_codes, lens)))
     return k, v
@@ -804,8 +812,8 @@ def attention_kv4(q, cache: KV4Cache, a: int, n: int, H: int, lens=None, scratch
         with _Placed(stream, q, *cache.tensors(), lens, scratch):
             return attention_kv4(q, cache, a, n, H, lens, scratch)
     ldq, rows = _queries(q, cache, a, H), cache.B * a
-    o = torch.empty((rows, H * cache.hd), dtype=torch.bfloat16, device=q.device)
-    lse = torch.empty((rows, H), dtype=torch.float32, device=q.device)
+    o = q.new_empty((rows, H * cache.hd))
+    lse = q.new_empty((rows, H), dtype=torch.float32)
     at, size, keep = _space(q, lib.dllm_attention_kv4_scratch_bytes(cache.B, a, n, H, cache.Hkv, cache.hd), scratch)
     _check(lib.dllm_attention_kv4(q.data_ptr(), ldq, cache.ref, o.data_ptr(), lse.data_ptr(), a, n, H, _lens(lens, cache),
                                   at, size, _stream_of(q, cache.k_codes, lens, keep)))
@@ -838,15 +846,15 @@ def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: 
     if _elsewhere(weight, stream):
         with _Placed(stream, weight, *cache.tensors(), lens, *(to.tensors() if to is not None else ())):
             return kv4_evict(cache, weight, n, keep, first, last, lens, to)
-    B, Hkv, dev = cache.B, cache.Hkv, cache.device
+    B, Hkv = cache.B, cache.Hkv
     _like(weight, torch.float32, (B, Hkv, cache.capacity), "weight")
     if keep <= 0:
         _refuse("keep must be positive")
     if to is None:
-        to = KV4Cache.from_tensors(*KV4Cache._tensors(torch.empty, B, Hkv, keep, cache.hd, dev))
-    new_weight = torch.empty((B, Hkv, to.capacity), dtype=torch.float32, device=dev)
-    index = torch.empty((B, Hkv, keep), dtype=torch.int32, device=dev)
-    new_lens = torch.empty((B,), dtype=torch.int32, device=dev)
+        to = cache._new_like(keep)
+    new_weight = weight.new_empty((B, Hkv, to.capacity))
+    index = weight.new_empty((B, Hkv, keep), dtype=torch.int32)
+    new_lens = index.new_empty((B,))
     _check(lib.dllm_kv4_evict(cache.ref, weight.data_ptr(), n, keep, first, last, _lens(lens, cache), to.ref,
                               new_weight.data_ptr(), index.data_ptr(), new_lens.data_ptr(),
                               _stream_of(cache.k_codes, weight, lens, to.k_codes)))
