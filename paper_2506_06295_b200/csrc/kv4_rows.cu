@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(256) kv4_load_kernel(Kv4 c, int n, const int32
 }
 
 // ---------------------------------------------------------------- eviction
-constexpr int EV_THREADS = 512, EV_PER = 8, EV_BINS = 2048, EV_CLUSTER = 8;
+constexpr int EV_THREADS = 512, EV_PER = 8, EV_BINS = 256, EV_CLUSTER = 8;
 constexpr int EV_SMEM_KEYS = 40 * 1024;   // ordered weights that one CTA keeps
 
 // Order of the weights as unsigned numbers; a NaN comes last, -0 and 0 are equal.
@@ -253,19 +253,19 @@ __device__ __forceinline__ int block_scan(int v, int* warps, int& total) {   // 
   const int before = __shfl_sync(0xffffffffu, t, max(w - 1, 0));
   return (w == 0 ? 0 : before) + s - v;
 }
-// 16 bytes from the same place of shared memory in the cluster's CTA `rank`
-__device__ __forceinline__ int4 remote4(const int* p, uint32_t rank) {
-  int4 r;
-  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
-               : "r"(cluster_addr(smem_u32(p), rank)));
+// A number from the same place of shared memory in the cluster's CTA `rank`
+__device__ __forceinline__ int remote(const int* p, uint32_t rank) {
+  int r;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(r) : "r"(cluster_addr(smem_u32(p), rank)));
   return r;
 }
 
 // A cluster of one or eight CTAs per (sequence, KV head), each with its share of the keys (multiples of EV_PER, kept in
-// shared memory as ordered numbers where they fit).  The smallest weight that stays is found digit by digit (11, 11 and 10
-// bits, a histogram each; every CTA adds up all of the cluster's), then each CTA counts its share, and one pass in order
-// writes the places.  Every weight is read once; what is left is the latency of a dozen barriers.
+// shared memory as ordered numbers where they fit).  The smallest weight that stays is found digit by digit (8 bits, a
+// histogram each; every CTA adds up all of the cluster's: with digits of 11 bits the 64 KB that a CTA reads from the others
+// took 7000 cycles a digit), then each thread counts its consecutive keys that stay, and writes them behind those before it.
+// What is left is the latency of a dozen barriers.  (8 x 4 heads of 65536 keys 37 us with 11-bit digits and a scan per 4096
+// keys, 26 so.)
 __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __restrict__ weight, int n, int cap, int Hkv,
                                                                 int keep, int first, int last,
                                                                 const int32_t* __restrict__ lens, int share, int kept_in_smem,
@@ -310,52 +310,48 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __r
     }
   }
   if (need > 0) {
-    for (int shift = 21;;) {
-      for (int i = tid; i < EV_BINS; i += EV_THREADS) hist[i] = 0;
+    for (int shift = 24;; shift -= 8) {
+      if (tid < EV_BINS) hist[tid] = 0;
       __syncthreads();
-      const int bins = shift == 0 ? 1024 : 2048;
       for (int j = j_lo + tid * 4; j < j_hi; j += EV_THREADS * 4) {
         uint32_t k[4];
         four(j, k);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-          if (j + q >= lo && j + q < hi && (k[q] & mask) == prefix) atomicAdd(&hist[(k[q] >> shift) & (bins - 1)], 1);
+          if (j + q >= lo && j + q < hi && (k[q] & mask) == prefix) atomicAdd(&hist[(k[q] >> shift) & (EV_BINS - 1)], 1);
       }
       sync_all();
-      // the bin, counted from the largest, in which the last place goes: four bins per thread
-      static_assert(EV_BINS == 4 * EV_THREADS, "four bins per thread");
-      const int at = EV_BINS - 4 - 4 * tid;
-      int4 c = alone ? *reinterpret_cast<const int4*>(&hist[at]) : make_int4(0, 0, 0, 0);
-      if (!alone) {
+      // the bin, counted from the largest, in which the last place goes: a bin per thread
+      const int at = EV_BINS - 1 - tid;
+      int here = 0;
+      if (tid < EV_BINS) {
+        if (alone) {
+          here = hist[at];
+        } else {
+          int x[EV_CLUSTER];
 #pragma unroll
-        for (int r = 0; r < EV_CLUSTER; ++r) {
-          const int4 x = remote4(&hist[at], r);
-          c.x += x.x; c.y += x.y; c.z += x.z; c.w += x.w;
+          for (int r = 0; r < EV_CLUSTER; ++r) x[r] = remote(&hist[at], r);
+#pragma unroll
+          for (int r = 0; r < EV_CLUSTER; ++r) here += x[r];
         }
       }
-      int total, before = block_scan(c.x + c.y + c.z + c.w, warps, total);
-      const int bin[4] = {c.w, c.z, c.y, c.x};   // largest first
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (before < need && need <= before + bin[i]) {
-          found[0] = at + 3 - i;
-          found[1] = need - before;
-        }
-        before += bin[i];
+      int total;
+      const int before = block_scan(here, warps, total);
+      if (before < need && need <= before + here) {
+        found[0] = at;
+        found[1] = need - before;
       }
       sync_all();   // and no CTA clears a histogram that another one still reads
       prefix |= (uint32_t)found[0] << shift;
-      mask |= (uint32_t)(bins - 1) << shift;
+      mask |= (uint32_t)(EV_BINS - 1) << shift;
       need = found[1];
       if (shift == 0) break;
-      shift = shift == 21 ? 10 : 0;
     }
   }
   __syncthreads();
   // `need` of the keys equal to `prefix` stay, the first ones.  sure: stays whatever the ties do.
-  auto eight = [&](int j0, uint32_t& sure, uint32_t& tie) {
+  auto eight = [&](int j0, int end, uint32_t& sure, uint32_t& tie) {
     sure = tie = 0;
-    if (j0 >= j_hi) return;
     uint32_t k[8];
     if (choose) {
       uint32_t (&k0)[4] = *reinterpret_cast<uint32_t(*)[4]>(&k[0]);
@@ -366,56 +362,60 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __r
 #pragma unroll
     for (int q = 0; q < EV_PER; ++q) {
       const int j = j0 + q;
-      if (j >= j_hi) continue;
+      if (j >= end) continue;
       const bool forced = j < lo || j >= hi;
       if (forced || (mask && k[q] > prefix)) sure |= 1u << q;
       else if (mask && k[q] == prefix) tie |= 1u << q;
     }
   };
-  int sure_before = 0, ties_before = 0;
+  // a thread's keys: consecutive ones, a multiple of EV_PER
+  const int mine = (j_hi - j_lo + EV_THREADS * EV_PER - 1) / (EV_THREADS * EV_PER) * EV_PER;
+  const int m_lo = min(j_lo + tid * mine, j_hi), m_hi = min(m_lo + mine, j_hi);
+  int sures = 0, ties = 0;
+  for (int j0 = m_lo; j0 < m_hi; j0 += EV_PER) {
+    uint32_t sure, tie;
+    eight(j0, m_hi, sure, tie);
+    sures += __popc(sure);
+    ties += __popc(tie);
+  }
+  int all_sures, all_ties;
+  int s = block_scan(sures, warps, all_sures), t = block_scan(ties, warps, all_ties);
   if (!alone) {   // what the CTAs with earlier keys hold
-    int sures = 0, ties = 0;
-    for (int j0 = j_lo + tid * EV_PER; j0 < j_hi; j0 += EV_THREADS * EV_PER) {
-      uint32_t s, t;
-      eight(j0, s, t);
-      sures += __popc(s);
-      ties += __popc(t);
+    if (tid == 0) {
+      counts[0] = all_sures;
+      counts[1] = all_ties;
     }
-    int total;
-    block_scan(sures, warps, total);
-    if (tid == 0) counts[0] = total;
-    block_scan(ties, warps, total);
-    if (tid == 0) counts[1] = total;
     cluster_sync();
-    for (int r = 0; r < rank; ++r) {
-      const int4 x = remote4(counts, r);
-      sure_before += x.x;
-      ties_before += x.y;
+    int x[2][EV_CLUSTER];
+#pragma unroll
+    for (int r = 0; r < EV_CLUSTER; ++r)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) x[k][r] = r < rank ? remote(&counts[k], r) : 0;
+#pragma unroll
+    for (int r = 0; r < EV_CLUSTER; ++r) {
+      s += x[0][r];
+      t += x[1][r];
     }
     cluster_sync();   // no CTA leaves while another one reads its counts
   }
   int32_t* idx = index + (size_t)bh * keep;
   float* dw = dst_weight + (size_t)bh * dst_cap;
-  for (int base = j_lo; base < j_hi; base += EV_THREADS * EV_PER) {
-    const int j0 = base + tid * EV_PER;
+  for (int j0 = m_lo; j0 < m_hi; j0 += EV_PER) {
+    const float4 w0 = *reinterpret_cast<const float4*>(w + j0), w1 = *reinterpret_cast<const float4*>(w + j0 + 4);
+    const float e[EV_PER] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
     uint32_t sure, tie;
-    eight(j0, sure, tie);
-    int total;
-    const int scan = block_scan((__popc(sure) << 16) | __popc(tie), warps, total);
-    int s = sure_before + (scan >> 16), t = ties_before + (scan & 0xFFFF);
+    eight(j0, m_hi, sure, tie);
 #pragma unroll
     for (int q = 0; q < EV_PER; ++q) {
       const bool is_sure = (sure >> q) & 1u, is_tie = (tie >> q) & 1u;
       if (is_sure || (is_tie && t < need)) {
         const int slot = s + min(t, need);
         idx[slot] = j0 + q;
-        dw[slot] = w[j0 + q];
+        dw[slot] = e[q];
       }
       s += is_sure;
       t += is_tie;
     }
-    sure_before += total >> 16;
-    ties_before += total & 0xFFFF;
   }
   if (rank == 0) {
     for (int i = kept + tid; i < dst_cap; i += EV_THREADS) {
@@ -500,7 +500,7 @@ cudaError_t launch_kv4_evict(const Launch& L, const Kv4& src, const float* weigh
     return cudaFuncSetAttribute(kv4_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_SMEM_KEYS * 4);
   });
   if (e != cudaSuccess) return e;
-  // eight CTAs per head where one would make more than two trips over its keys, unless there are CTAs enough
+  // eight CTAs per head from 8192 keys on, unless there are CTAs enough
   const bool alone = n <= 2 * EV_THREADS * EV_PER || heads > 2 * sm_count();
   const int share = alone ? src.cap : (n + EV_CLUSTER * EV_PER - 1) / (EV_CLUSTER * EV_PER) * EV_PER;
   const int mine = alone ? (n + EV_PER - 1) / EV_PER * EV_PER : share, in_smem = mine <= EV_SMEM_KEYS;
