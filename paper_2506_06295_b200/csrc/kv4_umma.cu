@@ -12,8 +12,8 @@
 // the CTA's keys).  The offsets' share of a score is a product of its own over sixteen elements: the row's sum in three fp16
 // parts (33 bits) times lo and times 8 step.  So scores are as good as fp32 sums, and the softmax needs nothing of a key but
 // its score -- the steps and offsets as four numbers per key cost 2048 of a tile's 3900 cycles in shared memory reads alone (a
-// uniform 16-byte read is four wavefronts).  V is rounded to fp16 once, and so is P (2^-11 of each term; bf16 outputs are
-// rounded by 2^-8); the powers of two keep the largest of either below 2^15.  A row's reference follows its maximum when that
+// uniform 16-byte read is four wavefronts).  V's offset lo + 8 step, V and P are each rounded to fp16 (2^-12 and 2^-11 of each
+// term; bf16 outputs are rounded by 2^-9 and more); the powers of two keep the largest of either below 2^15.  A row's reference follows its maximum when that
 // has grown by 2^4.
 // The contraction's order and O's columns are free, so the eight codes of a word stay in the order kv4_word gives, Q enters in
 // it and O leaves it.
@@ -357,7 +357,8 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     if (i < live) {
       // (K's scale: what a converting warp wrote ahead of its first tile)
       ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&kv_full[0]), 0u, abortp));
-      scale *= pow2(top[0] - 133);
+      // at least the smallest normal number: scores that small are all alike, and those behind the length stay -infinity
+      scale = fmaxf(scale * pow2(top[0] - 133), 1.17549435e-38f);
       for (int t = 0; t < n_tiles && ok; ++t) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[i]), (uint32_t)t & 1u, abortp));
         if (!ok) break;

@@ -243,6 +243,58 @@ def test_attention_over_values_of_very_different_steps(dllm, plan, a):
     assert bool(((lse.double().reshape(wl.shape) - wl).abs() <= se + 2.0 ** -23 * wl.abs()).all())
 
 
+@pytest.mark.parametrize("a", [3, 90])
+@pytest.mark.parametrize("kscale", [0.0, 1e-12, 1.0])
+@pytest.mark.parametrize("qscale", [0.0, 1e-38])
+def test_attention_of_queries_of_zeros(dllm, plan, a, kscale, qscale):
+    """Rows of zeros (a padded batch) over keys that were never stored, tiny ones and ordinary ones: every key counts alike, and
+    those behind the length for nothing."""
+    g = gen(12)
+    cache = ref.random_cache(dllm, g, 1, 2, 192, 128, scale=kscale if kscale else 1.0)
+    if kscale == 0.0:
+        cache.k_params.zero_()
+    v = torch.randn((1, 192, 256), generator=g, device="cuda").bfloat16()
+    keep = [t.clone() for t in (cache.k_codes, cache.k_params)]
+    dllm.kv4_store(cache, v, v)
+    cache.k_codes.copy_(keep[0])
+    cache.k_params.copy_(keep[1])
+    q = queries(g, 1, a, 4, 128, scale=qscale)
+    o, lse = dllm.attention_kv4(q, cache, a, 133, 4)
+    check_attention(q, cache, a, 133, 4, None, o, lse)
+    w = torch.zeros((1, 2, 192), device="cuda")
+    dllm.attention_weights_kv4(q, cache, lse, w, a, 133, 4)
+    want, err = ref.weights(q, cache, lse, a, 133, 4)
+    assert bool(((w.double() - want).abs() <= err + 2.0 ** -23 * want).all())
+
+
+def test_calls_on_two_streams_at_once(dllm):
+    """The same products, attention and weights on two streams, each with buffers of its own, twenty times over."""
+    g = gen(13)
+    cache = ref.random_cache(dllm, g, 1, 2, 20480, 128)
+    q = [queries(g, 1, a, 4, 128) for a in (4, 100)]
+    x, (W, sw) = queries(g, 1, 3, 8, 128), dllm.quantize_rows_s8(queries(g, 1, 512, 8, 128))
+
+    def work(i):
+        o, lse = dllm.attention_kv4(q[i], cache, q[i].shape[0], 20001, 4)
+        w = torch.zeros((1, 2, 20480), device="cuda")
+        dllm.attention_weights_kv4(q[i], cache, lse, w, q[i].shape[0], 20001, 4)
+        return o, lse, w, dllm.linear_s8(x, W, sw), *dllm.kv4_evict(cache, w, 20001, 9000)[1:]
+
+    want = [work(i) for i in (0, 1)]
+    torch.cuda.synchronize()
+    sides = [torch.cuda.Stream() for _ in (0, 1)]
+    got = []
+    for _ in range(20):
+        for i in (0, 1):
+            with torch.cuda.stream(sides[i]):
+                got.append((i, work(i)))
+    torch.cuda.synchronize()
+    for i, ts in got:
+        for t, u in zip(ts, want[i]):
+            assert torch.equal(t, u)
+    dllm.kernel_status()
+
+
 def test_attention_past_four_gigabytes(dllm, plan):
     """The last plane of a cache whose codes take 4.3 GB a tensor."""
     if plan[1] == 1 or plan == (1, 4):
@@ -357,6 +409,22 @@ def test_evict(dllm, B, n, keep, first, last, Hkv, hd, lens, ties):
                 assert torch.equal(dst[b, h, :L], src[b, h, rows])
                 assert bool((dst[b, h, L:] == 3).all())                    # rows behind the last one as they were
             assert torch.equal(nw[b, h, :L].nan_to_num(-9), w[b, h, rows].nan_to_num(-9)) and not nw[b, h, L:].any()
+
+
+@pytest.mark.parametrize("Hkv,n,lens", [(300, 41000, None), (300, 300, [41]), (2, 20000, [0]), (2, 20000, [2501]), (2, 330000, None)])
+def test_evict_of_many_heads_and_many_keys(dllm, Hkv, n, lens):
+    """Distinct weights: the kept keys are the largest ones, sorted.  Heads enough for a CTA each, keys beyond what shared memory
+    holds, and lengths that leave most CTAs of a cluster without a key."""
+    g = gen(n + Hkv)
+    cap, keep = -(-n // 64) * 64, min(n // 8, 5000)
+    cache = ref.random_cache(dllm, g, 1, Hkv, cap, 64)
+    w = torch.rand((1, Hkv, cap), generator=g, device="cuda").argsort(-1).float()
+    L = n if lens is None else lens[0]
+    _, nw, index, new = dllm.kv4_evict(cache, w, n, keep, lens=lens_of(lens))
+    kept = min(L, keep)
+    rows = w[..., :L].topk(kept).indices.sort(-1).values
+    assert new.tolist() == [kept] and torch.equal(index[..., :kept].long(), rows) and bool((index[..., kept:] == -1).all())
+    assert torch.equal(nw[..., :kept], w.gather(-1, rows)) and not nw[..., kept:].any()
 
 
 # ---------------------------------------------------------------- as they are used together
