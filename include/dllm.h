@@ -461,7 +461,7 @@ typedef struct {
   void* d_k_params;  /* [B, n_kv_heads, capacity, 2] bf16 (step, lo), 16-byte aligned */
   void* d_v_codes;
   void* d_v_params;
-  int32_t B, n_kv_heads, capacity, head_dim; /* capacity a multiple of 64, head_dim 64 or 128 */
+  int32_t B, n_kv_heads, capacity, head_dim; /* capacity a multiple of 64, at most 2^24; head_dim 64 or 128 */
 } dllm_kv4_cache;
 /* Rows of K and V into the cache.  d_k, d_v: B * a rows of n_kv_heads * head_dim
  * elements of `dtype`, ldk / ldv elements apart (columns of a product for Q, K and V
@@ -513,8 +513,8 @@ dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_k
  * the length is at most keep all stay.  Their K, V and weight go to rows 0, 1, .. of
  * `to` and d_to_weight (float [B, n_kv_heads, to->capacity], zeros behind them),
  * d_index (int32 [B, n_kv_heads, keep]) says where each came from (-1 behind them) and
- * d_to_lens (int32 [B]) how many stayed.  first + last <= keep <= to->capacity; `to`
- * must not overlap `from`.  Positions are in K already (it is cached rotated), so
+ * d_to_lens (int32 [B]) how many stayed.  first + last <= keep <= to->capacity; nothing
+ * that is written may overlap what is read.  Positions are in K already (it is cached rotated), so
  * attention over `to` needs nothing but the new lengths. */
 dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, int n, int keep, int first, int last,
                            const int32_t* d_lens, const dllm_kv4_cache* to, float* d_to_weight, int32_t* d_index,

@@ -612,7 +612,7 @@ Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
   Kv4Plan p;
   double best = -1.0;
   const long few = (rows + KA_ROWS - 1) / KA_ROWS * heads;
-  for (int S = 1; S <= 64 && S <= tiles && g_kernel != 2; ++S) {
+  for (int S = 1; S <= 64 && S <= tiles && (long)S * B <= 65535 && g_kernel != 2; ++S) {
     if (S > 1 && S < KA_CLUSTER && (S & (S - 1))) continue;   // clusters of a power of two
     const long per_warp = ((tiles + S - 1) / S + 3) / 4, waves = (few * S + 2 * sms - 1) / (2 * sms);
     const double us = (double)waves * (4.5 + (few * S > sms ? 2.1 : 1.5) * (double)per_warp) + (S > 1 ? 4.5 : 0.0);
@@ -622,7 +622,7 @@ Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
     }
   }
   const long many = (rows + 255) / 256 * heads, wide = (tiles + 1) / 2;
-  for (int S = 1; (rows > KA_ROWS || g_kernel == 2) && g_kernel != 1 && S <= 64 && S <= wide; ++S) {
+  for (int S = 1; (rows > KA_ROWS || g_kernel == 2) && g_kernel != 1 && S <= 64 && S <= wide && (long)S * B <= 65535; ++S) {
     const long waves = (many * S + sms - 1) / sms;
     const double us = (double)waves * (12.0 + 2.3 * (double)((wide + S - 1) / S)) + (S > 1 ? 5.0 + S * (double)B * a * H * 1040.0 / 10.0e6 : 0.0);
     if (best < 0.0 || us < best) {

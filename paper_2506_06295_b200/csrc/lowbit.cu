@@ -28,10 +28,12 @@ Launch on(void* stream) { return Launch{(cudaStream_t)stream, kernel_status_word
 
 constexpr int MOST_K = 131071;        // 128 * 128 * K stays below 2^31
 constexpr int MOST_N = 65535 * 128;   // weight tiles along a grid dimension
+constexpr int MOST_ROWS = 1 << 30, MOST_COLS = 1 << 30, MOST_KEYS = 1 << 24;   // indices of these and of a tile behind them: 32 bits
 
 dllm_status check_product(const void* W, size_t ldw, const float* sw, const void* C, int out_dtype, int M, int N, int K) {
   if (!W || !sw || !C || M <= 0 || N <= 0 || K <= 0) return fail(DLLM_INVALID_ARG, "bad arguments of an 8-bit product");
-  if (K > MOST_K || N > MOST_N) return fail(DLLM_UNSUPPORTED, "K must be at most %d and N at most %d", MOST_K, MOST_N);
+  if (K > MOST_K || N > MOST_N || M > MOST_ROWS)
+    return fail(DLLM_UNSUPPORTED, "K must be at most %d, N at most %d and M at most %d", MOST_K, MOST_N, MOST_ROWS);
   if (!known_dtype(out_dtype)) return fail(DLLM_INVALID_ARG, "bad output dtype");
   if (ldw % 16 || ldw < (size_t)K || !aligned16(W))
     return fail(DLLM_INVALID_ARG, "rows of W must be 16-byte aligned and at least K bytes apart");
@@ -51,6 +53,7 @@ dllm_status check_cache(const dllm_kv4_cache* c, Kv4* out) {
     return fail(DLLM_INVALID_ARG, "bad 4-bit cache");
   if (c->head_dim != 64 && c->head_dim != 128) return fail(DLLM_UNSUPPORTED, "a 4-bit cache has head_dim 64 or 128");
   if (c->capacity % KV4_KEYS) return fail(DLLM_INVALID_ARG, "the capacity must be a multiple of %d", KV4_KEYS);
+  if (c->capacity > MOST_KEYS) return fail(DLLM_UNSUPPORTED, "the capacity must be at most %d", MOST_KEYS);
   if (c->n_kv_heads > 65535 || (long)c->B * c->n_kv_heads > 65535)
     return fail(DLLM_UNSUPPORTED, "at most 65535 (sequence, KV head) pairs");
   if (!aligned16(c->d_k_codes) || !aligned16(c->d_k_params) || !aligned16(c->d_v_codes) || !aligned16(c->d_v_params))
@@ -81,6 +84,7 @@ extern "C" {
 dllm_status dllm_quantize_rows_s8(const void* d_x, size_t ldx, int dtype, void* d_q, size_t ldq, float* d_scale, int rows,
                                   int cols, void* stream) {
   if (!d_q || !d_scale || rows <= 0 || cols <= 0) return fail(DLLM_INVALID_ARG, "bad arguments of a row quantisation");
+  if (rows > MOST_ROWS || cols > MOST_COLS) return fail(DLLM_UNSUPPORTED, "at most %d rows and columns", MOST_ROWS);
   TRY(check_rows(d_x, ldx, dtype, cols));
   if (ldq % 16 || ldq < (size_t)cols || !aligned16(d_q))
     return fail(DLLM_INVALID_ARG, "rows of q must be 16-byte aligned and at least `cols` bytes apart");
@@ -88,7 +92,7 @@ dllm_status dllm_quantize_rows_s8(const void* d_x, size_t ldx, int dtype, void* 
 }
 
 size_t dllm_gemm_s8_scratch_bytes(int M, int N, int K) {
-  if (M <= 0 || N <= 0 || K <= 0 || K > MOST_K || N > MOST_N) return 0;
+  if (M <= 0 || N <= 0 || K <= 0 || K > MOST_K || N > MOST_N || M > MOST_ROWS) return 0;
   return gemm_s8_scratch_bytes(M, N, plan_gemm_s8(M, N, K));
 }
 
@@ -109,7 +113,7 @@ dllm_status dllm_gemm_s8(const void* d_A, size_t lda, const float* d_sa, const v
 }
 
 size_t dllm_linear_s8_scratch_bytes(int M, int N, int K) {
-  if (M <= 0 || N <= 0 || K <= 0 || K > MOST_K || N > MOST_N) return 0;
+  if (M <= 0 || N <= 0 || K <= 0 || K > MOST_K || N > MOST_N || M > MOST_ROWS) return 0;
   const size_t ldq = ((size_t)K + 15) & ~(size_t)15;
   return up256((size_t)M * ldq) + up256((size_t)M * 4) + gemm_s8_scratch_bytes(M, N, plan_gemm_s8(M, N, K));
 }
@@ -216,14 +220,14 @@ dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, in
     return fail(DLLM_INVALID_ARG, "eviction: n within the capacity, 0 <= first + last <= keep <= the new capacity");
   const size_t sr = (size_t)s.B * s.Hkv * s.cap, dr = (size_t)d.B * d.Hkv * d.cap;
   struct Span { const char *p; size_t n; };
-  const Span in[5] = {{(const char*)s.k, sr * s.hd / 2}, {(const char*)s.v, sr * s.hd / 2}, {(const char*)s.kp, sr * 4},
-                      {(const char*)s.vp, sr * 4}, {(const char*)d_weight, sr * 4}};
+  const Span in[6] = {{(const char*)s.k, sr * s.hd / 2}, {(const char*)s.v, sr * s.hd / 2}, {(const char*)s.kp, sr * 4},
+                      {(const char*)s.vp, sr * 4}, {(const char*)d_weight, sr * 4}, {(const char*)d_lens, d_lens ? (size_t)s.B * 4 : 0}};
   const Span out[7] = {{(const char*)d.k, dr * d.hd / 2}, {(const char*)d.v, dr * d.hd / 2}, {(const char*)d.kp, dr * 4},
                        {(const char*)d.vp, dr * 4}, {(const char*)d_to_weight, dr * 4},
                        {(const char*)d_index, (size_t)d.B * d.Hkv * keep * 4}, {(const char*)d_to_lens, (size_t)d.B * 4}};
   for (const Span& x : in)
     for (const Span& y : out)
-      if (x.p < y.p + y.n && y.p < x.p + x.n) return fail(DLLM_INVALID_ARG, "eviction: what is written overlaps what is read");
+      if (x.n && x.p < y.p + y.n && y.p < x.p + x.n) return fail(DLLM_INVALID_ARG, "eviction: what is written overlaps what is read");
   return done(launch_kv4_evict(on(stream), s, d_weight, n, keep, first, last, d_lens, d, d_to_weight, d_index, d_to_lens),
               "eviction");
 }

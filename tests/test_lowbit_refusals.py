@@ -47,6 +47,9 @@ def test_gemm(dllm):
         refused(dllm, "dllm_gemm_s8", a["A"], a["lda"], a["sa"], a["W"], a["ldw"], a["sw"], a["C"], a["dt"], a["M"], a["N"], a["K"],
                 a["s"], a["sb"], None)
     refused(dllm, "dllm_gemm_s8", P, 131072, P, P, 131072, P, P, 0, 3, 256, 131072, P, 1 << 40, None, status=dllm.UNSUPPORTED)
+    refused(dllm, "dllm_gemm_s8", P, 16, P, P, 16, P, P, 0, (1 << 30) + 1, 1, 16, P, 1 << 40, None, status=dllm.UNSUPPORTED)
+    refused(dllm, "dllm_quantize_rows_s8", P, 1 << 31, 1, P, 1 << 31, P, 1, (1 << 30) + 1, None, status=dllm.UNSUPPORTED)
+    assert dllm.lib.dllm_gemm_s8_scratch_bytes((1 << 30) + 1, 1, 16) == 0
 
 
 def test_linear(dllm):
@@ -62,7 +65,8 @@ def test_linear(dllm):
 def test_caches(dllm):
     for over, status in ((dict(k_codes=None), None), (dict(v_params=None), None), (dict(B=0), None), (dict(n_kv_heads=0), None),
                          (dict(capacity=100), None), (dict(capacity=0), None), (dict(head_dim=96), dllm.UNSUPPORTED),
-                         (dict(k_codes=P + 8), None), (dict(B=70000), dllm.UNSUPPORTED)):
+                         (dict(k_codes=P + 8), None), (dict(B=70000), dllm.UNSUPPORTED),
+                         (dict(capacity=(1 << 24) + 64), dllm.UNSUPPORTED)):
         refused(dllm, "dllm_kv4_load", cache(dllm, **over), 10, None, P, P, 0, None, status=status)
     refused(dllm, "dllm_kv4_load", None, 10, None, P, P, 0, None)
 
@@ -105,13 +109,14 @@ def test_attention_and_weights(dllm):
 def test_evict(dllm):
     src, far = cache(dllm, cap=256), P + (1 << 30)
     dst = cache(dllm, cap=64, at=far)
-    good = dict(src=src, w=P + (1 << 28), n=200, keep=50, first=3, last=5, dst=dst, dw=far + (1 << 28), idx=far + (1 << 29), nl=far + (3 << 28))
+    good = dict(src=src, w=P + (1 << 28), n=200, keep=50, first=3, last=5, lens=None, dst=dst, dw=far + (1 << 28), idx=far + (1 << 29), nl=far + (3 << 28))
     for bad in (dict(src=None), dict(dst=None), dict(w=None), dict(dw=None), dict(idx=None), dict(nl=None), dict(n=0), dict(n=257),
                 dict(keep=0), dict(keep=65), dict(first=-1), dict(last=-1), dict(first=30, last=21), dict(w=P + (1 << 28) + 4),
                 dict(dst=cache(dllm, cap=64, at=far, hd=64)), dict(dst=cache(dllm, cap=64, at=far, Hkv=2)),
+                dict(lens=far + (3 << 28)), dict(lens=far + (3 << 28) - 4),
                 dict(dst=cache(dllm, cap=64, at=P)), dict(dst=src), dict(dw=P + (1 << 28)), dict(idx=P), dict(nl=P + 64)):
         a = {**good, **bad}
-        refused(dllm, "dllm_kv4_evict", a["src"], a["w"], a["n"], a["keep"], a["first"], a["last"], None, a["dst"], a["dw"], a["idx"],
+        refused(dllm, "dllm_kv4_evict", a["src"], a["w"], a["n"], a["keep"], a["first"], a["last"], a["lens"], a["dst"], a["dw"], a["idx"],
                 a["nl"], None)
 
 
