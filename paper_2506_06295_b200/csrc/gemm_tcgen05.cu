@@ -545,6 +545,17 @@ bool make_tensor_map_s8(const void* base, uint64_t rows, uint64_t cols, uint64_t
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_tensor_map_heads(const void* base, uint64_t B, uint64_t a, uint64_t Hkv, uint64_t G, uint64_t hd, uint64_t ld,
+                           uint32_t box_g, uint32_t box_a, CUtensorMap* out) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[5] = {hd, G, Hkv, a, B}, strides[4] = {hd * 2, G * hd * 2, ld * 2, a * ld * 2};
+  cuuint32_t box[5] = {64, box_g, 1, box_a, 1}, estr[5] = {1, 1, 1, 1, 1};
+  return enc(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int sm_count() {
   static std::atomic<int> per_device[64];  // zero-initialised: not yet asked
   int dev = 0, v = 0;

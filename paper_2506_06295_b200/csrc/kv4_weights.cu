@@ -1,19 +1,25 @@
 // What every key of the 4-bit cache gets of many rows' attention, on the 5th-generation tensor cores (tcgen05).
 //
-// kv4_weights_umma_kernel: two tiles of 128 keys of one KV head x all rows ((query, head of the group) pairs), or a share of
-// them per CTA of a cluster; thirteen warps with fixed roles:
-//   warps 0-3, 4-7  a thread per key of tile 0 resp. 1: turns its key's codes into an operand row once, then adds up
-//                   2^(s - lse) over the rows, which are the columns of its lane of the accumulator
-//   warp 8          issues the tcgen05.mma: S^T = K Q^T for 128 rows at a time, into one of two accumulators per key tile
-//   warps 9-12      bring the rows in, as they are, and their sums and lse in parts (which kv4_row_parts_kernel has left: made
-//                   here, by every CTA again, they took 4500 cycles per 128 rows instead of the exponentials' 2048)
+// kv4_weights_umma_kernel: one CTA per multiprocessor that walks through units, two tiles of 128 keys of one KV head x all of its
+// rows ((query, head of the group) pairs); where the units are few, the CTAs of a cluster share a unit's rows.  Eighteen warps
+// with fixed roles:
+//   warps 0-7, 8-15  two threads per key of tile 0 resp. 1: turn the codes of the unit's keys into operand rows (while the rows
+//                    of the unit before are on), then each adds up 2^(s - lse) over its half of the rows, which are the columns
+//                    of its lane of the accumulator
+//   warp 16          issues the tcgen05.mma: S^T = K Q^T for 128 rows at a time, into one of two accumulators per key tile
+//   warp 17          requests the rows, as they are, by TMA (a tile is a box of the queries' tensor, see WkTiling), and their
+//                    sums and lse in parts (which kv4_row_parts_kernel has left: made here, by every CTA again, they took 4500
+//                    cycles per 128 rows instead of the exponentials' 2048)
 // With the keys along the lanes a key's numbers are its thread's registers, and what remains is made part of the product.  With
 // step = m 2^e (1 <= m < 2), v = code - 8, off = lo + 8 step and c = m log2(e) / sqrt(hd)
 //     (s - lse) log2(e) = c * ( q . (v 2^e) + (off / m) sum(q) + (1 / c) (-lse log2(e)) )
 // v 2^e is exact in bf16, so are the rows; the other two products are taken over sixteen more elements, both factors in three
 // bf16 parts (24 bits), the six larger partial products of each.  The thread multiplies by c: a multiplication, an exponential
 // and an addition per score, and the special-function unit's four results per scheduler and cycle are what it takes.
-// Every key is added to by one thread, the rows in their order, the shares of a cluster in theirs.
+// Every key's sum is taken by its two threads, the rows in their order, the shares of a cluster in theirs, and added once.
+// 4 sequences of 192 rows, 28 heads on 4, up to 16384 keys: 112 us, 78 of them exponentials at the special-function units' rate
+// (124 with a CTA per 256 keys, whose start and end took 7 us of each; 130 with rows brought in by cp.async, one tile on its way
+// at a time).  16 sequences of 512 rows x 1536 keys, 32 heads: 256 -> 205, of which 15 are the rows' parts.
 #include <algorithm>
 
 #include "kv4.cuh"
@@ -24,8 +30,8 @@ namespace dllm {
 
 namespace {
 
-constexpr int WK_TILE = 128, WK_KEYS = 2 * WK_TILE, WK_ROWS = 128, WK_STAGES = 2, WK_THREADS = 21 * 32, WK_MMA_WARP = 16,
-              WK_Q_WARP = 17, WK_CLUSTER = 8, WK_LENS = 1024;
+constexpr int WK_TILE = 128, WK_KEYS = 2 * WK_TILE, WK_ROWS = 128, WK_STAGES = 2, WK_THREADS = 18 * 32, WK_MMA_WARP = 16,
+              WK_Q_WARP = 17, WK_CLUSTER = 8;
 
 __device__ __forceinline__ float exp2_sfu(float x) {
   float y;
@@ -56,21 +62,41 @@ __device__ __forceinline__ void put_rows32(uint32_t base, int row, uint4 lo, uin
   put16(base + row * 32 + (16u ^ turn), hi);
 }
 
-// A row's sum and its lse in parts, 32 bytes per row: [B, Hkv, rows up to a multiple of 128].  Rows past the last one and rows
-// that saw no key: so large an lse that nothing is left.  HD / 8 threads per row.
+// The rows of a KV head in tiles of 128: heads of `queries` queries, gbox of the G heads each, so that a tile is a box of the
+// queries' tensor; what is left of the 128 holds nothing.  tiles: those of one KV head, `pieces` for the same queries.
+struct WkTiling {
+  int pieces, gbox, queries, tiles;
+};
+WkTiling wk_tiling(int a, int G) {
+  WkTiling best{0, 0, 0, 0};
+  const int least = (G + WK_ROWS - 1) / WK_ROWS;
+  for (int k = least; k < least + 8 && k <= G; ++k) {
+    WkTiling t;
+    t.gbox = (G + k - 1) / k;
+    t.pieces = (G + t.gbox - 1) / t.gbox;
+    t.queries = WK_ROWS / t.gbox;
+    t.tiles = (a + t.queries - 1) / t.queries * t.pieces;
+    if (best.tiles == 0 || t.tiles < best.tiles) best = t;
+  }
+  return best;
+}
+
+// A row's sum and its lse in parts, 32 bytes per row as they lie in shared memory: [B, Hkv, tiles, 128].  Rows that are none and
+// rows that saw no key: so large an lse that nothing is left.  HD / 8 threads per row.
 template <int HD>
 __global__ void __launch_bounds__(256) kv4_row_parts_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq,
                                                             const float* __restrict__ lse, uint4* __restrict__ parts, int B, int a,
-                                                            int H, int Hkv, int padded) {
+                                                            int H, int Hkv, WkTiling til) {
   constexpr int CHUNKS = HD / 8;
   pdl_wait();
   pdl_trigger();
   const int G = H / Hkv;
   const size_t unit = (size_t)blockIdx.x * 256 + threadIdx.x, record = unit / CHUNKS;
-  const int ch = (int)(unit % CHUNKS), vr = (int)(record % padded);
-  const size_t head = record / padded;
-  const int kh = (int)(head % Hkv), b = (int)(head / Hkv), i = vr / G, g = vr - i * G;
-  const bool live = b < B && vr < a * G;
+  const int ch = (int)(unit % CHUNKS), r = (int)(record % WK_ROWS);
+  const size_t tile = record / WK_ROWS, head = tile / til.tiles;
+  const int t = (int)(tile % til.tiles), kh = (int)(head % Hkv), b = (int)(head / Hkv);
+  const int i = t / til.pieces * til.queries + r / til.gbox, g = t % til.pieces * til.gbox + r % til.gbox;
+  const bool live = b < B && r < til.queries * til.gbox && i < a && g < G;
   float sum = 0.f;
   if (live) {
     const uint4 x = *reinterpret_cast<const uint4*>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + g) * HD + ch * 8);
@@ -87,13 +113,9 @@ __global__ void __launch_bounds__(256) kv4_row_parts_kernel(const __nv_bfloat16*
   float s[3], l[3];
   parts3(sum, s);
   parts3(-1.4426950408889634f * x, l);
-  parts[2 * record] = make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[0]), bf16_pair(s[1], s[0]), bf16_pair(l[0], l[1]));
-  parts[2 * record + 1] = make_uint4(bf16_pair(l[2], l[0]), bf16_pair(l[1], l[0]), 0u, 0u);
-}
-
-// 16 bytes to shared memory; live == false: zeros
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+  const size_t turn = (r >> 2) & 1;   // the 32-byte swizzle
+  parts[2 * record + turn] = make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[0]), bf16_pair(s[1], s[0]), bf16_pair(l[0], l[1]));
+  parts[2 * record + (turn ^ 1)] = make_uint4(bf16_pair(l[2], l[0]), bf16_pair(l[1], l[0]), 0u, 0u);
 }
 
 // A barrier of T threads that says whether all of them came with `x`
@@ -117,31 +139,27 @@ struct WkSmem {
 
 template <int HD>
 __global__ void __launch_bounds__(WK_THREADS, 1)
-    kv4_weights_umma_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c, const uint4* __restrict__ parts,
-                            const int32_t* __restrict__ lens, float* __restrict__ weight, int a, int n, int H, int shares,
+    kv4_weights_umma_kernel(const __grid_constant__ CUtensorMap tmQ, Kv4 c, const uint4* __restrict__ parts,
+                            const int32_t* __restrict__ lens, float* __restrict__ weight, int a, int n, WkTiling til, int shares,
                             float scale_log2, int* __restrict__ status) {
   using SM = WkSmem<HD>;
-  constexpr int CHUNKS = HD / 8;                 // 16-byte chunks of a row
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t k_full[2], q_full[WK_STAGES], q_empty[WK_STAGES], d_full[2][2], d_empty[2][2];
   __shared__ __align__(16) float total[2][WK_KEYS];
-  __shared__ int s_lens[WK_LENS];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * SM::KEYS;
   volatile int* abortp = &abort_flag;
-  const int G = H / c.Hkv, rows = a * G, heads = c.B * c.Hkv;
-  const int rank = shares > 1 ? (int)cluster_ctarank() : 0;
-  const int tiles_all = (rows + WK_ROWS - 1) / WK_ROWS, per_share = (tiles_all + shares - 1) / shares;
-  const int tile_lo = min(rank * per_share, tiles_all), n_tiles = min(tile_lo + per_share, tiles_all) - tile_lo;
+  const int rank = shares > 1 ? (int)cluster_ctarank() : 0, per_share = (til.tiles + shares - 1) / shares;
+  const int tile_lo = min(rank * per_share, til.tiles), n_tiles = min(tile_lo + per_share, til.tiles) - tile_lo;
 
   if (tid == 0) {
     abort_flag = 0;
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&k_full[i]), WK_MMA_WARP);   // one arrival per warp of the keys' threads
     for (int i = 0; i < WK_STAGES; ++i) {
-      mbar_init(smem_u32(&q_full[i]), 4);
+      mbar_init(smem_u32(&q_full[i]), 1);
       mbar_init(smem_u32(&q_empty[i]), 1);
     }
     for (int i = 0; i < 4; ++i) {
@@ -150,8 +168,13 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
     }
     mbar_fence_init();
   }
-  if (lens)
-    for (int i = tid; i < min(c.B, WK_LENS); i += WK_THREADS) s_lens[i] = lens[i];
+  // the rows of a stage that no box reaches: zeros
+  const int used = til.queries * til.gbox;
+  for (int i = tid; i < WK_STAGES * (HD / 64) * (WK_ROWS - used) * 8; i += WK_THREADS) {
+    const int ch = i & 7, r = (i >> 3) % (WK_ROWS - used), part = (i >> 3) / (WK_ROWS - used);
+    put16(ring + (part / (HD / 64)) * SM::STAGE + (part % (HD / 64)) * (WK_ROWS * 128) + (used + r) * 128 + ch * 16, make_uint4(0, 0, 0, 0));
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   if (warp == WK_MMA_WARP) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u)
                  : "memory");
@@ -164,79 +187,67 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
   pdl_trigger();
   bool ok = true;
 
-  // The CTA's units, each 256 keys of a head: the earlier keys of all heads first, so that what sequences of their own lengths
-  // leave out lies together.  Every role walks through them alike.
-  const int stride = (int)gridDim.x / shares;
+  // The CTA's units, each 256 keys of a head, those of a sequence block by block; every role walks through them alike (a warp
+  // together).  len == 0: none is left.
   struct Unit {
     int block, b, kh, len;
   };
-  auto unit_from = [&](int w) {   // unit w or the next one of the CTA's that has keys; len == 0: none
-    for (;; w += stride) {
-      Unit u;
-      u.block = w / heads;
-      const int head = w - u.block * heads;
-      u.b = head / c.Hkv;
-      u.kh = head - u.b * c.Hkv;
-      u.len = 0;
-      if (u.block * WK_KEYS >= n) return u;
-      const int len = lens ? min(u.b < WK_LENS ? s_lens[u.b] : lens[u.b], n) : n;
-      if (u.block * WK_KEYS < len) {
-        u.len = len;
-        return u;
+  int walk = (int)blockIdx.x / shares, before = 0, group = 0;   // unit; those of the sequences ahead of this group of 32
+  auto next_unit = [&]() {
+    Unit u{0, 0, 0, 0};
+    for (; group < c.B; group += 32) {
+      const int b = group + lane, len = b >= c.B ? 0 : lens ? min(max(lens[b], 0), n) : n;
+      const int units = (len + WK_KEYS - 1) / WK_KEYS * c.Hkv;
+      int upto = units;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += t;
       }
+      const uint32_t hit = __ballot_sync(0xffffffffu, walk < before + upto);
+      if (hit) {
+        const int l = __ffs(hit) - 1, into = walk - before - __shfl_sync(0xffffffffu, upto - units, l);
+        u.b = group + l;
+        u.len = __shfl_sync(0xffffffffu, len, l);
+        u.block = into / c.Hkv;
+        u.kh = into - u.block * c.Hkv;
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, upto, 31);
     }
+    walk += (int)gridDim.x / shares;
+    return u;
   };
-  auto after = [&](const Unit& u) { return unit_from(u.block * heads + u.b * c.Hkv + u.kh + stride); };
-  const Unit first = unit_from((int)blockIdx.x / shares);
+  const Unit first = next_unit();
 
   if (warp >= WK_Q_WARP) {
-    // ---------------- the rows: 16 (heads of 64: 8) threads per row ----------------
-    constexpr int SIDE = 128 / CHUNKS;
-    const int t = tid - WK_Q_WARP * 32, ch = t % CHUNKS, r0 = t / CHUNKS;
-    const int di = SIDE / G, dg = SIDE - di * G;   // SIDE rows further on
+    // ---------------- the rows ----------------
     pdl_wait();   // for the rows' parts; what the others read was there before the launch that makes them
-    auto landed = [&](int it) {
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&q_full[it % WK_STAGES]));
-    };
     int it = 0;
-    for (Unit w = first; w.len > 0 && ok; w = after(w)) {
-      int qi = (tile_lo * WK_ROWS + r0) / G, g = tile_lo * WK_ROWS + r0 - qi * G;
-      const __nv_bfloat16* const qb = q + (size_t)w.b * a * ldq + (size_t)w.kh * G * HD + ch * 8;
-      const uint4* const pb = parts + 2 * (((size_t)w.b * c.Hkv + w.kh) * tiles_all + tile_lo) * WK_ROWS;
+    for (Unit w = first; w.len > 0 && ok; w = next_unit()) {
+      const uint4* const pb = parts + 2 * (((size_t)w.b * c.Hkv + w.kh) * til.tiles + tile_lo) * WK_ROWS;
       for (int u = 0; u < n_tiles; ++u, ++it) {
-        if (it > 0) landed(it - 1);
-        const int st = it % WK_STAGES;
+        const int st = it % WK_STAGES, t = tile_lo + u;
         if (it >= WK_STAGES && !mbar_wait_warp(smem_u32(&q_empty[st]), (uint32_t)(it / WK_STAGES - 1) & 1u, abortp)) {
           ok = false;
           break;
         }
-        const uint32_t to = ring + st * SM::STAGE;
+        if (elect_one()) {
+          const uint32_t to = ring + st * SM::STAGE, bar = smem_u32(&q_full[st]);
+          mbar_expect_tx(bar, (uint32_t)used * HD * 2 + SM::MORE);
 #pragma unroll
-        for (int p = 0; p < WK_ROWS / SIDE; ++p) {
-          const int r = p * SIDE + r0;
-          copy16(to + (ch >> 3) * (WK_ROWS * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4), qi < a ? qb + (size_t)qi * ldq + g * HD : qb, qi < a);
-          qi += di;
-          g += dg;
-          if (g >= G) {
-            g -= G;
-            ++qi;
-          }
+          for (int h = 0; h < HD / 64; ++h)
+            tma_load_5d(to + h * (WK_ROWS * 128), &tmQ, bar, h * 64, t % til.pieces * til.gbox, w.kh, t / til.pieces * til.queries, w.b);
+          bulk_load_1d(to + SM::OPERAND, pb + 2 * (size_t)u * WK_ROWS, SM::MORE, bar);
         }
-        const uint32_t turn = (uint32_t)((t >> 2) & 1) << 4;
-        copy16(to + SM::OPERAND + t * 32 + turn, pb + 2 * ((size_t)u * WK_ROWS + t), true);
-        copy16(to + SM::OPERAND + t * 32 + (16u ^ turn), pb + 2 * ((size_t)u * WK_ROWS + t) + 1, true);
+        __syncwarp();
       }
     }
-    if (it > 0 && ok) landed(it - 1);
-    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == WK_MMA_WARP) {
     // ---------------- MMA issuer ----------------
     constexpr uint32_t idesc = make_idesc(WK_TILE, WK_ROWS);
     int it = 0, j = 0;
-    for (Unit w = first; w.len > 0 && ok; w = after(w), ++j) {
+    for (Unit w = first; w.len > 0 && ok; w = next_unit(), ++j) {
       ok = mbar_wait_warp(smem_u32(&k_full[j & 1]), (uint32_t)(j >> 1) & 1u, abortp);
       for (int u = 0; u < n_tiles && ok; ++u, ++it) {
         const int st = it % WK_STAGES, buf = it & 1;
@@ -325,7 +336,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
     }
     int it = 0, j = 0;
     for (Unit w = first, next; w.len > 0; w = next, mul = next_mul, ++j) {
-      next = after(w);
+      next = next_unit();
       if (next.len > 0) fetch(next);   // on its way during this unit's first rows
       const bool mine_to_add = shares == 1 && half == 0 && w.block * WK_KEYS + mine < w.len;
       const float had = mine_to_add ? weight[key_of(w)] : 0.f;
@@ -336,7 +347,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = d_lane + (uint32_t)(buf * WK_ROWS);
-        const int left = rows - (tile_lo + u) * WK_ROWS - half * (WK_ROWS / 2);   // rows of this thread's columns
+        const int t = tile_lo + u, left = min(til.queries, a - t / til.pieces * til.queries) * til.gbox - half * (WK_ROWS / 2);   // rows
 #pragma unroll
         for (int p = 0; p < WK_ROWS / 2; p += 32) {
           if (p >= left) break;
@@ -399,24 +410,27 @@ cudaError_t weights_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, cons
   cudaError_t e = once.run(
       [] { return cudaFuncSetAttribute(kv4_weights_umma_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); });
   if (e != cudaSuccess) return e;
-  // fewer CTAs than multiprocessors: the rows in shares, a power of two of them
-  const long blocks = (n + WK_KEYS - 1) / WK_KEYS, ctas = blocks * c.Hkv * c.B;
-  const int tiles = (int)(((long)a * (H / c.Hkv) + WK_ROWS - 1) / WK_ROWS);
+  const int G = H / c.Hkv;
+  const WkTiling til = wk_tiling(a, G);
+  CUtensorMap tmQ;
+  if (!make_tensor_map_heads(q, c.B, a, c.Hkv, G, HD, ldq, til.gbox, til.queries, &tmQ)) return cudaErrorInvalidValue;
+  // fewer units than multiprocessors: a unit's rows in shares, a power of two of them; otherwise each CTA walks through several
+  const long units = (long)((n + WK_KEYS - 1) / WK_KEYS) * c.Hkv * c.B;
   int shares = 1;
-  while (2 * shares <= WK_CLUSTER && 2 * shares <= tiles && ctas * 2 * shares <= sm_count()) shares *= 2;
-  const dim3 grid((unsigned)(shares > 1 ? ctas * shares : std::min<long>(ctas, sm_count())));
+  while (2 * shares <= WK_CLUSTER && 2 * shares <= til.tiles && units * 2 * shares <= sm_count()) shares *= 2;
+  const dim3 grid((unsigned)(shares > 1 ? units * shares : std::min<long>(units, sm_count())));
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
-  const size_t threads = (size_t)c.B * c.Hkv * tiles * WK_ROWS * (HD / 8);
+  const size_t threads = (size_t)c.B * c.Hkv * til.tiles * WK_ROWS * (HD / 8);
   e = launch_k(L, kv4_row_parts_kernel<HD>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, q, ldq, lse, parts, c.B, a, H,
-               c.Hkv, tiles * WK_ROWS);
+               c.Hkv, til);
   L.count();
   if (e != cudaSuccess) return e;
   Launch behind = L;
   behind.pdl = true;
-  e = shares == 1 ? launch_k(behind, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, q, ldq, c,
-                             (const uint4*)parts, lens, weight, a, n, H, shares, scale_log2, L.d_status)
-                  : launch_k_cluster(behind, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, dim3(shares, 1, 1), q, ldq, c,
-                                     (const uint4*)parts, lens, weight, a, n, H, shares, scale_log2, L.d_status);
+  e = shares == 1 ? launch_k(behind, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, tmQ, c, (const uint4*)parts, lens,
+                             weight, a, n, til, shares, scale_log2, L.d_status)
+                  : launch_k_cluster(behind, kv4_weights_umma_kernel<HD>, grid, dim3(WK_THREADS), SMEM, dim3(shares, 1, 1), tmQ, c,
+                                     (const uint4*)parts, lens, weight, a, n, til, shares, scale_log2, L.d_status);
   L.count();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -424,7 +438,7 @@ cudaError_t weights_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, cons
 }  // namespace
 
 size_t kv4_weights_umma_scratch_bytes(int B, int a, int H, int Hkv) {
-  return (size_t)B * Hkv * (((size_t)a * (H / Hkv) + WK_ROWS - 1) / WK_ROWS) * WK_ROWS * 32;
+  return (size_t)B * Hkv * wk_tiling(a, H / Hkv).tiles * WK_ROWS * 32;
 }
 
 cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,

@@ -190,6 +190,13 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
       : "memory");
 }
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3,
+                                            int c4) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
 
 // Host: bf16 tensor maps with a 64-element (128-byte) inner box and 128-byte
 // swizzle, cached by (base, shape, box).  2-D: [rows, cols] row-major, box
@@ -201,5 +208,9 @@ bool get_tensor_map_3d(const void* base, uint64_t batch, uint64_t rows, uint64_t
 // 8-bit integers [rows, cols] whose rows start ld bytes apart (a multiple of 16), box box_rows x 128, the same swizzle;
 // encoded anew at every call.
 bool make_tensor_map_s8(const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows, CUtensorMap* out);
+// bf16 rows of heads, [B * a, Hkv * G * hd] with rows ld elements apart: 64 elements of box_g heads of one KV head of box_a rows
+// of one sequence, box_g * box_a rows of 128 bytes with the 128-byte swizzle; not cached.
+bool make_tensor_map_heads(const void* base, uint64_t B, uint64_t a, uint64_t Hkv, uint64_t G, uint64_t hd, uint64_t ld,
+                           uint32_t box_g, uint32_t box_a, CUtensorMap* out);
 
 }  // namespace dllm

@@ -135,6 +135,9 @@ SHAPES = [  # B, a, n, H, Hkv, hd, lens
     (1, 200, 300, 7, 1, 128, [257]),
     (2, 300, 450, 4, 2, 128, [450, 33]),
     (1, 2, 20000, 8, 1, 128, None),
+    (2, 5, 700, 71, 1, 64, [700, 300]),
+    (1, 2, 300, 260, 1, 128, None),
+    (40, 80, 520, 2, 2, 64, [13 * b for b in range(40)]),
 ]
 
 
