@@ -721,12 +721,14 @@ class KV4Cache:
         return self
 
     def _new_like(self, capacity: int) -> "KV4Cache":
-        """A cache of the same sequences, heads and head size whose rows hold nothing yet."""
+        """A cache of the same sequences, heads and head size whose rows hold nothing yet: one allocation, of which the four
+        tensors are made when they are asked for."""
         B, Hkv, cap, half = self.B, self.Hkv, -(-capacity // 64) * 64, self.hd // 2
-        codes, pairs = self.k_codes.new_empty, self.k_params.new_empty
+        rows = B * Hkv * cap
+        store = self._base.new_empty((rows * (2 * half + 8),))
+        k, v, pairs = store.data_ptr(), store.data_ptr() + rows * half, store.data_ptr() + 2 * rows * half
         new = KV4Cache.__new__(KV4Cache)
-        new._hold(codes((B, Hkv, cap, half)), pairs((B, Hkv, cap, 2)), codes((B, Hkv, cap, half)), pairs((B, Hkv, cap, 2)),
-                  B, Hkv, cap, half)
+        new._hold(store, None, k, pairs, v, pairs + 4 * rows, B, Hkv, cap, half)
         return new
 
     def _bind(self, k_codes, k_params, v_codes, v_params) -> None:
@@ -740,17 +742,31 @@ class KV4Cache:
         _like(v_params, torch.bfloat16, (B, Hkv, cap, 2), "v_params")
         if not k_codes.device == k_params.device == v_codes.device == v_params.device:
             _refuse("a cache's tensors must be on one device")
-        self._hold(k_codes, k_params, v_codes, v_params, B, Hkv, cap, half)
+        self._hold(k_codes, (k_codes, k_params, v_codes, v_params), k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(),
+                   v_params.data_ptr(), B, Hkv, cap, half)
 
-    def _hold(self, k_codes, k_params, v_codes, v_params, B, Hkv, cap, half) -> None:
-        self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
-        self.B, self.Hkv, self.capacity, self.hd, self.device = B, Hkv, cap, 2 * half, k_codes.device
-        self.c = Kv4CacheStruct(k_codes.data_ptr(), k_params.data_ptr(), v_codes.data_ptr(), v_params.data_ptr(),
-                                B, Hkv, cap, 2 * half)
+    def _hold(self, base, tensors, k_codes, k_params, v_codes, v_params, B, Hkv, cap, half) -> None:
+        self._base, self._tensors = base, tensors      # bytes on the cache's device
+        self.B, self.Hkv, self.capacity, self.hd = B, Hkv, cap, 2 * half
+        self.c = Kv4CacheStruct(k_codes, k_params, v_codes, v_params, B, Hkv, cap, 2 * half)
         self.ref = C.byref(self.c)
 
     def tensors(self):
-        return self.k_codes, self.k_params, self.v_codes, self.v_params
+        """(k_codes, k_params, v_codes, v_params)"""
+        if self._tensors is None:
+            import torch
+            shape, half = (self.B, self.Hkv, self.capacity), self.hd // 2
+            rows = self.B * self.Hkv * self.capacity
+            k, v, kp, vp = self._base.split([rows * half, rows * half, 4 * rows, 4 * rows])
+            self._tensors = (k.view(*shape, half), kp.view(torch.bfloat16).view(*shape, 2), v.view(*shape, half),
+                             vp.view(torch.bfloat16).view(*shape, 2))
+        return self._tensors
+
+    k_codes = property(lambda self: self.tensors()[0])
+    k_params = property(lambda self: self.tensors()[1])
+    v_codes = property(lambda self: self.tensors()[2])
+    v_params = property(lambda self: self.tensors()[3])
+    device = property(lambda self: self._base.device)
 
 
 def _lens(lens, cache):
@@ -765,7 +781,7 @@ def kv4_store(cache: KV4Cache, k, v, pos=None, start: int = 0, stream=None) -> N
     """Rows of K and V, [B, a, Hkv * hd] or [B * a, Hkv * hd] (float32 / bfloat16, evenly spaced rows), into the cache: row j
     of a sequence at pos[b, j] (int32 [B, a]; outside of the capacity: nowhere) or start + j."""
     import torch
-    if _elsewhere(cache.k_codes, stream):
+    if _elsewhere(cache._base, stream):
         with _Placed(stream, *cache.tensors(), k, v, pos):
             return kv4_store(cache, k, v, pos, start)
     width = cache.Hkv * cache.hd
@@ -777,23 +793,23 @@ def kv4_store(cache: KV4Cache, k, v, pos=None, start: int = 0, stream=None) -> N
         _like(pos, torch.int32, (cache.B, a), "pos")
     _check(lib.dllm_kv4_store(cache.ref, k.data_ptr(), _row_pitch(k, width, "k"), v.data_ptr(), _row_pitch(v, width, "v"),
                               _dtype(k), a, None if pos is None else pos.data_ptr(), start,
-                              _stream_of(cache.k_codes, k, v, pos)))
+                              _stream_of(cache._base, k, v, pos)))
 
 
 def kv4_load(cache: KV4Cache, n: int, lens=None, dtype=None, stream=None):
     """(K, V) of the first n rows of every sequence as numbers, [B, n, Hkv * hd] in float32 or bfloat16 (the layout
     attention() reads); zeros from lens[b] on."""
     import torch
-    if _elsewhere(cache.k_codes, stream):
+    if _elsewhere(cache._base, stream):
         with _Placed(stream, *cache.tensors(), lens):
             return kv4_load(cache, n, lens, dtype)
     if not 0 < n <= cache.capacity:
         _refuse("n must lie within the capacity")
     shape, dtype = (cache.B, n, cache.Hkv * cache.hd), torch.float32 if dtype is None else dtype
-    k = cache.k_codes.new_empty(shape, dtype=dtype)
+    k = cache._base.new_empty(shape, dtype=dtype)
     v = k.new_empty(shape)
     _check(lib.dllm_kv4_load(cache.ref, n, _lens(lens, cache), k.data_ptr(), v.data_ptr(), _dtype(k),
-                             _stream_of(cache.k_codes, lens)))
+                             _stream_of(cache._base, lens)))
     return k, v
 
 
@@ -816,7 +832,7 @@ def attention_kv4(q, cache: KV4Cache, a: int, n: int, H: int, lens=None, scratch
     lse = q.new_empty((rows, H), dtype=torch.float32)
     at, size, keep = _space(q, lib.dllm_attention_kv4_scratch_bytes(cache.B, a, n, H, cache.Hkv, cache.hd), scratch)
     _check(lib.dllm_attention_kv4(q.data_ptr(), ldq, cache.ref, o.data_ptr(), lse.data_ptr(), a, n, H, _lens(lens, cache),
-                                  at, size, _stream_of(q, cache.k_codes, lens, keep)))
+                                  at, size, _stream_of(q, cache._base, lens, keep)))
     return o, lse
 
 
@@ -834,7 +850,7 @@ def attention_weights_kv4(q, cache: KV4Cache, lse, weight, a: int, n: int, H: in
     at, size, keep = _space(q, lib.dllm_attention_weights_kv4_scratch_bytes(cache.B, a, H, cache.Hkv), scratch)
     _check(lib.dllm_attention_weights_kv4(q.data_ptr(), ldq, cache.ref, lse.data_ptr(), weight.data_ptr(), a, n, H,
                                           _lens(lens, cache), at, size,
-                                          _stream_of(q, cache.k_codes, lse, weight, lens, keep)))
+                                          _stream_of(q, cache._base, lse, weight, lens, keep)))
 
 
 def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: int = 0, lens=None, to=None, stream=None):
@@ -857,7 +873,7 @@ def kv4_evict(cache: KV4Cache, weight, n: int, keep: int, first: int = 0, last: 
     new_lens = index.new_empty((B,))
     _check(lib.dllm_kv4_evict(cache.ref, weight.data_ptr(), n, keep, first, last, _lens(lens, cache), to.ref,
                               new_weight.data_ptr(), index.data_ptr(), new_lens.data_ptr(),
-                              _stream_of(cache.k_codes, weight, lens, to.k_codes)))
+                              _stream_of(cache._base, weight, lens, to._base)))
     return to, new_weight, index, new_lens
 
 
