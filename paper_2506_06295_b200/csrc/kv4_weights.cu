@@ -184,7 +184,6 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
-  pdl_trigger();
   bool ok = true;
 
   // The CTA's units, each 256 keys of a head, those of a sequence block by block; every role walks through them alike (a warp
@@ -222,7 +221,9 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
 
   if (warp >= WK_Q_WARP) {
     // ---------------- the rows ----------------
-    pdl_wait();   // for the rows' parts; what the others read was there before the launch that makes them
+    // for the rows' parts; what the others read was there before the launch that makes them
+    pdl_wait();
+    pdl_trigger();
     int it = 0;
     for (Unit w = first; w.len > 0 && ok; w = next_unit()) {
       const uint4* const pb = parts + 2 * (((size_t)w.b * c.Hkv + w.kh) * til.tiles + tile_lo) * WK_ROWS;
