@@ -510,7 +510,7 @@ dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_k
 /* Keeps, per sequence and KV head, min(length, keep) keys: the first `first` and the
  * last `last` of them (response rows, say) and, of the others, those with the largest
  * weights (equal ones: the lowest index; a NaN counts as lowest), in their order; where
- * the length is at most keep all stay.  Their K, V and weight go to rows 0, 1, .. of
+ * the length is at most keep all stay.  Their K, V and weight (-0 as 0) go to rows 0, 1, .. of
  * `to` and d_to_weight (float [B, n_kv_heads, to->capacity], zeros behind them),
  * d_index (int32 [B, n_kv_heads, keep]) says where each came from (-1 behind them) and
  * d_to_lens (int32 [B]) how many stayed.  first + last <= keep <= to->capacity; nothing

@@ -226,11 +226,12 @@ __global__ void __launch_bounds__(256) kv4_load_kernel(Kv4 c, int n, const int32
 constexpr int EV_THREADS = 512, EV_PER = 8, EV_BINS = 256, EV_CLUSTER = 8;
 constexpr int EV_SMEM_KEYS = 40 * 1024;   // ordered weights that one CTA keeps
 
-// Order of the weights as unsigned numbers; a NaN comes last, -0 and 0 are equal.
+// Order of the weights as unsigned numbers, and back; a NaN comes last (as 0), -0 is 0.  No weight has the largest number.
 __device__ __forceinline__ uint32_t weight_key(float w) {
   const uint32_t u = __float_as_uint(w + 0.f);
   return w != w ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t EV_STAYS = 0xFFFFFFFFu;   // the number of a key that stays whatever its weight
 
 __device__ __forceinline__ int block_scan(int v, int* warps, int& total) {   // exclusive; EV_THREADS threads
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -260,163 +261,34 @@ __device__ __forceinline__ int remote(const int* p, uint32_t rank) {
   return r;
 }
 
-// A cluster of one or eight CTAs per (sequence, KV head), each with its share of the keys (multiples of EV_PER, kept in
-// shared memory as ordered numbers where they fit).  The smallest weight that stays is found digit by digit (8 bits, a
-// histogram each; every CTA adds up all of the cluster's: with digits of 11 bits the 64 KB that a CTA reads from the others
-// took 7000 cycles a digit), then each thread counts its consecutive keys that stay, and writes them behind those before it.
-// What is left is the latency of a dozen barriers.  (8 x 4 heads of 65536 keys 37 us with 11-bit digits and a scan per 4096
-// keys, 26 so.)
+// A cluster of one or eight CTAs per (sequence, KV head), each with its share of the keys, kept in shared memory as ordered
+// numbers where they fit.  The smallest number that stays is found digit by digit (8 bits, a histogram of its own each, so that
+// one barrier of the cluster is enough; every CTA adds up all of the cluster's: with digits of 11 bits the 64 KB that a CTA reads
+// from the others took 7000 cycles a digit), until a digit's whole bin stays.  Then each warp counts what stays of a range of its
+// own, and writes it behind what stays ahead of it, 32 keys at a time.  What is left is the latency of barriers and of code that
+// runs once.  (8 x 4 heads of 65536 keys 37 us with 11-bit digits, 24 with keys compared to the forced ranges in every pass, 20
+// so.)
 __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __restrict__ weight, int n, int cap, int Hkv,
                                                                 int keep, int first, int last,
                                                                 const int32_t* __restrict__ lens, int share, int kept_in_smem,
                                                                 int dst_cap, float* __restrict__ dst_weight,
                                                                 int32_t* __restrict__ index, int32_t* __restrict__ new_lens) {
+  constexpr int WARPS = EV_THREADS / 32;
   extern __shared__ __align__(16) uint32_t keys[];
-  __shared__ __align__(16) int hist[EV_BINS];
-  __shared__ __align__(16) int counts[4];
+  __shared__ int hist[4][EV_BINS];
+  __shared__ int counts[2], of_warp[2][WARPS];
   __shared__ int warps[32];
-  __shared__ int found[2];
+  __shared__ int found[3];
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, rank = (int)cluster_ctarank();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rank = (int)cluster_ctarank();
   const bool alone = share >= cap;
   const int bh = alone ? blockIdx.x : blockIdx.x / EV_CLUSTER, b = bh / Hkv;
   const float* w = weight + (size_t)bh * cap;
-  const int len = lens ? min(max(lens[b], 0), n) : n, kept = min(len, keep);
-  const bool choose = len > keep;                       // else every key stays
-  const int lo = choose ? first : len, hi = choose ? len - last : len;   // keys lo .. hi - 1 compete
-  const int j_lo = min(rank * share, len), j_hi = min(j_lo + share, len);
-  int need = choose ? keep - first - last : 0;          // for this many places
-  uint32_t prefix = 0, mask = 0;                        // digits of the threshold found so far
-  auto sync_all = [&] {
-    if (alone) __syncthreads();
-    else cluster_sync();
-  };
-  auto four = [&](int j, uint32_t (&k)[4]) {            // the ordered weights of keys j .. j + 3 (j a multiple of 4)
-    if (kept_in_smem) {
-      const uint4 x = *reinterpret_cast<const uint4*>(keys + (j - j_lo));
-      k[0] = x.x; k[1] = x.y; k[2] = x.z; k[3] = x.w;
-    } else {
-      const float4 x = *reinterpret_cast<const float4*>(w + j);
-      k[0] = weight_key(x.x); k[1] = weight_key(x.y); k[2] = weight_key(x.z); k[3] = weight_key(x.w);
-    }
-  };
-  if (kept_in_smem && choose) {
-#pragma unroll 2
-    for (int j = j_lo + tid * 4; j < j_hi; j += EV_THREADS * 4) {
-      const float4 x = *reinterpret_cast<const float4*>(w + j);
-      *reinterpret_cast<uint4*>(keys + (j - j_lo)) =
-          make_uint4(weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w));
-    }
-  }
-  if (need > 0) {
-    for (int shift = 24;; shift -= 8) {
-      if (tid < EV_BINS) hist[tid] = 0;
-      __syncthreads();
-      for (int j = j_lo + tid * 4; j < j_hi; j += EV_THREADS * 4) {
-        uint32_t k[4];
-        four(j, k);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (j + q >= lo && j + q < hi && (k[q] & mask) == prefix) atomicAdd(&hist[(k[q] >> shift) & (EV_BINS - 1)], 1);
-      }
-      sync_all();
-      // the bin, counted from the largest, in which the last place goes: a bin per thread
-      const int at = EV_BINS - 1 - tid;
-      int here = 0;
-      if (tid < EV_BINS) {
-        if (alone) {
-          here = hist[at];
-        } else {
-          int x[EV_CLUSTER];
-#pragma unroll
-          for (int r = 0; r < EV_CLUSTER; ++r) x[r] = remote(&hist[at], r);
-#pragma unroll
-          for (int r = 0; r < EV_CLUSTER; ++r) here += x[r];
-        }
-      }
-      int total;
-      const int before = block_scan(here, warps, total);
-      if (before < need && need <= before + here) {
-        found[0] = at;
-        found[1] = need - before;
-      }
-      sync_all();   // and no CTA clears a histogram that another one still reads
-      prefix |= (uint32_t)found[0] << shift;
-      mask |= (uint32_t)(EV_BINS - 1) << shift;
-      need = found[1];
-      if (shift == 0) break;
-    }
-  }
-  __syncthreads();
-  // `need` of the keys equal to `prefix` stay, the first ones.  sure: stays whatever the ties do.
-  auto eight = [&](int j0, int end, uint32_t& sure, uint32_t& tie) {
-    sure = tie = 0;
-    uint32_t k[8];
-    if (choose) {
-      uint32_t (&k0)[4] = *reinterpret_cast<uint32_t(*)[4]>(&k[0]);
-      uint32_t (&k1)[4] = *reinterpret_cast<uint32_t(*)[4]>(&k[4]);
-      four(j0, k0);
-      four(j0 + 4, k1);
-    }
-#pragma unroll
-    for (int q = 0; q < EV_PER; ++q) {
-      const int j = j0 + q;
-      if (j >= end) continue;
-      const bool forced = j < lo || j >= hi;
-      if (forced || (mask && k[q] > prefix)) sure |= 1u << q;
-      else if (mask && k[q] == prefix) tie |= 1u << q;
-    }
-  };
-  // a thread's keys: consecutive ones, a multiple of EV_PER
-  const int mine = (j_hi - j_lo + EV_THREADS * EV_PER - 1) / (EV_THREADS * EV_PER) * EV_PER;
-  const int m_lo = min(j_lo + tid * mine, j_hi), m_hi = min(m_lo + mine, j_hi);
-  int sures = 0, ties = 0;
-  for (int j0 = m_lo; j0 < m_hi; j0 += EV_PER) {
-    uint32_t sure, tie;
-    eight(j0, m_hi, sure, tie);
-    sures += __popc(sure);
-    ties += __popc(tie);
-  }
-  int all_sures, all_ties;
-  int s = block_scan(sures, warps, all_sures), t = block_scan(ties, warps, all_ties);
-  if (!alone) {   // what the CTAs with earlier keys hold
-    if (tid == 0) {
-      counts[0] = all_sures;
-      counts[1] = all_ties;
-    }
-    cluster_sync();
-    int x[2][EV_CLUSTER];
-#pragma unroll
-    for (int r = 0; r < EV_CLUSTER; ++r)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) x[k][r] = r < rank ? remote(&counts[k], r) : 0;
-#pragma unroll
-    for (int r = 0; r < EV_CLUSTER; ++r) {
-      s += x[0][r];
-      t += x[1][r];
-    }
-    cluster_sync();   // no CTA leaves while another one reads its counts
-  }
   int32_t* idx = index + (size_t)bh * keep;
   float* dw = dst_weight + (size_t)bh * dst_cap;
-  for (int j0 = m_lo; j0 < m_hi; j0 += EV_PER) {
-    const float4 w0 = *reinterpret_cast<const float4*>(w + j0), w1 = *reinterpret_cast<const float4*>(w + j0 + 4);
-    const float e[EV_PER] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-    uint32_t sure, tie;
-    eight(j0, m_hi, sure, tie);
-#pragma unroll
-    for (int q = 0; q < EV_PER; ++q) {
-      const bool is_sure = (sure >> q) & 1u, is_tie = (tie >> q) & 1u;
-      if (is_sure || (is_tie && t < need)) {
-        const int slot = s + min(t, need);
-        idx[slot] = j0 + q;
-        dw[slot] = e[q];
-      }
-      s += is_sure;
-      t += is_tie;
-    }
-  }
+  const int len = lens ? min(max(lens[b], 0), n) : n, kept = min(len, keep);
+  const int j_lo = min(rank * share, len), j_hi = min(j_lo + share, len);
   if (rank == 0) {
     for (int i = kept + tid; i < dst_cap; i += EV_THREADS) {
       if (i < keep) idx[i] = -1;
@@ -424,6 +296,129 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __r
     }
     if (tid == 0 && bh % Hkv == 0) new_lens[b] = kept;
   }
+  if (len <= keep) {   // every key stays (the whole cluster)
+    for (int j = j_lo + tid; j < j_hi; j += EV_THREADS) {
+      idx[j] = j;
+      dw[j] = w[j];
+    }
+    return;
+  }
+  // Keys j .. j + 3 (j a multiple of 4) as numbers; those behind the length have the lowest one and lie behind all others.
+  auto read = [&](int j) {
+    const float4 x = *reinterpret_cast<const float4*>(w + j);
+    uint4 k = make_uint4(weight_key(x.x), weight_key(x.y), weight_key(x.z), weight_key(x.w));
+    if (j < first || j + 3 >= len - last) {
+      uint32_t* const e = &k.x;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (j + q < first || j + q >= len - last) e[q] = j + q < len ? EV_STAYS : 0u;
+    }
+    return k;
+  };
+  auto four = [&](int j) { return kept_in_smem ? *reinterpret_cast<const uint4*>(keys + (j - j_lo)) : read(j); };
+  for (int i = tid; i < 4 * EV_BINS; i += EV_THREADS) hist[0][i] = 0;
+  if (kept_in_smem) {
+#pragma unroll 4
+    for (int j = j_lo + tid * 4; j < j_hi; j += EV_THREADS * 4) *reinterpret_cast<uint4*>(keys + (j - j_lo)) = read(j);
+  }
+  __syncthreads();
+  uint32_t prefix = 0;   // the threshold's digits so far
+  int need = keep;       // of the keys that have them
+#pragma unroll 1
+  for (int d = 0; d < 4; ++d) {
+    const int shift = 24 - 8 * d;
+    const uint32_t mask = d == 0 ? 0u : 0xFFFFFFFFu << (shift + 8);
+    int* const h = hist[d];
+    for (int j = j_lo + tid * 4; j < j_hi; j += EV_THREADS * 4) {
+      const uint4 x = four(j);
+      const uint32_t k[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if ((k[q] & mask) == prefix) atomicAdd(&h[(k[q] >> shift) & (EV_BINS - 1)], 1);
+    }
+    if (alone) __syncthreads();
+    else cluster_sync();
+    // the bin, counted from the largest, in which the last place goes: a bin per thread
+    const int at = EV_BINS - 1 - tid;
+    int here = 0;
+    if (tid < EV_BINS) {
+      if (alone) {
+        here = h[at];
+      } else {
+        int x[EV_CLUSTER];
+#pragma unroll
+        for (int r = 0; r < EV_CLUSTER; ++r) x[r] = remote(&h[at], r);
+#pragma unroll
+        for (int r = 0; r < EV_CLUSTER; ++r) here += x[r];
+      }
+    }
+    int total;
+    const int before = block_scan(here, warps, total);
+    if (before < need && need <= before + here) {
+      found[0] = at;
+      found[1] = need - before;
+      found[2] = need == before + here;
+    }
+    __syncthreads();
+    prefix |= (uint32_t)found[0] << shift;
+    need = found[1];
+    if (found[2]) {   // the whole bin (its lowest number is not 0, or every key would stay)
+      prefix -= 1u;
+      need = 0;
+      break;
+    }
+  }
+  // What is larger than `prefix` stays, and the first `need` of those equal to it.
+  const int per = ((j_hi - j_lo + WARPS - 1) / WARPS + 127) / 128 * 128;   // keys of a warp
+  const int w_lo = min(j_lo + warp * per, j_hi), w_hi = min(w_lo + per, j_hi);
+  const uint32_t before_me = (1u << lane) - 1u;
+  auto one = [&](int j) -> uint32_t {
+    if (kept_in_smem) return keys[j - j_lo];
+    return j < first || j >= len - last ? EV_STAYS : weight_key(w[j]);
+  };
+  int sures = 0, ties = 0;
+#pragma unroll 4
+  for (int j = w_lo + lane; j < w_hi; j += 32) {
+    const uint32_t k = one(j);
+    sures += k > prefix;
+    ties += k == prefix;
+  }
+  sures = __reduce_add_sync(0xffffffffu, sures);
+  ties = __reduce_add_sync(0xffffffffu, ties);
+  if (lane == 0) {
+    of_warp[0][warp] = sures;
+    of_warp[1][warp] = ties;
+  }
+  __syncthreads();
+  // what stays ahead: in earlier warps (a lane each), and in the CTAs with earlier keys
+  const int of0 = lane < WARPS ? of_warp[0][lane] : 0, of1 = lane < WARPS ? of_warp[1][lane] : 0;
+  int s = __reduce_add_sync(0xffffffffu, lane < warp ? of0 : 0), t = __reduce_add_sync(0xffffffffu, lane < warp ? of1 : 0);
+  if (!alone) {
+    const int all0 = __reduce_add_sync(0xffffffffu, of0), all1 = __reduce_add_sync(0xffffffffu, of1);
+    if (tid == 0) {
+      counts[0] = all0;
+      counts[1] = all1;
+    }
+    cluster_sync();
+    s += __reduce_add_sync(0xffffffffu, lane < rank ? remote(&counts[0], lane) : 0);
+    t += __reduce_add_sync(0xffffffffu, lane < rank ? remote(&counts[1], lane) : 0);
+  }
+#pragma unroll 2
+  for (int j0 = w_lo; j0 < w_hi; j0 += 32) {
+    const int j = j0 + lane;
+    const uint32_t k = j < w_hi ? one(j) : 0u;
+    const bool sure = j < w_hi && k > prefix, tie = j < w_hi && k == prefix;
+    const uint32_t sure_of = __ballot_sync(0xffffffffu, sure), tie_of = __ballot_sync(0xffffffffu, tie);
+    const int at = t + __popc(tie_of & before_me);
+    if (sure || (tie && at < need)) {
+      const int slot = s + __popc(sure_of & before_me) + min(at, need);
+      idx[slot] = j;
+      dw[slot] = k == EV_STAYS ? w[j] : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+    }
+    s += __popc(sure_of);
+    t += __popc(tie_of);
+  }
+  if (!alone) cluster_sync();   // no CTA leaves while another one reads its numbers
 }
 
 // The rows that stay, 16 bytes per thread: HD / 32 threads for K and as many for V, the first of each with the pair.
