@@ -12,6 +12,7 @@
 
 #include "kv4.cuh"
 #include "tma.cuh"
+#include "umma.cuh"
 
 namespace dllm {
 
@@ -85,22 +86,35 @@ __device__ __forceinline__ void load_row(const __nv_bfloat16* p, float (&x)[16],
 // The codes of a lane's sixteen elements of a row with least `lo` and largest `hi`, and the row's pair.
 __device__ __forceinline__ uint2 encode16(const float (&x)[16], float lo, float hi, uint32_t& pair) {
   const __nv_bfloat16 lo_b = __float2bfloat16_rn(lo);
-  __nv_bfloat16 step_b = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+  // The IEEE quotient by 15: a product with the rounded reciprocal and one correction (right for every significand there is,
+  // where the product alone is off for 5.4 of 8.4 million), unless a remainder could leave fp32's range.
+  const float spread = __fsub_rn(hi, lo);
+  constexpr float FIFTEENTH = 1.f / 15.f;
+  float q15 = __fmul_rn(spread, FIFTEENTH);
+  q15 = __fmaf_rn(__fmaf_rn(-q15, 15.f, spread), FIFTEENTH, q15);
+  if (spread < 1e-28f) q15 = __fdiv_rn(spread, 15.f);
+  __nv_bfloat16 step_b = __float2bfloat16_rn(q15);
   if (__bfloat162float(step_b) == 0.f) step_b = __float2bfloat16_rn(1.f);
   const float lo_f = __bfloat162float(lo_b), step = __bfloat162float(step_b);
-  // The quotient by a product with the reciprocal and one correction, rounded by adding 1.5 * 2^23.  The corrected product is
-  // off by 2^-46 of itself before it is rounded, so it meets a tie exactly where the quotient does (half steps are exact, and
-  // the nearest other d is further off than half a unit of the quotient): this is rint of the IEEE quotient without its cost.
-  // Rows that it does not hold for are divided: tiny steps, and fp32 rows whose offset was rounded by so much that quotients
-  // leave 0..15.  Four codes add up to 16 bits in fp32.  (Store of 16 x 1536 tokens of 32 heads, bf16, 78 us of bytes: 310 us
-  // with a division per element, 130 us now.)
-  const float inv = __frcp_rn(step);
+  // The quotient by a product with the reciprocal (to 2^-23) and one correction, rounded by adding 1.5 * 2^23.  The corrected
+  // product is off by 2^-45 of itself before it is rounded, so it meets a tie exactly where the quotient does: half steps are
+  // exact, and a step has 8 bits, so the quotient of the nearest other d is 2^-32 of itself away from where it would be rounded
+  // to the tie.  This is rint of the IEEE quotient without its cost.  Rows that it does not hold for are divided: tiny and huge
+  // steps, and fp32 rows whose offset was rounded by so much that quotients leave 0..15.  Four codes add up to 16 bits in fp32.
+  // (Store of 16 x 1536 tokens of 32 heads, bf16, 78 us of bytes: 310 us with a division per element, 134 one element at a time,
+  // 116 now.)
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
   float u[16];
-  if (lo >= lo_f && __fsub_rn(hi, lo_f) <= 15.4f * step && step > 1e-30f) {
+  if (lo >= lo_f && __fsub_rn(hi, lo_f) <= 15.4f * step && step > 1e-30f && step < 1e30f) {
+    const float2 inv2 = make_float2(inv, inv), minus = make_float2(-step, -step), from = make_float2(-lo_f, -lo_f);
+    const float2 up = make_float2(12582912.f, 12582912.f), down = make_float2(-12582912.f, -12582912.f);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float d = __fsub_rn(x[i], lo_f), p = __fmul_rn(d, inv);
-      u[i] = __fsub_rn(__fadd_rn(__fmaf_rn(__fmaf_rn(-p, step, d), inv, p), 12582912.f), 12582912.f);
+    for (int i = 0; i < 16; i += 2) {   // two at a time, each as fp32's own operations
+      const float2 d = add2(make_float2(x[i], x[i + 1]), from), p = mul2(d, inv2);
+      const float2 r = add2(add2(fma2(fma2(p, minus, d), inv2, p), up), down);
+      u[i] = r.x;
+      u[i + 1] = r.y;
     }
   } else {
 #pragma unroll
