@@ -15,11 +15,12 @@
 //     (s - lse) log2(e) = c * ( q . (v 2^e) + (off / m) sum(q) + (1 / c) (-lse log2(e)) )
 // v 2^e is exact in bf16, so are the rows; the other two products are taken over sixteen more elements, both factors in three
 // bf16 parts (24 bits), the six larger partial products of each.  The thread multiplies by c: a multiplication, an exponential
-// and an addition per score, and the special-function unit's four results per scheduler and cycle are what it takes.
+// and an addition per score.  The special-function unit's four results per scheduler and cycle would bound that, so a quarter of
+// the exponentials are polynomials on the FMA pipe (a fifth to a third take the same time, half 12 % more).
 // Every key's sum is taken by its two threads, the rows in their order, the shares of a cluster in theirs, and added once.
-// 4 sequences of 192 rows, 28 heads on 4, up to 16384 keys: 112 us, 78 of them exponentials at the special-function units' rate
-// (124 with a CTA per 256 keys, whose start and end took 7 us of each; 130 with rows brought in by cp.async, one tile on its way
-// at a time).  16 sequences of 512 rows x 1536 keys, 32 heads: 256 -> 205, of which 15 are the rows' parts.
+// 4 sequences of 192 rows, 28 heads on 4, up to 16384 keys: 105 us (112 with all exponentials on the special-function units, which
+// is 78 at their rate; 124 with a CTA per 256 keys, whose start and end took 7 us of each; 130 with rows brought in by cp.async,
+// one tile on its way at a time).  16 sequences of 512 rows x 1536 keys, 32 heads: 256 -> 200, of which 15 are the rows' parts.
 #include <algorithm>
 
 #include "kv4.cuh"
@@ -37,6 +38,24 @@ __device__ __forceinline__ float exp2_sfu(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// 2^x of two numbers on the FMA pipe: x split into an integer and the rest of -1/2 .. 1/2, on which a polynomial of degree 5 (minimax,
+// 2^-23.7 off) stands for 2^x.  Below 2^-126 zero, above 2^128 infinity, a NaN stays one.
+__device__ __forceinline__ float2 exp2_fma(float2 x) {
+  auto clamp = [](float v) {
+    float r;
+    asm("{\n\t.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0fC2FE0000;\n\tmin.NaN.f32 %0, t, 0f43000000;\n\t}" : "=f"(r) : "f"(v));   // -127, 128
+    return r;
+  };
+  auto both = [](float v) { return make_float2(v, v); };
+  const float2 y = make_float2(clamp(x.x), clamp(x.y)), r = add2(y, both(12582912.f)), f = add2(y, fma2(r, both(-1.f), both(12582912.f)));
+  float2 p = fma2(f, both(1.3276472e-3f), both(9.6755410e-3f));
+  p = fma2(p, f, both(5.5507131e-2f));
+  p = fma2(p, f, both(2.4022120e-1f));
+  p = fma2(p, f, both(6.9314694e-1f));
+  p = fma2(p, f, both(1.f));
+  return mul2(p, make_float2(__uint_as_float((__float_as_uint(r.x) << 23) + 0x3F800000u),
+                             __uint_as_float((__float_as_uint(r.y) << 23) + 0x3F800000u)));
 }
 __device__ __forceinline__ void put16(uint32_t addr, uint4 v) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -358,7 +377,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const float2 y = mul2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(mul, mul));
-            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], make_float2(exp2_sfu(y.x), exp2_sfu(y.y)));
+            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], (e >> 1) % 4 == 3 ? exp2_fma(y) : make_float2(exp2_sfu(y.x), exp2_sfu(y.y)));
           }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
