@@ -452,7 +452,10 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     }
   }
   ok = __syncthreads_and(ok);
-  if (!ok && tid == 0 && status) atomicCAS(status, ST_OK, ST_TIMEOUT_ATTN_UMMA);
+  if (!ok) {   // gave up: what is on its way (products, copies) ends before memory is released
+    if (tid == 0 && status) atomicCAS(status, ST_OK, ST_TIMEOUT_ATTN_UMMA);
+    drain_delay();
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (warp == UK_MMA_WARP)

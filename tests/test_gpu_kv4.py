@@ -270,6 +270,20 @@ def test_attention_of_queries_of_zeros(dllm, plan, a, kscale, qscale):
     assert bool(((w.double() - want).abs() <= err + 2.0 ** -23 * want).all())
 
 
+@pytest.mark.parametrize("B,a,n,H,Hkv", [(700, 1, 640, 2, 1), (100, 70, 300, 1, 1)])
+def test_many_sequences(dllm, plan, B, a, n, H, Hkv):
+    """More sequences than a warp has lanes, the first ones without keys; ranges of keys times sequences within a grid's limit."""
+    g = gen(14)
+    cache = ref.random_cache(dllm, g, B, Hkv, -(-n // 64) * 64, 64)
+    q, lens = queries(g, B, a, H, 64), lens_of([0] * 64 + [(37 * b) % (n + 1) for b in range(64, B)])
+    o, lse = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+    check_attention(q, cache, a, n, H, lens, o, lse)
+    w = torch.zeros((B, Hkv, cache.capacity), device="cuda")
+    dllm.attention_weights_kv4(q, cache, lse, w, a, n, H, lens=lens)
+    want, err = ref.weights(q, cache, lse, a, n, H, lens)
+    assert bool(((w.double() - want).abs() <= err + 2.0 ** -23 * want).all())
+
+
 def test_calls_on_two_streams_at_once(dllm):
     """The same products, attention and weights on two streams, each with buffers of its own, twenty times over."""
     g = gen(13)
