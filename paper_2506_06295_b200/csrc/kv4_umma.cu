@@ -172,12 +172,6 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
     const int t = tid - (OF_V ? UK_V_WARP : UK_K_WARP) * 32;
     const uint8_t* const codes = (OF_V ? c.v : c.k) + (plane + (size_t)tile_lo * UK_KEYS) * (HD / 2);
     const uint32_t* const pairs = (OF_V ? c.vp : c.kp) + plane + (size_t)tile_lo * UK_KEYS;
-    const int f = largest(pairs, t, T, OF_V ? 4 : 3);
-    if (lane == 0) atomicMax(&top[OF_V], f);
-    if constexpr (OF_V) asm volatile("bar.sync 3, %0;" ::"n"(T) : "memory");
-    else asm volatile("bar.sync 4, %0;" ::"n"(T) : "memory");
-    // V: |lo + step * code| < 2^(f - 125), to 2^15.  K: |lo|, 8 step < 2^(f - 126), to 2^7; 2^8 times that beside the sums
-    const float scale = pow2(OF_V ? 140 - top[1] : 133 - top[0]);
     uint4 x[N];
     uint32_t pr[N];
     auto fetch = [&](int round) {
@@ -191,7 +185,13 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         }
       }
     };
-    fetch(0);
+    fetch(0);   // on its way while the largest numbers are looked for
+    const int f = largest(pairs, t, T, OF_V ? 4 : 3);
+    if (lane == 0) atomicMax(&top[OF_V], f);
+    if constexpr (OF_V) asm volatile("bar.sync 3, %0;" ::"n"(T) : "memory");
+    else asm volatile("bar.sync 4, %0;" ::"n"(T) : "memory");
+    // V: |lo + step * code| < 2^(f - 125), to 2^15.  K: |lo|, 8 step < 2^(f - 126), to 2^7; 2^8 times that beside the sums
+    const float scale = pow2(OF_V ? 140 - top[1] : 133 - top[0]);
     for (int it = 0; it < 2 * n_tiles; ++it) {
       const int tile = it >> 1, st = tile % UK_STAGES;
       if (!(it & 1) && tile >= UK_STAGES &&
