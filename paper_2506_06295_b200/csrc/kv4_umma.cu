@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
         auto scores = [&](int part, uint32_t (&r)[32]) {
           tmem_ld32(s_col + (uint32_t)(part * 32), r);
-          tmem_ld_wait();
+          tmem_ld32_wait(r);
           if (valid < UK_KEYS) {   // the last tile of the sequence
 #pragma unroll
             for (int j = 0; j < 32; ++j)
@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
             for (int cc = 0; cc < HD; cc += 32) {
               uint32_t r[32];
               tmem_ld32(o_col + (uint32_t)cc, r);
-              tmem_ld_wait();
+              tmem_ld32_wait(r);
 #pragma unroll
               for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * corr);
               tmem_st32(o_col + (uint32_t)cc, r);
@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         for (int cc = 0; cc < HD; cc += 32) {
           uint32_t r[32];
           tmem_ld32(o_col + (uint32_t)cc, r);
-          tmem_ld_wait();
+          tmem_ld32_wait(r);
           if (!is_live) continue;
 #pragma unroll
           for (int k = 0; k < 32; k += 8) {

@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
           if (p >= left) break;
           uint32_t r[32];
           tmem_ld32(d + (uint32_t)p, r);
-          tmem_ld_wait();
+          tmem_ld32_wait(r);
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const float2 y = mul2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(mul, mul));
