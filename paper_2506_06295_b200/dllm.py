@@ -807,7 +807,7 @@ def kv4_load(cache: KV4Cache, n: int, lens=None, dtype=None, stream=None):
         _refuse("n must lie within the capacity")
     shape, dtype = (cache.B, n, cache.Hkv * cache.hd), torch.float32 if dtype is None else dtype
     k = cache._base.new_empty(shape, dtype=dtype)
-    v = k.new_empty(shape)
+    v = torch.empty_like(k)
     _check(lib.dllm_kv4_load(cache.ref, n, _lens(lens, cache), k.data_ptr(), v.data_ptr(), _dtype(k),
                              _stream_of(cache._base, lens)))
     return k, v

@@ -365,6 +365,45 @@ def test_attention_on_another_stream_and_in_a_graph(dllm, n):
     check_attention(q, cache, 4, n, 4, lens, o, lse)
 
 
+def test_all_calls_in_one_graph(dllm):
+    """Rows stored, attended to, scored, evicted and read back, few and many of them, and products, captured once and replayed on
+    other rows and lengths: what the calls give one by one."""
+    g = gen(15)
+    B, n, H, Hkv, hd = 2, 8192, 8, 4, 128
+    cache, again = dllm.KV4Cache(B, Hkv, n, hd), dllm.KV4Cache(B, Hkv, n, hd)
+    k = torch.randn((B, n, Hkv * hd), generator=g, device="cuda").bfloat16()
+    qs = [queries(g, B, a, H, hd) for a in (4, 200)]
+    xs = [queries(g, 1, rows, 16, hd) for rows in (3, 700)]
+    W, sw = dllm.quantize_rows_s8(queries(g, 1, 1024, 16, hd))
+    w, lens = torch.zeros((B, Hkv, n), device="cuda"), lens_of([8000, 5000])
+
+    def work(cache):
+        out = []
+        dllm.kv4_store(cache, k, k)
+        w.zero_()
+        for q in qs:
+            a = q.shape[0] // B
+            o, lse = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+            dllm.attention_weights_kv4(q, cache, lse, w, a, n, H, lens=lens)
+            out += [o, lse]
+        small, *rest = dllm.kv4_evict(cache, w, n, 1000, 4, 32, lens=lens)
+        return [*out, *rest, *dllm.kv4_load(small, 1000, lens=rest[2]), *(dllm.linear_s8(x, W, sw) for x in xs)]
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = work(cache)
+    for t in (k, *qs, *xs):
+        t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+    lens.copy_(lens_of([900, 8192]))
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    kept = [t.clone() for t in got]
+    for x, y in zip(kept, work(again)):
+        assert torch.equal(x, y)
+    dllm.kernel_status()
+
+
 # ---------------------------------------------------------------- weights
 @pytest.mark.parametrize("B,a,n,H,Hkv,hd,lens", SHAPES)
 def test_weights(dllm, plan, B, a, n, H, Hkv, hd, lens):
