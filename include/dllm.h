@@ -484,8 +484,10 @@ dllm_status dllm_kv4_load(const dllm_kv4_cache* cache, int n, const int32_t* d_l
  * n).  d_o bf16 [B * a, n_heads * head_dim]; d_lse (may be NULL) float [B * a,
  * n_heads]: the natural logarithm of each row's sum of exp(q . k / sqrt(head_dim)).
  * A row without keys gives zeros and -infinity.  Keys from the length on count for
- * nothing whatever stands there.  The steps and offsets are applied in fp32 outside
- * the matrix products, which work on the codes themselves. */
+ * nothing whatever stands there.  Scores are as good as fp32 sums over the cache's
+ * numbers; weights and values enter the second product in fp16, scaled into its range.
+ * d_scratch: as many bytes as the query asks for on the device that is current (NULL
+ * where that is 0), 16-byte aligned; calls that may overlap on the GPU need one each. */
 size_t dllm_attention_kv4_scratch_bytes(int B, int a, int n, int n_heads, int n_kv_heads, int head_dim);
 dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, void* d_o, float* d_lse, int a,
                                int n, int n_heads, const int32_t* d_lens, void* d_scratch, size_t scratch_bytes,

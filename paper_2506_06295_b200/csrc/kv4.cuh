@@ -5,11 +5,12 @@
 // contiguous ([B, Hkv, capacity, .]), so a tile of keys is one block of memory; capacity is a multiple of KV4_KEYS, so a
 // whole tile may be read wherever a sequence ends.
 //
-// No kernel multiplies the numbers themselves.  With v = u - 8 (a small integer, exact in fp16 and bf16)
+// With v = u - 8 (a small integer, exact in fp16 and bf16)
 //     q . k   = step * (q . v) + (lo + 8 step) * sum(q)
 //     sum p k = sum (p step) v + sum p (lo + 8 step)
-// so the matrix instructions work on exact integers, the steps and offsets stay in fp32 outside, and centring the codes
-// keeps the rounding of p * step from being multiplied by the offset.
+// For few rows the matrix instructions work on these exact integers, the steps and offsets stay in fp32 outside, and centring
+// the codes keeps the rounding of p * step from being multiplied by the offset.  What the tcgen05 kernels make of it stands at
+// kv4_umma.cu and kv4_weights.cu: exact products step * v for the scores, numbers rounded to fp16 once for the outputs.
 #pragma once
 #include <cuda_fp16.h>
 
