@@ -20,7 +20,7 @@
 // Every key's sum is taken by its two threads, the rows in their order, the shares of a cluster in theirs, and added once.
 // 4 sequences of 192 rows, 28 heads on 4, up to 16384 keys: 105 us (112 with all exponentials on the special-function units, which
 // is 78 at their rate; 124 with a CTA per 256 keys, whose start and end took 7 us of each; 130 with rows brought in by cp.async,
-// one tile on its way at a time).  16 sequences of 512 rows x 1536 keys, 32 heads: 256 -> 200, of which 15 are the rows' parts.
+// one tile on its way at a time).  16 sequences of 512 rows x 1536 keys, 32 heads: 256 -> 196, of which 15 are the rows' parts.
 #include <algorithm>
 
 #include "kv4.cuh"
@@ -384,8 +384,8 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&d_empty[i][buf]));
         // The other half of the keys' buffers is free: the products of the unit before this one are complete, since this warp
-        // has had all of their results.
-        if (u == 0 && next.len > 0) next_mul = convert(j + 1);
+        // has had all of their results.  (The four groups of warps in turn, so that the exponentials of the others go on.)
+        if (u == min(2 * i + half, n_tiles - 1) && next.len > 0) next_mul = convert(j + 1);
       }
       const float got = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       if (shares > 1) {
