@@ -18,9 +18,9 @@
 // and an addition per score.  The special-function unit's four results per scheduler and cycle would bound that, so a quarter of
 // the exponentials are polynomials on the FMA pipe (a fifth to a third take the same time, half 12 % more).
 // Every key's sum is taken by its two threads, the rows in their order, the shares of a cluster in theirs, and added once.
-// 4 sequences of 192 rows, 28 heads on 4, up to 16384 keys: 105 us (112 with all exponentials on the special-function units, which
+// 4 sequences of 192 rows, 28 heads on 4, up to 16384 keys: 104 us (112 with all exponentials on the special-function units, which
 // is 78 at their rate; 124 with a CTA per 256 keys, whose start and end took 7 us of each; 130 with rows brought in by cp.async,
-// one tile on its way at a time).  16 sequences of 512 rows x 1536 keys, 32 heads: 256 -> 196, of which 15 are the rows' parts.
+// one tile on its way at a time).  16 sequences of 512 rows x 1536 keys, 32 heads: 256 -> 183, of which 15 are the rows' parts.
 #include <algorithm>
 
 #include "kv4.cuh"
@@ -350,19 +350,28 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
       return mul;
     };
     float mul = 0.f, next_mul = 0.f;
+    Unit next{0, 0, 0, 0}, third{0, 0, 0, 0};   // the unit whose codes are in registers or on their way, and the one behind it
     if (first.len > 0) {
       fetch(first);
       mul = convert(0);
+      next = next_unit();
+      if (next.len > 0) fetch(next);
     }
     int it = 0, j = 0;
-    for (Unit w = first, next; w.len > 0; w = next, mul = next_mul, ++j) {
-      next = next_unit();
-      if (next.len > 0) fetch(next);   // on its way during this unit's first rows
+    for (Unit w = first; w.len > 0; w = next, next = third, mul = next_mul, ++j) {
       const bool mine_to_add = shares == 1 && half == 0 && w.block * WK_KEYS + mine < w.len;
       const float had = mine_to_add ? weight[key_of(w)] : 0.f;
       float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
       for (int u = 0; u < n_tiles; ++u, ++it) {
         const int buf = it & 1;
+        // The next unit's keys, whose half of the buffers is free: the products of the unit before this one are complete, since
+        // this warp has had all of their results.  (The four groups of warps in turn, so that the exponentials of the others go
+        // on; ahead of the wait, so that the products of a unit of one tile run meanwhile.)
+        if (u == min(2 * i + half, n_tiles - 1) && next.len > 0) {
+          next_mul = convert(j + 1);
+          third = next_unit();
+          if (third.len > 0) fetch(third);
+        }
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&d_full[i][buf]), (uint32_t)(it >> 1) & 1u, abortp));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -383,9 +392,6 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&d_empty[i][buf]));
-        // The other half of the keys' buffers is free: the products of the unit before this one are complete, since this warp
-        // has had all of their results.  (The four groups of warps in turn, so that the exponentials of the others go on.)
-        if (u == min(2 * i + half, n_tiles - 1) && next.len > 0) next_mul = convert(j + 1);
       }
       const float got = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       if (shares > 1) {
