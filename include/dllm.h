@@ -316,7 +316,9 @@ dllm_status dllm_kernel_status(void* stream);
  * the one-CTA bf16 GEMM kernel leaves out one activation-tile copy, so one of
  * its pipeline stages never completes, its waits run into the limit, the CTA
  * records the status code, skips its epilogue, frees its tensor memory and
- * returns normally; (0) switches that off.  Both calls synchronise the device. */
+ * returns normally; one CTA of every launch of the 4-bit cache's tcgen05 weights
+ * leaves out a copy likewise.  (0) switches that off.  Both calls synchronise the
+ * device. */
 dllm_status dllm_debug_set_wait_limit_ns(uint64_t ns);
 /* Tuning / test hook: kernel choice of the bf16 projections, for every later
  * call in this process: 0 automatic (persistent CTA pairs above 128 activation
@@ -502,7 +504,8 @@ dllm_status dllm_debug_kv4_plan(int kernel, int splits);
  * capacity]) += the sum over the a queries and the query heads of KV head h of
  * exp(q . k_j / sqrt(head_dim) - lse), for j below the sequence's length; the other
  * weights stay as they are.  d_lse as dllm_attention_kv4 leaves it; a row whose lse is
- * -infinity gives nothing.  Sums are taken in a fixed order.  d_scratch: as many bytes as
+ * -infinity gives nothing.  Sums are taken in a fixed order, and a key's is added whole or, where a
+ * wait of the call gave up (DLLM_TIMEOUT), not at all.  d_scratch: as many bytes as
  * the query asks for (NULL where that is 0), 16-byte aligned; calls that may overlap on
  * the GPU need one each. */
 size_t dllm_attention_weights_kv4_scratch_bytes(int B, int a, int n_heads, int n_kv_heads);

@@ -85,5 +85,6 @@ size_t kv4_weights_umma_scratch_bytes(int B, int a, int H, int Hkv);
 cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                     int a, int n, int H, const int32_t* lens, void* scratch);
 cudaError_t set_wait_limit_kv4_weights(unsigned long long ns);
+cudaError_t set_debug_skip_kv4_weights(int enable);   // dllm_debug_skip_one_load
 
 }  // namespace dllm

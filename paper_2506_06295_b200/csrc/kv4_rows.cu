@@ -268,12 +268,6 @@ __device__ __forceinline__ int block_scan(int v, int* warps, int& total) {   // 
   const int before = __shfl_sync(0xffffffffu, t, max(w - 1, 0));
   return (w == 0 ? 0 : before) + s - v;
 }
-// A number from the same place of shared memory in the cluster's CTA `rank`
-__device__ __forceinline__ int remote(const int* p, uint32_t rank) {
-  int r;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(r) : "r"(cluster_addr(smem_u32(p), rank)));
-  return r;
-}
 
 // A cluster of one or eight CTAs per (sequence, KV head), each with its share of the keys, kept in shared memory as ordered
 // numbers where they fit.  The smallest number that stays is found digit by digit (8 bits, a histogram of its own each, so that

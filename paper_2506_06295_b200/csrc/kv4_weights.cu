@@ -31,6 +31,10 @@ namespace dllm {
 
 namespace {
 
+// Test hook (dllm_debug_skip_one_load): while non-zero, the last CTA that shares the first unit (the first one where none is
+// shared) leaves out a box of its first rows, so that its waits run into their limit.
+static __device__ int g_debug_skip = 0;
+
 constexpr int WK_TILE = 128, WK_KEYS = 2 * WK_TILE, WK_ROWS = 128, WK_STAGES = 2, WK_THREADS = 18 * 32, WK_MMA_WARP = 16,
               WK_Q_WARP = 17, WK_CLUSTER = 8;
 
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
   __shared__ __align__(8) uint64_t k_full[2], q_full[WK_STAGES], q_empty[WK_STAGES], d_full[2][2], d_empty[2][2];
   __shared__ __align__(16) float total[2][WK_KEYS];
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, complete;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, ring = base + 2 * SM::KEYS;
@@ -240,6 +244,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
 
   if (warp >= WK_Q_WARP) {
     // ---------------- the rows ----------------
+    const bool skip = g_debug_skip != 0 && (int)blockIdx.x == shares - 1;
     // for the rows' parts; what the others read was there before the launch that makes them
     pdl_wait();
     pdl_trigger();
@@ -256,7 +261,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
           const uint32_t to = ring + st * SM::STAGE, bar = smem_u32(&q_full[st]);
           mbar_expect_tx(bar, (uint32_t)used * HD * 2 + SM::MORE);
 #pragma unroll
-          for (int h = 0; h < HD / 64; ++h)
+          for (int h = skip && it == 0 ? 1 : 0; h < HD / 64; ++h)
             tma_load_5d(to + h * (WK_ROWS * 128), &tmQ, bar, h * 64, t % til.pieces * til.gbox, w.kh, t / til.pieces * til.queries, w.b);
           bulk_load_1d(to + SM::OPERAND, pb + 2 * (size_t)u * WK_ROWS, SM::MORE, bar);
         }
@@ -418,14 +423,20 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
   if (shares > 1) {   // the cluster has one unit, or none
     float got = tid < WK_KEYS ? total[0][tid] + total[1][tid] : 0.f;
     if (tid < WK_KEYS) total[0][tid] = got;
+    if (tid == 0) complete = ok;
     cluster_sync();
-    if (rank == 0 && tid < WK_KEYS && first.block * WK_KEYS + tid < first.len) {
+    if (rank == 0 && tid < WK_KEYS) {
+      // all shares or nothing: where one of them gave up, the weights stay as they were
+      const int of = lane < shares ? remote(&complete, lane) : 1;
+      const bool mine = first.block * WK_KEYS + tid < first.len;
+      float* const to = weight + ((size_t)first.b * c.Hkv + first.kh) * c.cap + first.block * WK_KEYS + tid;
+      const float had = mine ? *to : 0.f;
       for (int s = 1; s < shares; ++s) {
         float x;
         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(cluster_addr(smem_u32(&total[0][tid]), s)));
         got += x;
       }
-      weight[((size_t)first.b * c.Hkv + first.kh) * c.cap + first.block * WK_KEYS + tid] += got;
+      if (__all_sync(0xffffffffu, of != 0) && mine) *to = had + got;
     }
     cluster_sync();   // no CTA leaves while another one reads its sums
   }
@@ -476,6 +487,13 @@ cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, 
                     : weights_as<128>(L, (const __nv_bfloat16*)q, ldq, c, lse, weight, a, n, H, lens, (uint4*)scratch);
 }
 
+}  // namespace dllm
+
+namespace dllm {
+cudaError_t set_debug_skip_kv4_weights(int enable) {
+  const int v = enable != 0;
+  return cudaMemcpyToSymbol(g_debug_skip, &v, sizeof v);
+}
 }  // namespace dllm
 
 DLLM_WAIT_LIMIT_HOOK(kv4_weights)

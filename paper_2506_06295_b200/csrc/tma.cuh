@@ -179,6 +179,12 @@ __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
+// A number from the same place of shared memory in the cluster's CTA `rank`; between two cluster_sync().
+__device__ __forceinline__ int remote(const int* p, uint32_t rank) {
+  int r;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(r) : "r"(cluster_addr(smem_u32(p), rank)));
+  return r;
+}
 // every thread of every CTA of the cluster
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");

@@ -540,7 +540,7 @@ def debug_set_wait_limit_ns(ns: int) -> None:
 
 
 def debug_skip_one_load(enable: bool) -> None:
-    """Test hook: the first CTA of every one-CTA bf16 GEMM launch leaves out one tile copy (its waits run out)."""
+    """Test hook: one CTA of every launch of the kernels that include/dllm.h names leaves out one copy (its waits run out)."""
     _check(lib.dllm_debug_skip_one_load(int(enable)))
 
 

@@ -1,0 +1,66 @@
+"""The bounded waits of the 8-bit and 4-bit kernels, made to run out without faulting or hanging anything: a host-set flag makes
+one CTA of a launch leave out one copy or one arrival, and a limit of a few milliseconds ends the waits for it.  The call reports
+DLLM_TIMEOUT once, what it could not finish stays unwritten, and the next call works as if nothing had happened."""
+import pytest
+import torch
+
+from tests import lowbit_ref as ref
+
+pytestmark = pytest.mark.gpu
+LIMIT_NS = 3_000_000      # 3 ms per wait
+
+
+@pytest.fixture(scope="module")
+def dllm():
+    from paper_2506_06295_b200 import build as build_mod
+    build_mod.build()
+    from paper_2506_06295_b200 import dllm as d
+    yield d
+    d.debug_skip_one_load(False)          # whatever a failing test left behind
+    d.debug_set_wait_limit_ns(0)
+    d.debug_kv4_plan()
+
+
+def run_out(dllm, call):
+    """`call` with one of its CTAs' waits running out: it must report that, at its limit, and once."""
+    dllm.kernel_status()                  # clean to start with
+    dllm.debug_set_wait_limit_ns(LIMIT_NS)
+    dllm.debug_skip_one_load(True)
+    try:
+        t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        t0.record()
+        call()
+        t1.record()
+        with pytest.raises(dllm.DllmError) as e:
+            dllm.kernel_status()
+        assert e.value.status == dllm.TIMEOUT
+        assert 0.5 * LIMIT_NS / 1e6 < t0.elapsed_time(t1) < 1000.0
+    finally:
+        dllm.debug_skip_one_load(False)
+        dllm.debug_set_wait_limit_ns(0)
+    dllm.kernel_status()                  # the word was cleared by the read
+
+
+@pytest.mark.parametrize("a,n,hd", [(512, 512, 128), (512, 512, 64), (256, 40000, 128)])
+def test_weights_are_added_whole_or_not_at_all(dllm, a, n, hd):
+    """512 rows of two heads over 512 keys: four units of 256 keys, their rows in eight shares of one tile of 128 each, the last
+    of which gives up.  40000 keys: a CTA for each of several units.  The keys of the unit that gave up keep their weights to the
+    bit; every other key gets all of its sum or nothing."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(a + n + hd)
+    Hkv, H, cap = 2, 4, -(-n // 64) * 64
+    cache = ref.random_cache(dllm, g, 1, Hkv, cap, hd)
+    q = torch.randn((a, H * hd), generator=g, device="cuda").bfloat16()
+    _, lse = dllm.attention_kv4(q, cache, a, n, H)
+    had = torch.rand((1, Hkv, cap), generator=g, device="cuda")
+    want = had.clone()
+    dllm.attention_weights_kv4(q, cache, lse, want, a, n, H)
+    w = had.clone()
+    run_out(dllm, lambda: dllm.attention_weights_kv4(q, cache, lse, w, a, n, H))
+    assert torch.equal(w[0, 0, :256], had[0, 0, :256])
+    assert bool(((w == had) | (w == want)).all())
+    assert n > 1000 or torch.equal(w[0, 1], want[0, 1]) and torch.equal(w[0, 0, 256:], want[0, 0, 256:])
+    w = had.clone()
+    dllm.attention_weights_kv4(q, cache, lse, w, a, n, H)
+    assert torch.equal(w, want)
+    dllm.kernel_status()
