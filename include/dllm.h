@@ -316,9 +316,9 @@ dllm_status dllm_kernel_status(void* stream);
  * the one-CTA bf16 GEMM kernel leaves out one activation-tile copy, so one of
  * its pipeline stages never completes, its waits run into the limit, the CTA
  * records the status code, skips its epilogue, frees its tensor memory and
- * returns normally; one CTA of every launch of the 4-bit cache's tcgen05 weights
- * leaves out a copy likewise.  (0) switches that off.  Both calls synchronise the
- * device. */
+ * returns normally; one CTA of every launch of the one-CTA kernel of the 8-bit
+ * products and of the 4-bit cache's tcgen05 weights leaves out a copy likewise.
+ * (0) switches that off.  Both calls synchronise the device. */
 dllm_status dllm_debug_set_wait_limit_ns(uint64_t ns);
 /* Tuning / test hook: kernel choice of the bf16 projections, for every later
  * call in this process: 0 automatic (persistent CTA pairs above 128 activation

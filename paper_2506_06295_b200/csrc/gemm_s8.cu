@@ -18,6 +18,10 @@ namespace dllm {
 
 namespace {
 
+// Test hook (dllm_debug_skip_one_load): while non-zero, CTA (0, 0, last range of k) of every launch of the one-CTA kernel leaves
+// out its first tile of A, so that its waits run into their limit.
+static __device__ int g_debug_skip = 0;
+
 constexpr int S8_K = 128;    // integers of k per stage: one 128-byte swizzle row
 
 // W columns (rows of A) of a finished tile, TMEM lane = weight row: 128 threads, tl = 0..127 = lane, all in step.  split: the
@@ -111,7 +115,9 @@ __global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_consta
   const int kb0 = blockIdx.z * kb_per_split, nkb = min(num_kb, kb0 + kb_per_split) - kb0;   // >= 1 by the plan
   const uint32_t tiles = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const int pre = min(stages, nkb);  // stages whose weight tile is requested before the dependency wait
+  int dbg_skip = 0;
   if (warp == 0) {
+    dbg_skip = g_debug_skip;  // read here, long before it is used: not on the path behind the dependency wait
     if (elect_one()) {
       abort_flag = 0;
       for (int s = 0; s < stages; ++s) {
@@ -150,6 +156,7 @@ __global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_consta
     for (int i = 0; i < nkb; ++i) {
       const uint32_t fb = smem_u32(&full_bar[s]), dst = tiles + s * SL::STAGE_BYTES;
       const int kc = (kb0 + i) * S8_K;
+      const bool skip = i == 0 && dbg_skip != 0 && (blockIdx.x | blockIdx.y) == 0 && blockIdx.z == gridDim.z - 1;
       if (i >= pre && !mbar_wait_warp(smem_u32(&empty_bar[s]), ph ^ 1u, abortp)) {
         if (status && lane == 0) atomicCAS(status, ST_OK, ST_TIMEOUT_TMA);
         break;
@@ -159,7 +166,7 @@ __global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_consta
           mbar_expect_tx(fb, SL::STAGE_BYTES);
           tma_load_2d_weights<ONCE>(dst, &tmW, fb, kc, n0);
         }
-        tma_load_2d(dst + W_STAGE_BYTES, &tmA, fb, kc, m0);
+        if (!skip) tma_load_2d(dst + W_STAGE_BYTES, &tmA, fb, kc, m0);
       }
       __syncwarp();
       if (++s == stages) {
@@ -223,6 +230,7 @@ __global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_consta
     }
     cluster_sync();
     const int rank = (int)cluster_ctarank(), n = n0 + lane * 4;   // four columns per lane, a row per warp
+    const int gave_up = lane < S ? remote(&abort_flag, lane) : 0;   // one of the ranges: the tile stays as it was
     float w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = n + e < N ? sw[n + e] : 0.f;
@@ -236,6 +244,7 @@ __global__ void __launch_bounds__(S8_THREADS) gemm_s8_kernel(const __grid_consta
         const int4 x = remote4(cluster_addr(at, s));
         sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
       }
+      if (__any_sync(0xffffffffu, gave_up != 0)) break;   // (requested together with the integers)
       const float a = sa[m0 + row], y[4] = {__int2float_rn(sum.x) * a * w[0], __int2float_rn(sum.y) * a * w[1],
                                             __int2float_rn(sum.z) * a * w[2], __int2float_rn(sum.w) * a * w[3]};
       T* const dst = out + (size_t)(m0 + row) * N + n;
@@ -593,6 +602,13 @@ cudaError_t launch_quantize_rows_s8(const Launch& L, const void* x, size_t ldx, 
                             : quantize_as(L, (const float*)x, ldx, q, ldq, scale, rows, cols);
 }
 
+}  // namespace dllm
+
+namespace dllm {
+cudaError_t set_debug_skip_gemm_s8(int enable) {
+  const int v = enable != 0;
+  return cudaMemcpyToSymbol(g_debug_skip, &v, sizeof v);
+}
 }  // namespace dllm
 
 DLLM_WAIT_LIMIT_HOOK(gemm_s8)

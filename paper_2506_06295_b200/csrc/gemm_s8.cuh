@@ -14,5 +14,6 @@ cudaError_t launch_gemm_s8(const Launch& L, const int8_t* A, size_t lda, const f
                            const float* sw, void* out, int out_dtype, int M, int N, int K, const GemmPlan& plan, void* scratch,
                            const char** err);
 cudaError_t set_wait_limit_gemm_s8(unsigned long long ns);
+cudaError_t set_debug_skip_gemm_s8(int enable);   // dllm_debug_skip_one_load
 
 }  // namespace dllm

@@ -64,3 +64,25 @@ def test_weights_are_added_whole_or_not_at_all(dllm, a, n, hd):
     dllm.attention_weights_kv4(q, cache, lse, w, a, n, H)
     assert torch.equal(w, want)
     dllm.kernel_status()
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(3, 300, 4096), (60, 300, 2048), (40, 300, 200), (200, 513, 4096)])
+def test_a_tile_of_a_product_is_written_whole_or_not_at_all(dllm, M, N, K, out):
+    """Few rows: the first tile of 128 columns is cut into ranges of k (eight, four, one and eight of them) whose last one gives up.
+    The tile keeps what stood there; the others are right."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(M + K)
+    A = torch.randint(-128, 128, (M, -(-K // 16) * 16), generator=g, device="cuda", dtype=torch.int8)[:, :K]
+    W = torch.randint(-128, 128, (N, -(-K // 16) * 16), generator=g, device="cuda", dtype=torch.int8)[:, :K]
+    sa, sw = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+    want = dllm.gemm_s8(A, sa, W, sw, out_dtype=out)
+    y = torch.full((M, N), -77.0, dtype=out, device="cuda")
+    run_out(dllm, lambda: dllm.gemm_s8(A, sa, W, sw, out=y))
+    rows = min(M, 128)                   # of a tile
+    part = want.clone()
+    part[:rows, :128] = -77.0
+    assert torch.equal(y, part)
+    assert dllm.gemm_s8(A, sa, W, sw, out=y) is y
+    dllm.kernel_status()
+    assert torch.equal(y, want)
