@@ -429,6 +429,31 @@ def test_weights(dllm, plan, B, a, n, H, Hkv, hd, lens):
     assert torch.equal(w, again)
 
 
+def test_exponentials_of_the_weights_alone(dllm):
+    """One row per sequence that counts, a query of zeros, over one key: the key gets exp(-lse), by the special-function unit or,
+    in rows 6 and 7 of eight, by a polynomial.  x = -lse log2(e), |x| <= 0.73, is off by at most 2^-21.3 of itself (the constant,
+    the product, 1 / c and c 2^-25 + 3 * 2^-24, parts left out 2^-26, the matrix instruction's sum 2^-22), so 2e-7 of the result;
+    the exponentials by 2^-22.5 each (1.7e-7).  What is rounded either way leaves the mean of 2048 results of a class of rows, with lse
+    as often positive as negative, where the polynomial's own mean puts it: 1.7e-8 off."""
+    g = gen(16)
+    B, a, hd = 8192, 128, 64
+    cache = dllm.KV4Cache(B, 1, 64, hd)
+    cache.k_params[..., 0] = (1 + torch.rand((B, 1, 64), generator=g, device="cuda")).bfloat16()
+    half = (torch.rand(B // 2, generator=g, device="cuda") - 0.5)[:, None]
+    live = torch.cat([half, -half], 1).flatten()               # each value beside its negative
+    row = (torch.arange(B, device="cuda") // 2) % a
+    lse = torch.full((B, a), -math.inf, device="cuda")
+    lse[torch.arange(B, device="cuda"), row] = live
+    w = torch.zeros((B, 1, 64), device="cuda")
+    dllm.attention_weights_kv4(torch.zeros((B * a, hd), device="cuda").bfloat16(), cache, lse.reshape(B * a, 1), w, a, 1, 1)
+    assert not w[:, 0, 1:].any()
+    off = w[:, 0, 0].double() / torch.exp(-live.double()) - 1
+    assert float(off.abs().max()) < 4e-7
+    poly = off[row % 8 >= 6]
+    assert poly.numel() == B // 4 and abs(float(poly.mean())) < 4e-8, float(poly.mean())
+    dllm.kernel_status()
+
+
 # ---------------------------------------------------------------- eviction
 @pytest.mark.parametrize("B,n,keep,first,last,Hkv,hd,lens,ties", [
     (1, 1, 1, 0, 0, 1, 64, None, False), (1, 100, 1, 0, 0, 2, 128, None, False), (1, 100, 40, 0, 0, 2, 128, None, True),
