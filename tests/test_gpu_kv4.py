@@ -229,6 +229,38 @@ def test_attention_of_very_large_and_very_small_numbers(dllm, plan, a, qs, cs):
     check_attention(q, cache, a, 311, 2, None, o, lse)
 
 
+def offset_cache(dllm, g, B, Hkv, cap, hd):
+    """Keys and values whose offsets are some sixty steps: what a score then is made of is the offset times the query's sum."""
+    cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
+    for t in (cache.k_params, cache.v_params):
+        t[..., 1] += 12 * torch.randn((B, Hkv, cap), generator=g, device="cuda").bfloat16()
+    return cache
+
+
+def offset_queries(g, B, a, H, hd):
+    """Rows whose mean is as large as their spread, so small that the scores (some 1.06 * 12 * 0.015 * sqrt(hd) = 2) leave the softmax
+    spread."""
+    return (0.015 * (1 + torch.randn((B * a, H * hd), generator=g, device="cuda"))).bfloat16()
+
+
+@pytest.mark.parametrize("B,a,n,H,Hkv,hd,lens", [(1, 1, 65, 1, 1, 128, None), (2, 9, 700, 14, 2, 128, [700, 333]), (1, 64, 768, 4, 4, 64, None),
+                                                 (2, 150, 450, 4, 2, 128, [450, 33]), (1, 300, 1300, 2, 1, 64, None)])
+def test_scores_made_of_offsets(dllm, plan, B, a, n, H, Hkv, hd, lens):
+    """Sums and offsets reach both tensor-core kernels in parts: two parts of three would be off by 2^-17 of a score, and the
+    bounds allow some 2^-19 of it."""
+    g = gen(17 + n)
+    cache = offset_cache(dllm, g, B, Hkv, -(-n // 64) * 64, hd)
+    q, lens = offset_queries(g, B, a, H, hd), lens_of(lens)
+    o, lse = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+    check_attention(q, cache, a, n, H, lens, o, lse)
+    w = torch.zeros((B, Hkv, cache.capacity), device="cuda")
+    dllm.attention_weights_kv4(q, cache, lse, w, a, n, H, lens=lens)
+    want, err = ref.weights(q, cache, lse, a, n, H, lens)
+    bound = err + 2.0 ** -23 * want
+    assert bool(((w.double() - want).abs() <= bound).all()), float(((w.double() - want).abs() / bound.clamp_min(1e-300)).max())
+    dllm.kernel_status()
+
+
 @pytest.mark.parametrize("a", [4, 100])
 def test_attention_over_values_of_very_different_steps(dllm, plan, a):
     g = gen(8)
