@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __r
   if (len <= keep) {   // every key stays (the whole cluster)
     for (int j = j_lo + tid; j < j_hi; j += EV_THREADS) {
       idx[j] = j;
-      dw[j] = w[j];
+      dw[j] = w[j] + 0.f;   // -0 as 0
     }
     return;
   }
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(EV_THREADS) kv4_select_kernel(const float* __r
     if (sure || (tie && at < need)) {
       const int slot = s + __popc(sure_of & before_me) + min(at, need);
       idx[slot] = j;
-      dw[slot] = k == EV_STAYS ? w[j] : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+      dw[slot] = k == EV_STAYS ? w[j] + 0.f : __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
     }
     s += __popc(sure_of);
     t += __popc(tie_of);

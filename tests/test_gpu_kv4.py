@@ -540,6 +540,20 @@ def test_evict_of_many_heads_and_many_keys(dllm, Hkv, n, lens):
     assert torch.equal(nw[..., :kept], w.gather(-1, rows)) and not nw[..., kept:].any()
 
 
+@pytest.mark.parametrize("n,keep,first,last", [(300, 300, 0, 0), (300, 120, 40, 40), (9000, 9000, 3, 3), (9000, 5000, 1500, 1500), (41000, 600, 200, 200)])
+def test_evicted_weights_of_minus_zero_are_zero(dllm, n, keep, first, last):
+    """To the bit, whichever way a key stays: by its place, by its weight, or because all do."""
+    g = gen(n + keep)
+    cap = -(-n // 64) * 64
+    cache = ref.random_cache(dllm, g, 1, 2, cap, 64)
+    w = torch.randint(0, 3, (1, 2, cap), generator=g, device="cuda").float()
+    w[(torch.rand(w.shape, generator=g, device="cuda") < 0.5) & (w == 0)] = -0.0
+    _, nw, index, _ = dllm.kv4_evict(cache, w, n, keep, first, last)
+    want = w.gather(-1, index.long())
+    assert bool((want.view(torch.int32) == -2 ** 31).any())          # some of those that stayed were -0
+    assert torch.equal(nw[..., :keep].view(torch.int32), (want + 0.0).view(torch.int32))
+
+
 # ---------------------------------------------------------------- as they are used together
 def test_a_prompt_is_cached_scored_and_thinned_out(dllm):
     """Prompt and response rows go into the cache, the response's queries attend and score, half of the prompt leaves, and
