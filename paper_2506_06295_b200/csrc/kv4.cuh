@@ -68,18 +68,26 @@ cudaError_t launch_kv4_store(const Launch& L, const Kv4& c, const void* k, const
 cudaError_t launch_kv4_load(const Launch& L, const Kv4& c, int n, const int32_t* lens, void* k, void* v, int dtype);
 cudaError_t launch_kv4_evict(const Launch& L, const Kv4& src, const float* weight, int n, int keep, int first, int last,
                              const int32_t* lens, const Kv4& dst, float* dst_weight, int32_t* index, int32_t* new_lens);
-// kv4_attention.cu
+// kv4_attention.cu.  A call makes its plan once: its scratch is checked against the plan that is launched, whatever another
+// thread does to the hook meanwhile.
 void set_kv4_plan(int kernel, int splits);   // dllm_debug_kv4_plan
-size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd);
-cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n,
-                                 int H, const int32_t* lens, float* scratch, size_t scratch_floats);
+struct Kv4Plan {
+  bool umma = false;
+  int S = 1;                // ranges of keys
+  bool clustered = false;   // they merge inside a cluster, without scratch
+};
+Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv);
+size_t kv4_attention_scratch_bytes(const Kv4Plan& plan, int B, int a, int H, int hd);
+cudaError_t launch_kv4_attention(const Launch& L, const Kv4Plan& plan, const void* q, size_t ldq, const Kv4& c, void* o, float* lse,
+                                 int a, int n, int H, const int32_t* lens, float* scratch);
+bool plan_kv4_weights(int a, int H, int Hkv);   // whether they take the tcgen05 kernel
+size_t kv4_weights_scratch_bytes(bool umma, int B, int a, int H, int Hkv);
+cudaError_t launch_kv4_weights(const Launch& L, bool umma, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
+                               int a, int n, int H, const int32_t* lens, void* scratch);
 // kv4_umma.cu
 cudaError_t launch_kv4_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n, int H,
                             const int32_t* lens, float* o_part, float2* ml_part, int S);
 cudaError_t set_wait_limit_kv4_umma(unsigned long long ns);
-size_t kv4_weights_scratch_bytes(int B, int a, int H, int Hkv);
-cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
-                               int a, int n, int H, const int32_t* lens, void* scratch);
 // kv4_weights.cu
 size_t kv4_weights_umma_scratch_bytes(int B, int a, int H, int Hkv);
 cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,

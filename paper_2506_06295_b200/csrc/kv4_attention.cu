@@ -10,6 +10,7 @@
 // The order of the contraction's elements is free, which lets a thread's share of K be sixteen consecutive bytes of a key
 // and lets ldmatrix.trans bring pairs of keys together for V.
 #include <algorithm>
+#include <atomic>
 
 #include "kv4.cuh"
 #include "tma.cuh"
@@ -583,63 +584,16 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
   }
 }
 
-// Which kernel, and how many ranges the keys are cut into, by what they take (us, B200):
-//   few rows   16 rows a CTA, two CTAs to an SM: 4.5 at its ends, and for a tile of 64 keys of each of its four warps 1.5, 2.1
-//              beside a second CTA; 4.5 more where ranges are merged, by a cluster of up to eight as by a launch (which a call's
-//              host side and scratch make the dearer one)
-//   tcgen05    256 rows a CTA, one to an SM: 12 at its ends, 2.3 for a tile of 128 keys, 5 for a merge and its bytes
-// Measured / by this, few rows then tcgen05, each in its best number of ranges:  64 x 768 x 32 heads 8.7 / 9, 17 / 18;
-// 128 x 768 x 32 12.7 / 10.8, 17.8 / 18;  256 x 768 x 32 23 / 22, 24.7 / 26;  512 x 1024 x 32 47 / 52, 33 / 30;  128 x 512 x 28 on 4
-// 10.1 / 8.7, 21 / 21;  100 x 16384 x 8 48 / 43, 32 / 36;  16 sequences of 80 x 1536 x 32 158 / 154, 132 / 158;  8 of 16 x 32768 x
-// 28 on 4 270 / 273, 155 / 164.
-struct Kv4Plan {
-  bool umma = false;
-  int S = 1;
-  bool clustered = false;   // the splits merge inside a cluster, without scratch
-};
-int g_kernel = 0, g_splits = 0;   // dllm_debug_kv4_plan
-
-Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
-  const long rows = (long)a * (H / Hkv), heads = (long)Hkv * B, tiles = (n + KV4_KEYS - 1) / KV4_KEYS, sms = sm_count();
-  Kv4Plan p;
-  double best = -1.0;
-  const long few = (rows + KA_ROWS - 1) / KA_ROWS * heads;
-  for (int S = 1; S <= 64 && S <= tiles && (long)S * B <= 65535 && g_kernel != 2; ++S) {
-    if (S > 1 && S < KA_CLUSTER && (S & (S - 1))) continue;   // clusters of a power of two
-    const long per_warp = ((tiles + S - 1) / S + 3) / 4, waves = (few * S + 2 * sms - 1) / (2 * sms);
-    const double us = (double)waves * (4.5 + (few * S > sms ? 2.1 : 1.5) * (double)per_warp) + (S > 1 ? 4.5 : 0.0);
-    if (best < 0.0 || us < best) {
-      best = us;
-      p.S = S;
-    }
-  }
-  const long many = (rows + 255) / 256 * heads, wide = (tiles + 1) / 2;
-  for (int S = 1; (rows > KA_ROWS || g_kernel == 2) && g_kernel != 1 && S <= 64 && S <= wide && (long)S * B <= 65535; ++S) {
-    const long waves = (many * S + sms - 1) / sms;
-    const double us = (double)waves * (12.0 + 2.3 * (double)((wide + S - 1) / S)) + (S > 1 ? 5.0 + S * (double)B * a * H * 1040.0 / 10.0e6 : 0.0);
-    if (best < 0.0 || us < best) {
-      best = us;
-      p.S = S;
-      p.umma = true;
-    }
-  }
-  if (g_splits > 0) p.S = (int)std::min<long>(g_splits, p.umma ? wide : tiles);
-  p.clustered = !p.umma && p.S > 1 && p.S <= KA_CLUSTER && !(p.S & (p.S - 1));
-  return p;
-}
-
 template <int HD>
-cudaError_t attention_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, const Kv4& c, __nv_bfloat16* o, float* lse, int a,
-                         int n, int H, const int32_t* lens, float* scratch, size_t scratch_floats) {
+cudaError_t attention_as(const Launch& L, const Kv4Plan& plan, const __nv_bfloat16* q, size_t ldq, const Kv4& c, __nv_bfloat16* o,
+                         float* lse, int a, int n, int H, const int32_t* lens, float* scratch) {
   static DeviceOnce once;
   cudaError_t e = once.run([] {
     return cudaFuncSetAttribute(kv4_attn_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KaSmem<HD>::TOTAL);
   });
   if (e != cudaSuccess) return e;
-  const size_t total = (size_t)c.B * a * H, part = total * (HD + 2);
-  const Kv4Plan plan = plan_kv4(c.B, a, n, H, c.Hkv);
-  int S = plan.S;
-  if (S > 1 && !plan.clustered) S = std::max(1, (int)std::min<size_t>(S, scratch ? scratch_floats / part : 0));
+  const size_t total = (size_t)c.B * a * H;
+  const int S = plan.S;
   float* const o_part = scratch;
   float2* const ml_part = reinterpret_cast<float2*>(scratch + (S > 1 && !plan.clustered ? (size_t)S * total * HD : 0));
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)HD);
@@ -662,36 +616,74 @@ cudaError_t attention_as(const Launch& L, const __nv_bfloat16* q, size_t ldq, co
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
+std::atomic<int> g_plan_hook{0};   // dllm_debug_kv4_plan: kernel + 4 * splits
+
 }  // namespace
 
-size_t kv4_attention_scratch_floats(int B, int a, int n, int H, int Hkv, int hd) {
-  const Kv4Plan plan = plan_kv4(B, a, n, H, Hkv);
-  const int S = plan.S;
-  return S > 1 && !plan.clustered ? (size_t)S * B * a * H * (hd + 2) : 0;
+// Which kernel, and how many ranges the keys are cut into, by what they take (us, B200):
+//   few rows   16 rows a CTA, two CTAs to an SM: 4.5 at its ends, and for a tile of 64 keys of each of its four warps 1.5, 2.1
+//              beside a second CTA; 4.5 more where ranges are merged, by a cluster of up to eight as by a launch (which a call's
+//              host side and scratch make the dearer one)
+//   tcgen05    256 rows a CTA, one to an SM: 12 at its ends, 2.3 for a tile of 128 keys, 5 for a merge and its bytes
+// Measured / by this, few rows then tcgen05, each in its best number of ranges:  64 x 768 x 32 heads 8.7 / 9, 17 / 18;
+// 128 x 768 x 32 12.7 / 10.8, 17.8 / 18;  256 x 768 x 32 23 / 22, 24.7 / 26;  512 x 1024 x 32 47 / 52, 33 / 30;  128 x 512 x 28 on 4
+// 10.1 / 8.7, 21 / 21;  100 x 16384 x 8 48 / 43, 32 / 36;  16 sequences of 80 x 1536 x 32 158 / 154, 132 / 158;  8 of 16 x 32768 x
+// 28 on 4 270 / 273, 155 / 164.
+Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
+  const int hook = g_plan_hook.load(std::memory_order_relaxed), kernel = hook & 3, splits = hook >> 2;
+  const long rows = (long)a * (H / Hkv), heads = (long)Hkv * B, tiles = (n + KV4_KEYS - 1) / KV4_KEYS, sms = sm_count();
+  Kv4Plan p;
+  double best = -1.0;
+  const long few = (rows + KA_ROWS - 1) / KA_ROWS * heads;
+  for (int S = 1; S <= 64 && S <= tiles && (long)S * B <= 65535 && kernel != 2; ++S) {
+    if (S > 1 && S < KA_CLUSTER && (S & (S - 1))) continue;   // clusters of a power of two
+    const long per_warp = ((tiles + S - 1) / S + 3) / 4, waves = (few * S + 2 * sms - 1) / (2 * sms);
+    const double us = (double)waves * (4.5 + (few * S > sms ? 2.1 : 1.5) * (double)per_warp) + (S > 1 ? 4.5 : 0.0);
+    if (best < 0.0 || us < best) {
+      best = us;
+      p.S = S;
+    }
+  }
+  const long many = (rows + 255) / 256 * heads, wide = (tiles + 1) / 2;
+  for (int S = 1; (rows > KA_ROWS || kernel == 2) && kernel != 1 && S <= 64 && S <= wide && (long)S * B <= 65535; ++S) {
+    const long waves = (many * S + sms - 1) / sms;
+    const double us = (double)waves * (12.0 + 2.3 * (double)((wide + S - 1) / S)) + (S > 1 ? 5.0 + S * (double)B * a * H * 1040.0 / 10.0e6 : 0.0);
+    if (best < 0.0 || us < best) {
+      best = us;
+      p.S = S;
+      p.umma = true;
+    }
+  }
+  if (splits > 0) p.S = (int)std::max(1L, std::min({(long)splits, p.umma ? wide : tiles, 65535L / B}));
+  p.clustered = !p.umma && p.S > 1 && p.S <= KA_CLUSTER && !(p.S & (p.S - 1));
+  return p;
 }
 
-cudaError_t launch_kv4_attention(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n,
-                                 int H, const int32_t* lens, float* scratch, size_t scratch_floats) {
+size_t kv4_attention_scratch_bytes(const Kv4Plan& plan, int B, int a, int H, int hd) {
+  return plan.S > 1 && !plan.clustered ? (size_t)plan.S * B * a * H * (hd + 2) * sizeof(float) : 0;
+}
+
+cudaError_t launch_kv4_attention(const Launch& L, const Kv4Plan& plan, const void* q, size_t ldq, const Kv4& c, void* o, float* lse,
+                                 int a, int n, int H, const int32_t* lens, float* scratch) {
   auto* const qb = (const __nv_bfloat16*)q;
   auto* const ob = (__nv_bfloat16*)o;
-  return c.hd == 64 ? attention_as<64>(L, qb, ldq, c, ob, lse, a, n, H, lens, scratch, scratch_floats)
-                    : attention_as<128>(L, qb, ldq, c, ob, lse, a, n, H, lens, scratch, scratch_floats);
+  return c.hd == 64 ? attention_as<64>(L, plan, qb, ldq, c, ob, lse, a, n, H, lens, scratch)
+                    : attention_as<128>(L, plan, qb, ldq, c, ob, lse, a, n, H, lens, scratch);
 }
 
-void set_kv4_plan(int kernel, int splits) {
-  g_kernel = kernel;
-  g_splits = splits;
+void set_kv4_plan(int kernel, int splits) { g_plan_hook.store(kernel + 4 * splits, std::memory_order_relaxed); }
+
+bool plan_kv4_weights(int a, int H, int Hkv) {
+  return (g_plan_hook.load(std::memory_order_relaxed) & 3) == 2 || (long)a * (H / Hkv) > KV4_WEIGHTS_ROWS;
 }
 
-static bool weights_on_umma(int a, int H, int Hkv) { return g_kernel == 2 || (long)a * (H / Hkv) > KV4_WEIGHTS_ROWS; }
-
-size_t kv4_weights_scratch_bytes(int B, int a, int H, int Hkv) {
-  return weights_on_umma(a, H, Hkv) ? kv4_weights_umma_scratch_bytes(B, a, H, Hkv) : 0;
+size_t kv4_weights_scratch_bytes(bool umma, int B, int a, int H, int Hkv) {
+  return umma ? kv4_weights_umma_scratch_bytes(B, a, H, Hkv) : 0;
 }
 
-cudaError_t launch_kv4_weights(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
+cudaError_t launch_kv4_weights(const Launch& L, bool umma, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                int a, int n, int H, const int32_t* lens, void* scratch) {
-  if (weights_on_umma(a, H, c.Hkv)) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens, scratch);
+  if (umma) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens, scratch);
   // three CTAs to an SM, each over its share of the keys
   const long blocks = (n + KW_KEYS - 1) / KW_KEYS, heads = (long)c.Hkv * c.B;
   const dim3 grid((unsigned)std::max(1L, std::min(blocks, (3L * sm_count() + heads - 1) / heads)), c.Hkv, c.B);

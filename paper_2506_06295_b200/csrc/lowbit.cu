@@ -172,7 +172,7 @@ size_t dllm_attention_kv4_scratch_bytes(int B, int a, int n, int n_heads, int n_
   if (B <= 0 || a <= 0 || n <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || (head_dim != 64 && head_dim != 128) ||
       (long)a * n_heads > (1L << 30) / B)
     return 0;
-  return kv4_attention_scratch_floats(B, a, n, n_heads, n_kv_heads, head_dim) * 4;
+  return kv4_attention_scratch_bytes(plan_kv4(B, a, n, n_heads, n_kv_heads), B, a, n_heads, head_dim);
 }
 
 dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, void* d_o, float* d_lse, int a, int n,
@@ -181,17 +181,17 @@ dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache
   TRY(check_cache(cache, &c));
   TRY(check_queries(d_q, ldq, c, a, n, n_heads));
   if (!d_o || !aligned16(d_o)) return fail(DLLM_INVALID_ARG, "the output must be 16-byte aligned");
-  const size_t need = dllm_attention_kv4_scratch_bytes(c.B, a, n, n_heads, c.Hkv, c.hd);
+  const Kv4Plan plan = plan_kv4(c.B, a, n, n_heads, c.Hkv);
+  const size_t need = kv4_attention_scratch_bytes(plan, c.B, a, n_heads, c.hd);
   if (need && (!d_scratch || !aligned16(d_scratch) || scratch_bytes < need))
     return fail(DLLM_INVALID_ARG, "this attention needs %zu bytes of 16-byte aligned scratch", need);
-  return done(launch_kv4_attention(on(stream), d_q, ldq, c, d_o, d_lse, a, n, n_heads, d_lens, (float*)d_scratch,
-                                   scratch_bytes / 4),
+  return done(launch_kv4_attention(on(stream), plan, d_q, ldq, c, d_o, d_lse, a, n, n_heads, d_lens, (float*)d_scratch),
               "attention over the 4-bit cache");
 }
 
 size_t dllm_attention_weights_kv4_scratch_bytes(int B, int a, int n_heads, int n_kv_heads) {
   if (B <= 0 || a <= 0 || n_heads <= 0 || n_kv_heads <= 0 || n_heads % n_kv_heads || (long)a * n_heads > (1L << 30) / B) return 0;
-  return kv4_weights_scratch_bytes(B, a, n_heads, n_kv_heads);
+  return kv4_weights_scratch_bytes(plan_kv4_weights(a, n_heads, n_kv_heads), B, a, n_heads, n_kv_heads);
 }
 
 dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, const float* d_lse,
@@ -201,10 +201,11 @@ dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_k
   TRY(check_cache(cache, &c));
   TRY(check_queries(d_q, ldq, c, a, n, n_heads));
   if (!d_lse || !d_weight) return fail(DLLM_INVALID_ARG, "lse or weight is NULL");
-  const size_t need = kv4_weights_scratch_bytes(c.B, a, n_heads, c.Hkv);
+  const bool umma = plan_kv4_weights(a, n_heads, c.Hkv);
+  const size_t need = kv4_weights_scratch_bytes(umma, c.B, a, n_heads, c.Hkv);
   if (need && (!d_scratch || !aligned16(d_scratch) || scratch_bytes < need))
     return fail(DLLM_INVALID_ARG, "these weights need %zu bytes of 16-byte aligned scratch", need);
-  return done(launch_kv4_weights(on(stream), d_q, ldq, c, d_lse, d_weight, a, n, n_heads, d_lens, d_scratch), "attention weights");
+  return done(launch_kv4_weights(on(stream), umma, d_q, ldq, c, d_lse, d_weight, a, n, n_heads, d_lens, d_scratch), "attention weights");
 }
 
 dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, int n, int keep, int first, int last,
