@@ -213,14 +213,15 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
       }
     }
     __syncwarp();
-    // scores in log2 units; their maxima (two keys of a row per instruction)
+    // scores in log2 units; their maxima (two keys of a row per instruction).  The row's scale comes
+    // ahead of the step: huge steps under tiny queries then stay within fp32's range.
     float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
     for (int nt = 0; nt < 8; ++nt) {
       const float4 k = par[2 * (nt * 4 + t)];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float2 x = fma2(mul2(make_float2(s[nt][2 * h], s[nt][2 * h + 1]), make_float2(k.x, k.y)), make_float2(alpha[h], alpha[h]),
+        const float2 x = fma2(mul2(make_float2(s[nt][2 * h], s[nt][2 * h + 1]), make_float2(alpha[h], alpha[h])), make_float2(k.x, k.y),
                               mul2(make_float2(k.z, k.w), make_float2(beta[h], beta[h])));
         s[nt][2 * h] = x.x;
         s[nt][2 * h + 1] = x.y;
@@ -572,7 +573,7 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
         const float4 p = par[nt * 8 + 2 * t + e];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          got[i] += exp2_fast(fmaf(s[i >> 1][2 * (i & 1) + e] * step[i], p.x, fmaf(off[i], p.y, -p.z)));
+          got[i] += exp2_fast(fmaf(s[i >> 1][2 * (i & 1) + e] * p.x, step[i], fmaf(off[i], p.y, -p.z)));
       }
     }
 #pragma unroll

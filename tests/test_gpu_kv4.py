@@ -229,6 +229,23 @@ def test_attention_of_very_large_and_very_small_numbers(dllm, plan, a, qs, cs):
     check_attention(q, cache, a, 311, 2, None, o, lse)
 
 
+@pytest.mark.parametrize("a", [4, 100])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_huge_keys_under_tiny_queries(dllm, plan, a, hd):
+    """Steps of 4 * 10^33 times a product of codes and scaled queries, some 2^18, leave fp32's range; the scores (some tens) do not."""
+    g = gen(19)
+    cache, ordinary = ref.random_cache(dllm, g, 1, 2, 320, hd, scale=2e34), ref.random_cache(dllm, g, 1, 2, 320, hd)
+    cache.v_params.copy_(ordinary.v_params)
+    q = queries(g, 1, a, 2, hd, scale=2e-33)
+    o, lse = dllm.attention_kv4(q, cache, a, 311, 2)
+    check_attention(q, cache, a, 311, 2, None, o, lse)
+    w = torch.zeros((1, 2, 320), device="cuda")
+    dllm.attention_weights_kv4(q, cache, lse, w, a, 311, 2)
+    want, err = ref.weights(q, cache, lse, a, 311, 2)
+    # an exponential below fp32's smallest normal number is 0: at most that much per row
+    assert bool(((w.double() - want).abs() <= err + 2.0 ** -23 * want + a * 2.0 ** -126).all())
+
+
 def offset_cache(dllm, g, B, Hkv, cap, hd):
     """Keys and values whose offsets are some sixty steps: what a score then is made of is the offset times the query's sum."""
     cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
