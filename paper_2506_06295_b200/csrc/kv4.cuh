@@ -53,6 +53,11 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)
 __device__ __forceinline__ float kv4_step(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float kv4_lo(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 
+// Unnormalised outputs, which are sums over up to 2^24 keys, are kept times 2^-24: a mean of numbers near the end of fp32's range
+// then stays within it on its way.  (Values below 2^-102 lose bits by it: what a key adds is off by 2^-126 of its weight, fp32's
+// smallest normal number.)
+constexpr float KV4_SUM_DOWN = 1.f / 16777216.f, KV4_SUM_UP = 16777216.f;
+
 // What the host hands to the kernels.
 struct Kv4 {
   uint8_t* k = nullptr;      // codes [B, Hkv, cap, hd / 2]

@@ -187,8 +187,8 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
     float4* const par = reinterpret_cast<float4*>(ring_g + SM::PAR);
     par[2 * lane] = make_float4(kv4_step(kp.x), kv4_step(kp.y), fmaf(8.f, kv4_step(kp.x), kv4_lo(kp.x)),
                                 fmaf(8.f, kv4_step(kp.y), kv4_lo(kp.y)));
-    par[2 * lane + 1] = make_float4(kv4_step(vp.x) * up, kv4_step(vp.y) * up, fmaf(8.f, kv4_step(vp.x), kv4_lo(vp.x)),
-                                    fmaf(8.f, kv4_step(vp.y), kv4_lo(vp.y)));
+    par[2 * lane + 1] = make_float4(kv4_step(vp.x) * up, kv4_step(vp.y) * up, fmaf(8.f, kv4_step(vp.x), kv4_lo(vp.x)) * KV4_SUM_DOWN,
+                                    fmaf(8.f, kv4_step(vp.y), kv4_lo(vp.y)) * KV4_SUM_DOWN);
 
     float s[8][4];
 #pragma unroll
@@ -305,9 +305,9 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
 
-  // ---- the warps' rows, unnormalised, one after the other in shared memory
+  // ---- the warps' rows, unnormalised (times KV4_SUM_DOWN), one after the other in shared memory
   float* const xo = reinterpret_cast<float*>(smem + warp * SM::WARP);
-  const float down = kv4_down(v_ex);
+  const float down = kv4_down(v_ex) * KV4_SUM_DOWN;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float lh = l[h].x + l[h].y, zh = z[h].x + z[h].y;
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
         l2 = fmaf(f, ml[k].y, l2);
         y.x = fmaf(f, x[k].x, y.x); y.y = fmaf(f, x[k].y, y.y); y.z = fmaf(f, x[k].z, y.z); y.w = fmaf(f, x[k].w, y.w);
       }
-      const float inv = l2 == 0.f ? 0.f : 1.f / l2;
+      const float inv = l2 == 0.f ? 0.f : KV4_SUM_UP / l2;
       const int i2 = vr2 / G;
       const size_t orow = ((size_t)b * a + i2) * H + kh * G + (vr2 - i2 * G);
       const __nv_bfloat162 lo = __floats2bfloat162_rn(y.x * inv, y.y * inv), hi = __floats2bfloat162_rn(y.z * inv, y.w * inv);
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
       *reinterpret_cast<float4*>(o_part + at * HD + col + e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
     return;
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row without keys: zeros
+  const float inv = sum == 0.f ? 0.f : KV4_SUM_UP / sum;   // a row without keys: zeros
 #pragma unroll
   for (int e = 0; e < PER; e += 8) {
     float v[8];
@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const float* __restric
         for (int e = 0; e < PER; ++e) out[e] = fmaf(f, x[k][e], out[e]);
     }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = sum == 0.f ? 0.f : KV4_SUM_UP / sum;
   __nv_bfloat16* dst = o + row * HD + lane * PER;
 #pragma unroll
   for (int e = 0; e < PER; e += 2)

@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
       if (ok) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const float l = (l2.x + l2.y) * pow2(-UK_P_BITS), down = pow2(top[1] - 140 - UK_P_BITS);
-        const float f = S > 1 ? down : l == 0.f ? 0.f : down / l;
+        const float f = S > 1 ? down * KV4_SUM_DOWN : l == 0.f ? 0.f : down / l;
         const size_t orow = ((size_t)b * a + qi) * H + kh * G + g;
 #pragma unroll
         for (int cc = 0; cc < HD; cc += 32) {

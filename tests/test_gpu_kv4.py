@@ -246,6 +246,21 @@ def test_huge_keys_under_tiny_queries(dllm, plan, a, hd):
     assert bool(((w.double() - want).abs() <= err + 2.0 ** -23 * want + a * 2.0 ** -126).all())
 
 
+@pytest.mark.parametrize("a", [4, 100])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_values_near_the_largest_number(dllm, plan, a, hd):
+    """Values of some 10^37 under hundreds of keys of like weight: their sums leave fp32's range, their mean does not."""
+    g = gen(20)
+    cache, huge = ref.random_cache(dllm, g, 1, 2, 1280, hd), ref.random_cache(dllm, g, 1, 2, 1280, hd, scale=2e37)
+    huge.v_params[..., 1] = -2.5 * huge.v_params[..., 0]          # 0 .. 15 steps of up to 7e36 from -2.5 of them on
+    cache.v_params.copy_(huge.v_params)
+    assert bool(torch.isfinite(cache.v_params[..., 1].float() + 15 * cache.v_params[..., 0].float()).all())
+    q = queries(g, 1, a, 2, hd, scale=0.1)
+    o, lse = dllm.attention_kv4(q, cache, a, 1271, 2)
+    assert float(ref.attention(q, cache, a, 1271, 2)[0].abs().max()) > 1e37
+    check_attention(q, cache, a, 1271, 2, None, o, lse)
+
+
 def offset_cache(dllm, g, B, Hkv, cap, hd):
     """Keys and values whose offsets are some sixty steps: what a score then is made of is the offset times the query's sum."""
     cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
