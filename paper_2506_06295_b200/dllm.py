@@ -577,6 +577,8 @@ class _Placed:
 
     def __init__(self, stream, *inputs):
         import torch
+        if stream is not None and stream.device != inputs[0].device:
+            _refuse(f"a stream of {stream.device} for tensors on {inputs[0].device}")
         self.device = torch.cuda.device(inputs[0].device)
         self.stream = torch.cuda.stream(stream)
         self.inputs = inputs if stream is not None else ()

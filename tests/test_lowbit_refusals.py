@@ -139,3 +139,20 @@ def test_binding_refuses_what_the_library_cannot_see(dllm):
         dllm._row_pitch(torch.zeros(2, 4, 8)[:, :3], 8, "x")
     assert dllm._row_pitch(torch.zeros(2, 3, 24)[:, :, 8:16], 8, "x") == 24
     assert dllm._row_pitch(torch.zeros(1, 1, 24)[:, :, 8:16], 8, "x") == 16
+
+
+def test_binding_refuses_a_stream_of_another_device(dllm):
+    """Which would otherwise be left aside for the current one of the tensors' device."""
+    import types
+
+    import torch
+    on = lambda i, **more: types.SimpleNamespace(device=torch.device("cuda", i), is_cuda=True, get_device=lambda: i, **more)  # noqa: E731
+    x, stream = on(0), on(1)
+    cache = types.SimpleNamespace(_base=x, tensors=lambda: (x, x, x, x))
+    for call in (lambda: dllm.quantize_rows_s8(x, stream=stream), lambda: dllm.gemm_s8(x, x, x, x, stream=stream),
+                 lambda: dllm.linear_s8(x, x, x, stream=stream), lambda: dllm.kv4_store(cache, x, x, stream=stream),
+                 lambda: dllm.kv4_load(cache, 1, stream=stream), lambda: dllm.attention_kv4(x, cache, 1, 1, 1, stream=stream),
+                 lambda: dllm.attention_weights_kv4(x, cache, x, x, 1, 1, 1, stream=stream),
+                 lambda: dllm.kv4_evict(cache, x, 1, 1, stream=stream)):
+        with pytest.raises(dllm.DllmError, match="stream of cuda:1"):
+            call()
