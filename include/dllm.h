@@ -317,7 +317,8 @@ dllm_status dllm_kernel_status(void* stream);
  * its pipeline stages never completes, its waits run into the limit, the CTA
  * records the status code, skips its epilogue, frees its tensor memory and
  * returns normally; one CTA of every launch of the one-CTA kernel of the 8-bit
- * products and of the 4-bit cache's tcgen05 weights leaves out a copy likewise.
+ * products and of the 4-bit cache's tcgen05 weights leaves out a copy likewise,
+ * one of its tcgen05 attention waits for what never comes.
  * (0) switches that off.  Both calls synchronise the device. */
 dllm_status dllm_debug_set_wait_limit_ns(uint64_t ns);
 /* Tuning / test hook: kernel choice of the bf16 projections, for every later

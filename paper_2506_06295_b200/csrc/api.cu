@@ -1367,6 +1367,7 @@ dllm_status dllm_debug_skip_one_load(int enable) {
   CU_TRY(nullptr, cudaDeviceSynchronize());
   CU_TRY(nullptr, set_debug_skip_act_load(enable));
   CU_TRY(nullptr, set_debug_skip_gemm_s8(enable));
+  CU_TRY(nullptr, set_debug_skip_kv4_umma(enable));
   CU_TRY(nullptr, set_debug_skip_kv4_weights(enable));
   CU_TRY(nullptr, cudaDeviceSynchronize());
   return DLLM_OK;

@@ -93,6 +93,7 @@ cudaError_t launch_kv4_weights(const Launch& L, bool umma, const void* q, size_t
 cudaError_t launch_kv4_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, void* o, float* lse, int a, int n, int H,
                             const int32_t* lens, float* o_part, float2* ml_part, int S);
 cudaError_t set_wait_limit_kv4_umma(unsigned long long ns);
+cudaError_t set_debug_skip_kv4_umma(int enable);   // dllm_debug_skip_one_load
 // kv4_weights.cu
 size_t kv4_weights_umma_scratch_bytes(int B, int a, int H, int Hkv);
 cudaError_t launch_kv4_weights_umma(const Launch& L, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,

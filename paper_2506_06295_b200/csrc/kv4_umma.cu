@@ -28,6 +28,10 @@ namespace dllm {
 
 namespace {
 
+// Test hook (dllm_debug_skip_one_load): while non-zero, the issuer of CTA (0, 0, 0) waits for products that it has not issued
+// instead of for Q, so that the CTA's waits run into their limit.
+static __device__ int g_debug_skip = 0;
+
 constexpr int UK_ROWS = 128, UK_KEYS = 2 * KV4_KEYS, UK_STAGES = 2, UK_THREADS = 16 * 32, UK_MMA_WARP = 8, UK_K_WARP = 9, UK_V_WARP = 12;
 constexpr int UK_P_BITS = 10;   // P = p * 2^10: fp16's small numbers are further away
 
@@ -269,7 +273,8 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
       }
       __syncwarp();
     };
-    ok = mbar_wait_warp(smem_u32(&q_bar), 0u, abortp);
+    const bool skip = g_debug_skip != 0 && (blockIdx.x | blockIdx.y | blockIdx.z) == 0;   // (Q takes longer than this read)
+    ok = mbar_wait_warp(smem_u32(skip ? &o_full[0] : &q_bar), 0u, abortp);
     if (ok) ok = ready(0);
     for (int i = 0; i < live && ok; ++i) issue_s(i, 0);
     for (int t = 0; t < n_tiles && ok; ++t) {
@@ -484,6 +489,13 @@ cudaError_t launch_kv4_umma(const Launch& L, const void* q, size_t ldq, const Kv
                     : umma_as<128>(L, (const __nv_bfloat16*)q, ldq, c, (__nv_bfloat16*)o, lse, a, n, H, lens, o_part, ml_part, S);
 }
 
+}  // namespace dllm
+
+namespace dllm {
+cudaError_t set_debug_skip_kv4_umma(int enable) {
+  const int v = enable != 0;
+  return cudaMemcpyToSymbol(g_debug_skip, &v, sizeof v);
+}
 }  // namespace dllm
 
 DLLM_WAIT_LIMIT_HOOK(kv4_umma)

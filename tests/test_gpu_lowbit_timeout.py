@@ -86,3 +86,35 @@ def test_a_tile_of_a_product_is_written_whole_or_not_at_all(dllm, M, N, K, out):
     assert dllm.gemm_s8(A, sa, W, sw, out=y) is y
     dllm.kernel_status()
     assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_attention_of_many_rows_gives_up_and_goes_on(dllm, hd, splits):
+    """300 rows of two heads over 700 keys: the CTA of the first 256 rows of the first head (and of the first range of keys, where
+    there are several) gives up.  Its rows stay as they were (with one range); all others are right."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(hd + splits)
+    a, n, H = 300, 700, 2
+    cache = ref.random_cache(dllm, g, 1, H, 704, hd)
+    q = torch.randn((a, H * hd), generator=g, device="cuda").bfloat16()
+    dllm.debug_kv4_plan(2, splits)
+    try:
+        want, want_lse = dllm.attention_kv4(q, cache, a, n, H)
+        o, lse = torch.full_like(want, -77.0), torch.full_like(want_lse, -77.0)
+        need = dllm.lib.dllm_attention_kv4_scratch_bytes(1, a, n, H, H, hd)
+        assert (need > 0) == (splits > 1)
+        scratch = torch.zeros(max(need, 16), dtype=torch.uint8, device="cuda")
+        run_out(dllm, lambda: dllm._check(dllm.lib.dllm_attention_kv4(
+            q.data_ptr(), H * hd, cache.ref, o.data_ptr(), lse.data_ptr(), a, n, H, None, scratch.data_ptr(), need,
+            torch.cuda.current_stream().cuda_stream)))
+        lost = torch.zeros((a, H), dtype=torch.bool, device="cuda")
+        lost[:256, 0] = True
+        if splits == 1:
+            assert bool((o.reshape(a, H, hd)[lost] == -77.0).all()) and bool((lse[lost] == -77.0).all())
+        assert torch.equal(o.reshape(a, H, hd)[~lost], want.reshape(a, H, hd)[~lost]) and torch.equal(lse[~lost], want_lse[~lost])
+        o, lse = dllm.attention_kv4(q, cache, a, n, H, scratch=scratch if need else None)
+        assert torch.equal(o, want) and torch.equal(lse, want_lse)
+        dllm.kernel_status()
+    finally:
+        dllm.debug_kv4_plan()
