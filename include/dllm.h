@@ -519,8 +519,9 @@ dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_k
  * the length is at most keep all stay.  Their K, V and weight (-0 as 0) go to rows 0, 1, .. of
  * `to` and d_to_weight (float [B, n_kv_heads, to->capacity], zeros behind them),
  * d_index (int32 [B, n_kv_heads, keep]) says where each came from (-1 behind them) and
- * d_to_lens (int32 [B]) how many stayed.  first + last <= keep <= to->capacity; nothing
- * that is written may overlap what is read.  Positions are in K already (it is cached rotated), so
+ * d_to_lens (int32 [B]) how many stayed.  first + last <= keep <= to->capacity; d_weight
+ * 16-byte aligned; nothing that is written may overlap what is read or what else is
+ * written.  Positions are in K already (it is cached rotated), so
  * attention over `to` needs nothing but the new lengths. */
 dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, int n, int keep, int first, int last,
                            const int32_t* d_lens, const dllm_kv4_cache* to, float* d_to_weight, int32_t* d_index,

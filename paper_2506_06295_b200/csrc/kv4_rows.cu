@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(256) kv4_gather_kernel(Kv4 src, Kv4 dst, const
   const int bh = blockIdx.y, unit = blockIdx.x * 256 + threadIdx.x, slot = unit / PER, part = unit % PER;
   if (slot >= keep) return;
   const int j = index[(size_t)bh * keep + slot];
-  if (j < 0) return;
+  if ((uint32_t)j >= (uint32_t)src.cap) return;   // -1: no row
   const size_t from = (size_t)bh * src.cap + j, to = (size_t)bh * dst.cap + slot;
   const bool of_v = part >= CH;
   const int c = of_v ? part - CH : part;

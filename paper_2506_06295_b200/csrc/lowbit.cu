@@ -226,9 +226,13 @@ dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, in
   const Span out[7] = {{(const char*)d.k, dr * d.hd / 2}, {(const char*)d.v, dr * d.hd / 2}, {(const char*)d.kp, dr * 4},
                        {(const char*)d.vp, dr * 4}, {(const char*)d_to_weight, dr * 4},
                        {(const char*)d_index, (size_t)d.B * d.Hkv * keep * 4}, {(const char*)d_to_lens, (size_t)d.B * 4}};
-  for (const Span& x : in)
-    for (const Span& y : out)
-      if (x.n && x.p < y.p + y.n && y.p < x.p + x.n) return fail(DLLM_INVALID_ARG, "eviction: what is written overlaps what is read");
+  auto meet = [](const Span& x, const Span& y) { return x.n && y.n && x.p < y.p + y.n && y.p < x.p + x.n; };
+  for (const Span& y : out) {
+    for (const Span& x : in)
+      if (meet(x, y)) return fail(DLLM_INVALID_ARG, "eviction: what is written overlaps what is read");
+    for (const Span* z = out; z != &y; ++z)   // (the gather reads the index back: it must hold what the selection wrote)
+      if (meet(*z, y)) return fail(DLLM_INVALID_ARG, "eviction: two of the outputs overlap");
+  }
   return done(launch_kv4_evict(on(stream), s, d_weight, n, keep, first, last, d_lens, d, d_to_weight, d_index, d_to_lens),
               "eviction");
 }

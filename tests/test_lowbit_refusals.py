@@ -120,6 +120,20 @@ def test_evict(dllm):
                 a["nl"], None)
 
 
+def test_evict_into_outputs_that_overlap(dllm):
+    """The index is read back to move the rows: another output over it would send the reads anywhere."""
+    src, far = cache(dllm, cap=256), P + (1 << 30)
+    dst = cache(dllm, cap=64, at=far)
+    good = dict(dw=far + (1 << 28), idx=far + (1 << 29), nl=far + (3 << 28))
+    at = dict(k=far, kp=far + (1 << 24), v=far + (2 << 24), vp=far + (3 << 24))   # of 2 * 4 * 64 rows
+    for bad in (dict(idx=good["dw"]), dict(idx=good["dw"] + 2 * 4 * 64 * 4 - 4), dict(dw=good["idx"] + 2 * 4 * 50 * 4 - 16), dict(nl=good["idx"]),
+                dict(nl=good["dw"] + 16), dict(idx=at["k"]), dict(idx=at["vp"] + 16), dict(dw=at["v"]), dict(nl=at["kp"])):
+        a = {**good, **bad}
+        refused(dllm, "dllm_kv4_evict", src, P + (1 << 28), 200, 50, 3, 5, None, dst, a["dw"], a["idx"], a["nl"], None)
+        assert "outputs overlap" in dllm.last_error()
+    refused(dllm, "dllm_kv4_evict", src, P + (1 << 28), 200, 50, 3, 5, None, cache(dllm, cap=64, at=far, v_params=at["k"]), *good.values(), None)
+
+
 def test_binding_refuses_what_the_library_cannot_see(dllm):
     import torch
     with pytest.raises(dllm.DllmError):        # no CUDA tensors
