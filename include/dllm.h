@@ -505,7 +505,7 @@ dllm_status dllm_debug_kv4_plan(int kernel, int splits);
  * capacity]) += the sum over the a queries and the query heads of KV head h of
  * exp(q . k_j / sqrt(head_dim) - lse), for j below the sequence's length; the other
  * weights stay as they are.  d_lse as dllm_attention_kv4 leaves it; a row whose lse is
- * -infinity gives nothing.  Sums are taken in a fixed order, and a key's is added whole or, where a
+ * -infinity gives nothing, whatever it holds (to keys that are numbers).  Sums are taken in a fixed order, and a key's is added whole or, where a
  * wait of the call gave up (DLLM_TIMEOUT), not at all.  d_scratch: as many bytes as
  * the query asks for (NULL where that is 0), 16-byte aligned; calls that may overlap on
  * the GPU need one each. */

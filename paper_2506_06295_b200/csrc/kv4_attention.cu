@@ -46,14 +46,19 @@ __device__ __forceinline__ float kv4_down(int ex) { return __uint_as_float((uint
 
 // A lane's share of a row of Q: elements [t * HD / 4, (t + 1) * HD / 4) as fp16 pairs in the order of kv4_word, scaled by
 // kv4_up of the row's largest; the four lanes of a row must call it together.  alpha: what the scaled product has to be
-// multiplied by, beta: the row's sum, both times scale_log2.
+// multiplied by, beta: the row's sum, both times scale_log2.  live: the row may be read; counts: else it is as good as zeros,
+// whatever it holds.
 template <int HD>
-__device__ __forceinline__ void q_share(const __nv_bfloat16* row, bool live, int t, float scale_log2, uint32_t (&w)[HD / 8],
-                                        float& alpha, float& beta) {
+__device__ __forceinline__ void q_share(const __nv_bfloat16* row, bool live, bool counts, int t, float scale_log2,
+                                        uint32_t (&w)[HD / 8], float& alpha, float& beta) {
   uint4 raw[HD / 32];
 #pragma unroll
   for (int i = 0; i < HD / 32; ++i)
     raw[i] = live ? *reinterpret_cast<const uint4*>(row + t * (HD / 4) + i * 8) : make_uint4(0, 0, 0, 0);
+  if (!counts) {
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+  }
   float top = 0.f, sum = 0.f;
 #pragma unroll
   for (int i = 0; i < HD / 32; ++i) {
@@ -151,7 +156,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
   for (int h = 0; h < 2; ++h) {
     const int r = row0 + g + 8 * h, i = r / G;
     uint32_t w[HD / 8];
-    q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + r - i * G) * HD, r < rows, t, scale_log2, w, alpha[h], beta[h]);
+    q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + r - i * G) * HD, r < rows, true, t, scale_log2, w, alpha[h], beta[h]);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       aq[ks][h] = w[2 * ks];
@@ -517,19 +522,14 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
     const int r = pass * 32 + tid / 4, i = r / G, share = tid & 3;
     if (pass * 32 >= rows) break;
     const bool live = r < rows;
+    const float e = live ? lse[((size_t)b * a + i) * H + kh * G + (r - i * G)] : -INFINITY;
     uint32_t x[HD / 8];
     float alpha, beta;
-    q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + r - i * G) * HD, live, share, scale_log2, x, alpha, beta);
+    q_share<HD>(q + ((size_t)b * a + i) * ldq + (size_t)(kh * G + r - i * G) * HD, live, e != -INFINITY, share, scale_log2, x, alpha, beta);
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) qs[u][r][share] = make_uint4(x[4 * u], x[4 * u + 1], x[4 * u + 2], x[4 * u + 3]);
-    if (share == 0) {
-      float y = INFINITY;      // rows past the last one and rows that saw no key give nothing
-      if (live) {
-        const float e = lse[((size_t)b * a + i) * H + kh * G + (r - i * G)];
-        if (e != -INFINITY) y = e * 1.4426950408889634f;
-      }
-      par[r] = make_float4(alpha, beta, y, 0.f);
-    }
+    // rows past the last one and rows that saw no key give nothing
+    if (share == 0) par[r] = make_float4(alpha, beta, e != -INFINITY ? e * 1.4426950408889634f : INFINITY, 0.f);
   }
   __syncthreads();
   for (; key0 - warp * 32 - g < len; key0 += gridDim.x * KW_KEYS) {

@@ -108,7 +108,8 @@ WkTiling wk_tiling(int a, int G) {
 }
 
 // A row's sum and its lse in parts, 32 bytes per row as they lie in shared memory: [B, Hkv, tiles, 128].  Rows that are none and
-// rows that saw no key: so large an lse that nothing is left.  HD / 8 threads per row.
+// rows that saw no key: a sum of zero and so large an lse that nothing is left; the latter have a 1 in the last place, which meets a
+// zero in the product, and tells the issuer to put zeros in the row's place (it may hold anything).  HD / 8 threads per row.
 template <int HD>
 __global__ void __launch_bounds__(256) kv4_row_parts_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq,
                                                             const float* __restrict__ lse, uint4* __restrict__ parts, int B, int a,
@@ -134,14 +135,18 @@ __global__ void __launch_bounds__(256) kv4_row_parts_kernel(const __nv_bfloat16*
   for (int o = CHUNKS / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (ch != 0 || b >= B) return;
   float x = live ? lse[((size_t)b * a + i) * H + kh * G + g] : INFINITY;
-  if (x == -INFINITY) x = INFINITY;
+  const bool saw_none = x == -INFINITY;
+  if (saw_none) {
+    x = INFINITY;
+    sum = 0.f;
+  }
   x = x > 1e30f ? 1e30f : x < -1e30f ? -1e30f : x;   // (a NaN stays one)
   float s[3], l[3];
   parts3(sum, s);
   parts3(-1.4426950408889634f * x, l);
   const size_t turn = (r >> 2) & 1;   // the 32-byte swizzle
   parts[2 * record + turn] = make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[0]), bf16_pair(s[1], s[0]), bf16_pair(l[0], l[1]));
-  parts[2 * record + (turn ^ 1)] = make_uint4(bf16_pair(l[2], l[0]), bf16_pair(l[1], l[0]), 0u, 0u);
+  parts[2 * record + (turn ^ 1)] = make_uint4(bf16_pair(l[2], l[0]), bf16_pair(l[1], l[0]), 0u, saw_none ? 0x3F800000u : 0u);
 }
 
 // A barrier of T threads that says whether all of them came with `x`
@@ -274,12 +279,32 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
   } else if (warp == WK_MMA_WARP) {
     // ---------------- MMA issuer ----------------
     constexpr uint32_t idesc = make_idesc(WK_TILE, WK_ROWS);
+    // Zeros in the place of rows that saw no key
+    auto rows_that_count = [&](uint32_t stage) {
+      uint32_t none[WK_ROWS / 32], any = 0;
+#pragma unroll
+      for (int k = 0; k < WK_ROWS / 32; ++k) {
+        const int r = k * 32 + lane;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(none[k]) : "r"(stage + SM::OPERAND + r * 32 + (16u ^ ((uint32_t)((r >> 2) & 1) << 4)) + 12u) : "memory");
+        any |= none[k];
+      }
+      if (!__any_sync(0xffffffffu, any != 0u)) return;
+#pragma unroll
+      for (int k = 0; k < WK_ROWS / 32; ++k)
+        if (none[k])
+#pragma unroll 1
+          for (int ch = 0; ch < HD / 8; ++ch)
+            put16(stage + (ch >> 3) * (WK_ROWS * 128) + (k * 32 + lane) * 128 + (ch & 7) * 16, make_uint4(0, 0, 0, 0));
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor cores read them
+      __syncwarp();
+    };
     int it = 0, j = 0;
     for (Unit w = first; w.len > 0 && ok; w = next_unit(), ++j) {
       ok = mbar_wait_warp(smem_u32(&k_full[j & 1]), (uint32_t)(j >> 1) & 1u, abortp);
       for (int u = 0; u < n_tiles && ok; ++u, ++it) {
         const int st = it % WK_STAGES, buf = it & 1;
         ok = mbar_wait_warp(smem_u32(&q_full[st]), (uint32_t)(it / WK_STAGES) & 1u, abortp);
+        if (ok) rows_that_count(ring + st * SM::STAGE);
         for (int i = 0; i < 2 && ok; ++i) {
           if (it >= 2) ok = mbar_wait_warp(smem_u32(&d_empty[i][buf]), (uint32_t)(it / 2 - 1) & 1u, abortp);
           if (!ok) break;

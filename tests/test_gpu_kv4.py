@@ -493,6 +493,35 @@ def test_weights(dllm, plan, B, a, n, H, Hkv, hd, lens):
     assert torch.equal(w, again)
 
 
+@pytest.mark.parametrize("B,a,n,H,Hkv,hd,lens", [(1, 3, 65, 4, 4, 128, None), (2, 9, 700, 14, 2, 128, [700, 333]), (1, 60, 513, 2, 2, 64, None),
+                                                 (2, 150, 450, 4, 2, 128, [450, 33]), (1, 300, 40000, 1, 1, 64, None)])
+def test_rows_that_saw_no_key_give_nothing_whatever_they_hold(dllm, plan, B, a, n, H, Hkv, hd, lens):
+    """Rows of a padded batch, left out by an lse of -infinity, hold NaN, infinities or the largest numbers."""
+    g = gen(21 + n)
+    cap = -(-n // 64) * 64
+    cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
+    q, lens = queries(g, B, a, H, hd), lens_of(lens)
+    _, lse = dllm.attention_kv4(q, cache, a, n, H, lens=lens)
+    out = torch.rand((B * a, H), generator=g, device="cuda") < 0.3
+    out[0], out[-1] = True, False
+    if Hkv > 1:
+        out[:, :H // Hkv] = True                      # all rows of the first KV head
+    lse[out] = -math.inf
+    zeros = q.reshape(B * a, H, hd).clone()
+    zeros[out] = 0
+    had = torch.rand((B, Hkv, cap), generator=g, device="cuda")
+    got, err = ref.weights(zeros.reshape(B * a, H * hd), cache, lse, a, n, H, lens)
+    want = had.double() + got
+    for bad in (math.nan, math.inf, -math.inf, 3.3e38, -3.3e38):
+        rows = zeros.clone()
+        rows[out] = bad
+        w = had.clone()
+        dllm.attention_weights_kv4(rows.reshape(B * a, H * hd), cache, lse, w, a, n, H, lens=lens)
+        assert bool(((w.double() - want).abs() <= err + 2.0 ** -23 * want).all())
+        assert Hkv == 1 or torch.equal(w[:, 0], had[:, 0])
+    dllm.kernel_status()
+
+
 def test_exponentials_of_the_weights_alone(dllm):
     """One row per sequence that counts, a query of zeros, over one key: the key gets exp(-lse), by the special-function unit or,
     in rows 6 and 7 of eight, by a polynomial.  x = -lse log2(e), |x| <= 0.73, is off by at most 2^-21.3 of itself (the constant,
