@@ -23,6 +23,12 @@ dllm_status done(cudaError_t e, const char* what, const char* why = nullptr) {
 }
 bool known_dtype(int dtype) { return dtype == DLLM_FP32 || dtype == DLLM_BF16; }
 bool aligned16(const void* p) { return !((uintptr_t)p & 15); }
+// float and int32 arrays, those that are there
+template <typename... P>
+dllm_status check_words(const P*... p) {
+  if (((0 | ... | (uintptr_t)p) & 3) != 0) return fail(DLLM_INVALID_ARG, "an array of float or int32 is not aligned to 4 bytes");
+  return DLLM_OK;
+}
 size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 Launch on(void* stream) { return Launch{(cudaStream_t)stream, kernel_status_word(), nullptr}; }
 
@@ -38,7 +44,7 @@ dllm_status check_product(const void* W, size_t ldw, const float* sw, const void
   if (ldw % 16 || ldw < (size_t)K || !aligned16(W))
     return fail(DLLM_INVALID_ARG, "rows of W must be 16-byte aligned and at least K bytes apart");
   if ((uintptr_t)C % (out_dtype == DLLM_BF16 ? 2 : 4)) return fail(DLLM_INVALID_ARG, "the output is not aligned to its type");
-  return DLLM_OK;
+  return check_words(sw);
 }
 dllm_status check_rows(const void* x, size_t ldx, int dtype, int cols) {
   if (!x || !known_dtype(dtype)) return fail(DLLM_INVALID_ARG, "rows must be fp32 or bf16");
@@ -86,6 +92,7 @@ dllm_status dllm_quantize_rows_s8(const void* d_x, size_t ldx, int dtype, void* 
   if (!d_q || !d_scale || rows <= 0 || cols <= 0) return fail(DLLM_INVALID_ARG, "bad arguments of a row quantisation");
   if (rows > MOST_ROWS || cols > MOST_COLS) return fail(DLLM_UNSUPPORTED, "at most %d rows and columns", MOST_ROWS);
   TRY(check_rows(d_x, ldx, dtype, cols));
+  TRY(check_words(d_scale));
   if (ldq % 16 || ldq < (size_t)cols || !aligned16(d_q))
     return fail(DLLM_INVALID_ARG, "rows of q must be 16-byte aligned and at least `cols` bytes apart");
   return done(launch_quantize_rows_s8(on(stream), d_x, ldx, dtype, (int8_t*)d_q, ldq, d_scale, rows, cols), "row quantisation");
@@ -100,6 +107,7 @@ dllm_status dllm_gemm_s8(const void* d_A, size_t lda, const float* d_sa, const v
                          void* d_C, int out_dtype, int M, int N, int K, void* d_scratch, size_t scratch_bytes, void* stream) {
   if (!d_A || !d_sa) return fail(DLLM_INVALID_ARG, "bad arguments of an 8-bit product");
   TRY(check_product(d_W, ldw, d_sw, d_C, out_dtype, M, N, K));
+  TRY(check_words(d_sa));
   if (lda % 16 || lda < (size_t)K || !aligned16(d_A))
     return fail(DLLM_INVALID_ARG, "rows of A must be 16-byte aligned and at least K bytes apart");
   const GemmPlan plan = plan_gemm_s8(M, N, K);
@@ -147,6 +155,7 @@ dllm_status dllm_kv4_store(const dllm_kv4_cache* cache, const void* d_k, size_t 
   if (!d_pos && (long)start + a > c.cap) return fail(DLLM_INVALID_ARG, "rows %d .. %d do not fit the capacity", start, start + a - 1);
   TRY(check_rows(d_k, ldk, dtype, c.Hkv * c.hd));
   TRY(check_rows(d_v, ldv, dtype, c.Hkv * c.hd));
+  TRY(check_words(d_pos));
   return done(launch_kv4_store(on(stream), c, d_k, d_v, ldk, ldv, dtype, a, d_pos, start), "4-bit store");
 }
 
@@ -158,6 +167,7 @@ dllm_status dllm_kv4_load(const dllm_kv4_cache* cache, int n, const int32_t* d_l
   if (!known_dtype(dtype)) return fail(DLLM_INVALID_ARG, "bad dtype");
   if (((uintptr_t)d_k | (uintptr_t)d_v) % (dtype == DLLM_BF16 ? 2 : 4))
     return fail(DLLM_INVALID_ARG, "the outputs are not aligned to their type");
+  TRY(check_words(d_lens));
   return done(launch_kv4_load(on(stream), c, n, d_lens, d_k, d_v, dtype), "4-bit load");
 }
 
@@ -181,6 +191,7 @@ dllm_status dllm_attention_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache
   TRY(check_cache(cache, &c));
   TRY(check_queries(d_q, ldq, c, a, n, n_heads));
   if (!d_o || !aligned16(d_o)) return fail(DLLM_INVALID_ARG, "the output must be 16-byte aligned");
+  TRY(check_words(d_lse, d_lens));
   const Kv4Plan plan = plan_kv4(c.B, a, n, n_heads, c.Hkv);
   const size_t need = kv4_attention_scratch_bytes(plan, c.B, a, n_heads, c.hd);
   if (need && (!d_scratch || !aligned16(d_scratch) || scratch_bytes < need))
@@ -201,6 +212,7 @@ dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_k
   TRY(check_cache(cache, &c));
   TRY(check_queries(d_q, ldq, c, a, n, n_heads));
   if (!d_lse || !d_weight) return fail(DLLM_INVALID_ARG, "lse or weight is NULL");
+  TRY(check_words(d_lse, d_weight, d_lens));
   const bool umma = plan_kv4_weights(a, n_heads, c.Hkv);
   const size_t need = kv4_weights_scratch_bytes(umma, c.B, a, n_heads, c.Hkv);
   if (need && (!d_scratch || !aligned16(d_scratch) || scratch_bytes < need))
@@ -216,6 +228,7 @@ dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, in
   TRY(check_cache(to, &d));
   if (!d_weight || !d_to_weight || !d_index || !d_to_lens || !aligned16(d_weight))
     return fail(DLLM_INVALID_ARG, "an argument of the eviction is NULL, or its weights are not 16-byte aligned");
+  TRY(check_words(d_lens, d_to_weight, d_index, d_to_lens));
   if (s.B != d.B || s.Hkv != d.Hkv || s.hd != d.hd) return fail(DLLM_INVALID_ARG, "the caches differ in batch, heads or head_dim");
   if (n <= 0 || n > s.cap || keep <= 0 || keep > d.cap || first < 0 || last < 0 || (long)first + last > keep)
     return fail(DLLM_INVALID_ARG, "eviction: n within the capacity, 0 <= first + last <= keep <= the new capacity");

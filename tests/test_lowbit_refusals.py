@@ -134,6 +134,25 @@ def test_evict_into_outputs_that_overlap(dllm):
     refused(dllm, "dllm_kv4_evict", src, P + (1 << 28), 200, 50, 3, 5, None, cache(dllm, cap=64, at=far, v_params=at["k"]), *good.values(), None)
 
 
+def test_arrays_of_words_off_alignment(dllm):
+    """A load from such an address would fault; NULL where it is allowed is none."""
+    c, big = cache(dllm), cache(dllm, at=P + (1 << 30))
+    calls = [("dllm_quantize_rows_s8", (P, 100, 1, P, 112, P, 3, 100, None), (5,)),
+             ("dllm_gemm_s8", (P, 4096, P, P, 4096, P, P, 1, 3, 256, 4096, P, 1 << 30, None), (2, 5)),
+             ("dllm_linear_s8", (P, 4096, 1, P, 4096, P, P, 1, 3, 256, 4096, P, 1 << 30, None), (5,)),
+             ("dllm_kv4_store", (c, P, 512, P, 512, 1, 4, P, 0, None), (7,)),
+             ("dllm_kv4_load", (c, 10, P, P, P, 0, None), (2,)),
+             ("dllm_attention_kv4", (P, 1024, c, P, P, 3, 128, 8, P, P, 1 << 40, None), (4, 8)),
+             ("dllm_attention_weights_kv4", (P, 1024, c, P, P, 3, 128, 8, P, P, 1 << 40, None), (3, 4, 8)),
+             ("dllm_kv4_evict", (c, P + (1 << 28), 100, 50, 0, 0, P + (1 << 29), big, P + (5 << 28), P + (6 << 28), P + (7 << 28), None),
+              (6, 8, 9, 10))]
+    for name, args, words in calls:
+        for w in words:
+            for off in (1, 2):
+                refused(dllm, name, *(x + off if k == w else x for k, x in enumerate(args)))
+                assert "aligned" in dllm.last_error()
+
+
 def test_binding_refuses_what_the_library_cannot_see(dllm):
     import torch
     with pytest.raises(dllm.DllmError):        # no CUDA tensors
