@@ -488,7 +488,11 @@ dllm_status dllm_kv4_load(const dllm_kv4_cache* cache, int n, const int32_t* d_l
  * n_heads]: the natural logarithm of each row's sum of exp(q . k / sqrt(head_dim)).
  * A row without keys gives zeros and -infinity.  Keys from the length on count for
  * nothing whatever stands there.  Scores are as good as fp32 sums over the cache's
- * numbers; weights and values enter the second product in fp16, scaled into its range.
+ * numbers, where the rows are many (the tcgen05 kernel) over numbers that are each off
+ * by up to 2^-31 of the largest offset, or eight steps, among the keys of that sequence
+ * and KV head: keys 2^20 times smaller than the largest get inexact scores.  Weights and
+ * values enter the second product in fp16 (2^-11 of each), scaled by a power of two of
+ * the largest among them: a value 2^-30 of it and a weight 2^-24 of the largest lose bits.
  * d_scratch: as many bytes as the query asks for on the device that is current (NULL
  * where that is 0), 16-byte aligned; calls that may overlap on the GPU need one each. */
 size_t dllm_attention_kv4_scratch_bytes(int B, int a, int n, int n_heads, int n_kv_heads, int head_dim);

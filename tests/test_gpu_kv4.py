@@ -261,6 +261,28 @@ def test_values_near_the_largest_number(dllm, plan, a, hd):
     check_attention(q, cache, a, 1271, 2, None, o, lse)
 
 
+@pytest.mark.parametrize("a", [4, 100])
+@pytest.mark.parametrize("big", [2.0 ** 10, 2.0 ** 16])
+def test_keys_of_very_different_size(dllm, plan, a, big):
+    """A few keys `big` times the others, whose scores under queries with a mean are so low that they count for nothing.  The
+    others' numbers are off by up to 2^-31 of the largest number M in the tcgen05 kernel, so a score by 2^-31 M sum|q| / sqrt(hd)."""
+    g = gen(22)
+    hd, n = 128, 640
+    cache = ref.random_cache(dllm, g, 1, 2, n, hd)
+    cache.k_params[:, :, 100:600:100, 1] = -big       # their offsets; their steps stay as they are
+    q = (1 + torch.randn((a, 4 * hd), generator=g, device="cuda")).bfloat16()
+    assert bool((q.double().reshape(a, 4, hd).sum(-1) > 30).all())
+    o, lse = dllm.attention_kv4(q, cache, a, n, 4)
+    want, wl, oe, se = ref.attention(q, cache, a, n, 4)
+    small = cache.k_params.clone()
+    small[:, :, 100:600:100] = 0
+    _, _, oe, se = ref.attention(q, dllm.KV4Cache.from_tensors(cache.k_codes, small, cache.v_codes, cache.v_params), a, n, 4)   # bounds of the others
+    ds = 2.0 ** -31 * big * q.double().reshape(1, a, 4, hd).abs().sum(-1) / math.sqrt(hd)
+    size = float((16 * cache.v_params[..., 0].abs() + cache.v_params[..., 1].abs()).double().max())
+    assert bool(((lse.double().reshape(wl.shape) - wl).abs() <= se + ds + 2.0 ** -22 * (1 + wl.abs())).all())
+    assert bool(((o.double().reshape(want.shape) - want).abs() <= oe + 2 * ds[..., None] * size + 2.0 ** -8 * 1.01 * want.abs()).all())
+
+
 def offset_cache(dllm, g, B, Hkv, cap, hd):
     """Keys and values whose offsets are some sixty steps: what a score then is made of is the offset times the query's sum."""
     cache = ref.random_cache(dllm, g, B, Hkv, cap, hd)
