@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(256) kv4_load_kernel(Kv4 c, int n, const int32
 }
 
 // ---------------------------------------------------------------- eviction
-constexpr int EV_THREADS = 512, EV_PER = 8, EV_BINS = 256, EV_CLUSTER = 8;
+constexpr int EV_THREADS = 512, EV_UNIT = 8, EV_BINS = 256, EV_CLUSTER = 8;   // EV_UNIT: a CTA's share of the keys is a multiple
 constexpr int EV_SMEM_KEYS = 40 * 1024;   // ordered weights that one CTA keeps
 
 // Order of the weights as unsigned numbers, and back; a NaN comes last (as 0), -0 is 0.  No weight has the largest number.
@@ -503,10 +503,16 @@ cudaError_t launch_kv4_evict(const Launch& L, const Kv4& src, const float* weigh
     return cudaFuncSetAttribute(kv4_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_SMEM_KEYS * 4);
   });
   if (e != cudaSuccess) return e;
-  // eight CTAs per head from 8192 keys on, unless there are CTAs enough
-  const bool alone = n <= 2 * EV_THREADS * EV_PER || heads > 2 * sm_count();
-  const int share = alone ? src.cap : (n + EV_CLUSTER * EV_PER - 1) / (EV_CLUSTER * EV_PER) * EV_PER;
-  const int mine = alone ? (n + EV_PER - 1) / EV_PER * EV_PER : share, in_smem = mine <= EV_SMEM_KEYS;
+  // One CTA per head or a cluster of eight (us, selection and gather of a sixteenth, one / eight):
+  //   up to 8192 keys one, whatever the heads: 32 x 4128 10.0 / 12.0, 32 x 8192 12.6 / 12.4, 148 x 4128 12.1 / 30.5; of few heads with
+  //   most keys eight are ahead by little (8 x 4128 9.8 / 9.7, 8 x 8192 11.4 / 9.6)
+  //   beyond, eight where the heads are few: 8 x 16384 16.8 / 10.2, 32 x 16384 17.6 / 13.7, 48 x 32768 33.7 / 21.9, 64 x 16384 19.2 /
+  //   20.0; one where clusters would come in several rounds: 80 x 16384 21.1 / 25.9, 148 x 16384 30 / 44, 296 x 32768 111 / 129 (between
+  //   75 and 96 heads of 32768 keys eight are still ahead by a tenth)
+  //   more keys than one CTA keeps in shared memory: eight (148 x 41024 95 / 84, 16 x 65536 127 / 20, 600 x 65536 551 / 419)
+  const bool alone = n <= 8192 || (n <= EV_SMEM_KEYS && heads > sm_count() / 2);
+  const int share = alone ? src.cap : (n + EV_CLUSTER * EV_UNIT - 1) / (EV_CLUSTER * EV_UNIT) * EV_UNIT;
+  const int mine = alone ? (n + EV_UNIT - 1) / EV_UNIT * EV_UNIT : share, in_smem = mine <= EV_SMEM_KEYS;
   const size_t smem = in_smem ? (size_t)mine * 4 : 0;
   e = alone ? launch_k(L, kv4_select_kernel, dim3(heads), dim3(EV_THREADS), smem, weight, n, src.cap, src.Hkv, keep, first,
                        last, lens, share, in_smem, dst.cap, dst_weight, index, new_lens)

@@ -637,6 +637,21 @@ def test_evicted_weights_of_minus_zero_are_zero(dllm, n, keep, first, last):
     assert torch.equal(nw[..., :keep].view(torch.int32), (want + 0.0).view(torch.int32))
 
 
+@pytest.mark.parametrize("Hkv,n", [(75, 8256), (74, 8256), (160, 40960), (160, 41024), (700, 8300)])
+def test_evict_on_both_sides_of_the_choice_of_clusters(dllm, Hkv, n):
+    """One CTA per head and a cluster of eight give the same: weights of few values, so that places go by index."""
+    g = gen(n + Hkv)
+    cap, keep = -(-n // 64) * 64, 1000
+    cache = dllm.KV4Cache(1, Hkv, cap, 64)
+    w = torch.randint(0, 40, (1, Hkv, cap), generator=g, device="cuda").float()
+    _, nw, index, new = dllm.kv4_evict(cache, w, n, keep, 3, 5)
+    order = w[..., :n].clone()
+    order[..., :3] = order[..., n - 5:] = 1e9
+    rows = order.sort(dim=-1, descending=True, stable=True).indices[..., :keep].sort(-1).values
+    assert new.tolist() == [keep] and torch.equal(index.long(), rows)
+    assert torch.equal(nw[..., :keep], w.gather(-1, rows))
+
+
 # ---------------------------------------------------------------- as they are used together
 def test_a_prompt_is_cached_scored_and_thinned_out(dllm):
     """Prompt and response rows go into the cache, the response's queries attend and score, half of the prompt leaves, and
