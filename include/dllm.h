@@ -508,11 +508,13 @@ dllm_status dllm_debug_kv4_plan(int kernel, int splits);
 /* What every key gets of the rows' attention: d_weight[b, h, j] (float [B, n_kv_heads,
  * capacity]) += the sum over the a queries and the query heads of KV head h of
  * exp(q . k_j / sqrt(head_dim) - lse), for j below the sequence's length; the other
- * weights stay as they are.  d_lse as dllm_attention_kv4 leaves it; a row whose lse is
- * -infinity gives nothing, whatever it holds (to keys that are numbers).  Sums are taken in a fixed order, and a key's is added whole or, where a
- * wait of the call gave up (DLLM_TIMEOUT), not at all.  d_scratch: as many bytes as
- * the query asks for (NULL where that is 0), 16-byte aligned; calls that may overlap on
- * the GPU need one each. */
+ * weights stay as they are.  Scores are as good as fp32 sums (where the rows are many, a
+ * key's offset, a row's sum and its lse enter as three bf16 parts each, 24 bits), their
+ * exponentials are off by 2^-22.  d_lse as dllm_attention_kv4 leaves it; a row whose lse
+ * is -infinity gives nothing, whatever it holds (to keys that are numbers).  Sums are
+ * taken in a fixed order, and a key's is added whole or, where a wait of the call gave up
+ * (DLLM_TIMEOUT), not at all.  d_scratch: as many bytes as the query asks for (NULL where
+ * that is 0), 16-byte aligned; calls that may overlap on the GPU need one each. */
 size_t dllm_attention_weights_kv4_scratch_bytes(int B, int a, int n_heads, int n_kv_heads);
 dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_kv4_cache* cache, const float* d_lse,
                                        float* d_weight, int a, int n, int n_heads, const int32_t* d_lens, void* d_scratch,
@@ -525,8 +527,11 @@ dllm_status dllm_attention_weights_kv4(const void* d_q, size_t ldq, const dllm_k
  * d_index (int32 [B, n_kv_heads, keep]) says where each came from (-1 behind them) and
  * d_to_lens (int32 [B]) how many stayed.  first + last <= keep <= to->capacity; d_weight
  * 16-byte aligned; nothing that is written may overlap what is read or what else is
- * written.  Positions are in K already (it is cached rotated), so
- * attention over `to` needs nothing but the new lengths. */
+ * written.  Positions are in K already (it is cached rotated), so attention over `to`
+ * needs nothing but the new lengths.  The kept tokens differ from head to head (d_index
+ * says which), and dllm_kv4_store takes one position per token for all heads: afterwards
+ * it can replace the protected first and last rows, at their new places, and append
+ * behind the new length, but no row that was chosen by its weight. */
 dllm_status dllm_kv4_evict(const dllm_kv4_cache* from, const float* d_weight, int n, int keep, int first, int last,
                            const int32_t* d_lens, const dllm_kv4_cache* to, float* d_to_weight, int32_t* d_index,
                            int32_t* d_to_lens, void* stream);

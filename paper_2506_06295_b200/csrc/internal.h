@@ -47,7 +47,11 @@ struct Launch {
 // in the stream is still running, and everything it does before pdl_wait()
 // (set-up, prefetch of weights, which no kernel writes) overlaps the
 // predecessor's tail.  Every kernel of the library calls pdl_wait() before it
-// touches memory another kernel writes or reads.
+// touches memory that a launch it may overlap writes or reads: its predecessor,
+// and where that was launched with the attribute too, that one's.  (The keys'
+// warps of kv4_weights_umma_kernel touch the cache and the weights without it:
+// their launch's predecessor writes the rows' parts alone, and was launched
+// plainly, so everything older is complete.)
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_k(const Launch& L, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
                             Args... args) {

@@ -22,7 +22,8 @@ namespace dllm {
 
 constexpr int KV4_KEYS = 64;  // keys per tile, and what a cache's capacity is a multiple of
 
-// Two codes of a word -> two halves holding u - 8.  LO: nibbles 0 and 4, i.e. bits 0-3 and 16-19; HI: nibbles 1 and 5.
+// Two codes of a word -> two halves holding u - 8, without a conversion: the integer goes into the significand of a power of two
+// (the way Kim et al., arXiv 2211.10017, turn 8- and 4-bit weights into fp16).  LO: nibbles 0 and 4, i.e. bits 0-3 and 16-19; HI: nibbles 1 and 5.
 // 0x6400 is 1024 in fp16, whose last place is 1: or-ing a nibble in adds it (16 times it for the high one).
 __device__ __forceinline__ uint32_t kv4_half_lo(uint32_t w) {
   uint32_t r;

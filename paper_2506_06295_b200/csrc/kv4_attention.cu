@@ -2,7 +2,8 @@
 //
 // kv4_attn_kernel: 16 rows ((query, head of the group) pairs of one KV head) per CTA and split of the key range.  Its four
 // warps take key tiles of 64 in turn, each with a ring of its own that cp.async fills, so no warp waits for another before
-// the end; what they have is merged through shared memory there, splits by kv4_combine_kernel.  In a tile
+// the end; what they have is merged through shared memory there, ranges of keys inside a cluster (two, four or eight) or by
+// kv4_combine_kernel.  In a tile
 //     S = Q v_K^T, O += P~ v_V   mma.sync m16n8k16 on fp16, v = code - 8 made from the codes in registers
 // Q enters as fp16 scaled by a power of two per row (its bf16 mantissas are exact in it; what lies 2^38 below the row's
 // largest element is lost), P~ = p * step_V * 2^x with x from the largest step seen, so that it uses fp16's range: rounding
@@ -480,7 +481,8 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const float* __restric
 }
 
 // ---------------------------------------------------------------- weights
-// At most KW_ROWS rows per KV head: S^T = v_K Q^T with the keys along the rows.  A CTA makes fp16 operands of the rows once, in
+// At most KW_ROWS rows per KV head (what the operand array below holds; the tcgen05 kernel instead: 64 rows of 32 heads x 4128 keys
+// 15.7 here, 16.4 there, 16 sequences of 64 rows x 1536 54 / 70, 32 rows x 4128 10.0 / 15.2): S^T = v_K Q^T with the keys along the rows.  A CTA makes fp16 operands of the rows once, in
 // shared memory; its warps hold 32 keys each in registers and go over the rows, then take the next keys, whose codes are on
 // their way meanwhile.  A key's probabilities add up in its threads' registers (fp32, in the order of the rows), the four
 // threads of a key at the end.  No two CTAs add to the same key.
@@ -625,10 +627,14 @@ std::atomic<int> g_plan_hook{0};   // dllm_debug_kv4_plan: kernel + 4 * splits
 //   few rows   16 rows a CTA, two CTAs to an SM: 4.5 at its ends, and for a tile of 64 keys of each of its four warps 1.5, 2.1
 //              beside a second CTA; 4.5 more where ranges are merged, by a cluster of up to eight as by a launch (which a call's
 //              host side and scratch make the dearer one)
-//   tcgen05    256 rows a CTA, one to an SM: 12 at its ends, 2.3 for a tile of 128 keys, 5 for a merge and its bytes
+//   tcgen05    256 rows a CTA, one to an SM: 12 at its ends, 2.3 for a tile of 128 keys (2.8 with 256 rows and 2.2 with at most 128,
+//              measured over 1 to 64 tiles), 5 for a merge and its bytes
+// Over 485 shapes (1 to 16 sequences, 17 to 4096 rows per KV head, 256 to 32768 keys) the choice of kernel is 0.6 % above the better
+// one's time on the geometric mean, at most 22 % (with the two measured figures per tile 0.45 %, but other ranges: 12 % and 19 % lost
+// on some shapes for 17 % on others).
 // Measured / by this, few rows then tcgen05, each in its best number of ranges:  64 x 768 x 32 heads 8.7 / 9, 17 / 18;
 // 128 x 768 x 32 12.7 / 10.8, 17.8 / 18;  256 x 768 x 32 23 / 22, 24.7 / 26;  512 x 1024 x 32 47 / 52, 33 / 30;  128 x 512 x 28 on 4
-// 10.1 / 8.7, 21 / 21;  100 x 16384 x 8 48 / 43, 32 / 36;  16 sequences of 80 x 1536 x 32 158 / 154, 132 / 158;  8 of 16 x 32768 x
+// 10.1 / 8.7, 21 / 21;  100 x 16384 x 8 48 / 43, 32 / 36;  16 sequences of 80 x 1536 x 32 158 / 154, 131 / 158;  8 of 16 x 32768 x
 // 28 on 4 270 / 273, 155 / 164.
 Kv4Plan plan_kv4(int B, int a, int n, int H, int Hkv) {
   const int hook = g_plan_hook.load(std::memory_order_relaxed), kernel = hook & 3, splits = hook >> 2;
@@ -685,7 +691,8 @@ size_t kv4_weights_scratch_bytes(bool umma, int B, int a, int H, int Hkv) {
 cudaError_t launch_kv4_weights(const Launch& L, bool umma, const void* q, size_t ldq, const Kv4& c, const float* lse, float* weight,
                                int a, int n, int H, const int32_t* lens, void* scratch) {
   if (umma) return launch_kv4_weights_umma(L, q, ldq, c, lse, weight, a, n, H, lens, scratch);
-  // three CTAs to an SM, each over its share of the keys
+  // Three CTAs to an SM, each over its share of the keys (two / three / four, us: 32 rows of 32 heads x 4128 keys 10.5 / 10.0 / 9.7, 4
+  // sequences of 28 rows of 4 heads x 16384 16.8 / 15.0 / 13.2, 8 of 32 rows of 8 heads x 32768 116 / 98 / 107)
   const long blocks = (n + KW_KEYS - 1) / KW_KEYS, heads = (long)c.Hkv * c.B;
   const dim3 grid((unsigned)std::max(1L, std::min(blocks, (3L * sm_count() + heads - 1) / heads)), c.Hkv, c.B);
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)c.hd);

@@ -450,7 +450,10 @@ __global__ void __launch_bounds__(256) kv4_gather_kernel(Kv4 src, Kv4 dst, const
 template <typename T, int HD>
 cudaError_t store_as(const Launch& L, const Kv4& c, const T* k, const T* v, size_t ldk, size_t ldv, int a, const int32_t* pos,
                      int start) {
-  // five CTAs to an SM; enough of them that a last round of a few costs little
+  // Rows a CTA: few where there are few, so that all SMs have some; with positions more, which looks through fewer of the rows behind
+  // (1 / 2 / 4 / 8 / 16 / 32 rows, us: 64 scattered rows of 32 heads 3.3 / 4.5 / 6.9 / 11 / 20 / 37; 16 x 1536 in place 122 / 112 / 108 /
+  // 106 / 111 / 126, scattered 166 / 138 / 124 / 120 / 128 / 155; 32768 in place of 4 heads 126 / 65 / 35 / 21 / 20 / 20, scattered 730 /
+  // 416 / 280 / 267 / 355 / 600: the look through the positions grows with the square of a sequence's rows)
   const int rows = c.B * a, per = std::max(1, std::min(pos ? ST_ROWS : 4, rows / (16 * sm_count())));
   const bool vec = !(((uintptr_t)k | (uintptr_t)v) & 15) && !((ldk | ldv) * sizeof(T) & 15);
   const dim3 grid((rows + per - 1) / per);
