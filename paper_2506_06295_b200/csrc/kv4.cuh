@@ -51,6 +51,33 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 2^x on the special-function unit, 2^-22 off
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+// Operand rows of sixteen 16-bit numbers: 32 bytes with the 32-byte swizzle, K-major, 8-row groups 256 bytes apart.  The
+// descriptor, and the place of a row's first or second 16 bytes.
+__device__ __forceinline__ uint64_t make_smem_desc_32(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)6 << 61);
+}
+__device__ __forceinline__ uint32_t chunk_32(uint32_t base, int row, int chunk) {
+  return base + row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4);
+}
 __device__ __forceinline__ float kv4_step(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float kv4_lo(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
 

@@ -27,20 +27,6 @@ constexpr int KA_THREADS = 128, KA_ROWS = 16, KA_STAGES = 3, KA_CLUSTER = 8;
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 // Power of two that brings a number with exponent field `ex` to [2^13, 2^14), and its inverse.  Fields below 20 count as 20.
 __device__ __forceinline__ float kv4_up(int ex) { return __uint_as_float((uint32_t)(267 - max(ex, 20)) << 23); }
 __device__ __forceinline__ float kv4_down(int ex) { return __uint_as_float((uint32_t)(max(ex, 20) - 13) << 23); }
@@ -251,7 +237,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
       top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
       top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 2));
       const float now = fmaxf(m[h], top[h]);
-      corr[h] = now == m[h] ? 1.f : exp2_fast(m[h] - now);
+      corr[h] = now == m[h] ? 1.f : exp2_approx(m[h] - now);
       same = same && now == m[h];
       m[h] = now;
     }
@@ -277,7 +263,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
       const float4 v = par[2 * (nt * 4 + t) + 1];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float2 e = add2(make_float2(s[nt][2 * h], s[nt][2 * h + 1]), ref[h]), p = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+        const float2 e = add2(make_float2(s[nt][2 * h], s[nt][2 * h + 1]), ref[h]), p = make_float2(exp2_approx(e.x), exp2_approx(e.y));
         l[h] = add2(l[h], p);
         z[h] = fma2(p, make_float2(v.z, v.w), z[h]);
         const float2 w = mul2(p, make_float2(v.x, v.y));
@@ -351,7 +337,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
     for (int e = 0; e < PER; ++e) out[e] = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = exp2_fast(x_m[w][r] - ref);
+      const float f = exp2_approx(x_m[w][r] - ref);
       const float* x = reinterpret_cast<const float*>(smem + w * SM::WARP) + r * SM::XS + col;
       sum = fmaf(f, x_l[w][r], sum);
 #pragma unroll
@@ -392,7 +378,7 @@ __global__ void __launch_bounds__(KA_THREADS) kv4_attn_kernel(const __nv_bfloat1
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < KA_CLUSTER; ++k) {
-        const float f = exp2_fast(ml[k].x - ref);
+        const float f = exp2_approx(ml[k].x - ref);
         l2 = fmaf(f, ml[k].y, l2);
         y.x = fmaf(f, x[k].x, y.x); y.y = fmaf(f, x[k].y, y.y); y.z = fmaf(f, x[k].z, y.z); y.w = fmaf(f, x[k].w, y.w);
       }
@@ -445,7 +431,7 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const float* __restric
   for (int k = 0; k < 2; ++k)
     ml[k] = lane + 32 * k < S ? __ldcg(&ml_part[(size_t)(lane + 32 * k) * total + row]) : make_float2(-INFINITY, 0.f);
   const float top = warp_max(fmaxf(ml[0].x, ml[1].x));
-  const float ref = top == -INFINITY ? 0.f : top, f0 = exp2_fast(ml[0].x - ref), f1 = exp2_fast(ml[1].x - ref);
+  const float ref = top == -INFINITY ? 0.f : top, f0 = exp2_approx(ml[0].x - ref), f1 = exp2_approx(ml[1].x - ref);
   const float sum = warp_sum(fmaf(f0, ml[0].y, f1 * ml[1].y));
   float out[PER];
 #pragma unroll
@@ -481,11 +467,12 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(const float* __restric
 }
 
 // ---------------------------------------------------------------- weights
-// At most KW_ROWS rows per KV head (what the operand array below holds; the tcgen05 kernel instead: 64 rows of 32 heads x 4128 keys
-// 15.7 here, 16.4 there, 16 sequences of 64 rows x 1536 54 / 70, 32 rows x 4128 10.0 / 15.2): S^T = v_K Q^T with the keys along the rows.  A CTA makes fp16 operands of the rows once, in
+// At most KW_ROWS rows per KV head: S^T = v_K Q^T with the keys along the rows.  A CTA makes fp16 operands of the rows once, in
 // shared memory; its warps hold 32 keys each in registers and go over the rows, then take the next keys, whose codes are on
 // their way meanwhile.  A key's probabilities add up in its threads' registers (fp32, in the order of the rows), the four
 // threads of a key at the end.  No two CTAs add to the same key.
+// KW_ROWS is what the operand array holds; up to there this kernel is ahead of the tcgen05 one (us, here / there: 64 rows of 32 heads
+// x 4128 keys 15.7 / 16.4, 32 rows 10.0 / 15.2, 16 sequences of 64 rows x 1536 54 / 70, 64 rows of one head x 32768 6.1 / 8.1).
 constexpr int KW_KEYS = 128, KW_ROWS = KV4_WEIGHTS_ROWS;
 template <int HD>
 __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* __restrict__ q, size_t ldq, Kv4 c,
@@ -575,7 +562,7 @@ __global__ void __launch_bounds__(128) kv4_weights_kernel(const __nv_bfloat16* _
         const float4 p = par[nt * 8 + 2 * t + e];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          got[i] += exp2_fast(fmaf(s[i >> 1][2 * (i & 1) + e] * p.x, step[i], fmaf(off[i], p.y, -p.z)));
+          got[i] += exp2_approx(fmaf(s[i >> 1][2 * (i & 1) + e] * p.x, step[i], fmaf(off[i], p.y, -p.z)));
       }
     }
 #pragma unroll

@@ -36,16 +36,6 @@ constexpr int UK_ROWS = 128, UK_KEYS = 2 * KV4_KEYS, UK_STAGES = 2, UK_THREADS =
 constexpr int UK_P_BITS = 10;   // P = p * 2^10: fp16's small numbers are further away
 
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
 // 16 columns; the caller waits for the stores (tcgen05.wait::st)
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -58,24 +48,9 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool mn) {
   return (1u << 4) | ((mn ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 __device__ __forceinline__ __half2 as_half2(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
 __device__ __forceinline__ uint32_t as_u32(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
-__device__ __forceinline__ void st_shared16(uint32_t addr, uint4 v) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
 
-// Sixteen fp16 per row (32 bytes, 32-byte swizzle: K-major, 8-row groups 256 bytes apart)
-__device__ __forceinline__ uint64_t make_smem_desc_32(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) |
-         ((uint64_t)6 << 61);
-}
-__device__ __forceinline__ uint32_t chunk_32(uint32_t base, int row, int chunk) {
-  return base + row * 32 + ((chunk ^ ((row >> 2) & 1)) << 4);
-}
 template <int HD>
 struct UkSmem {
   // per stage K', V, and the offsets' sixteen elements per key
@@ -236,7 +211,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         }
         if (!OF_V && qd == 0) {   // beside the sum's parts (h, m, l, h, m, l, 0 ..): lo three times, 8 step three times
           const float lo1 = lo * 256.f, s8 = step * 2048.f;
-          st_shared16(chunk_32(stage + 2 * SM::TILE, r, 0), make_uint4(pack_half(lo1, lo1), pack_half(lo1, s8), pack_half(s8, s8), 0u));
+          st_shared16(chunk_32(stage + 2 * SM::TILE, r, 0), make_uint4(half_pair(lo1, lo1), half_pair(lo1, s8), half_pair(s8, s8), 0u));
           st_shared16(chunk_32(stage + 2 * SM::TILE, r, 1), make_uint4(0u, 0u, 0u, 0u));
         }
       }
@@ -340,8 +315,8 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         uint32_t r[4];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          r[2 * k] = pack_half(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k + 2] << 16) * up);
-          r[2 * k + 1] = pack_half(__uint_as_float(u[k] & 0xFFFF0000u) * up, __uint_as_float(u[k + 2] & 0xFFFF0000u) * up);
+          r[2 * k] = half_pair(__uint_as_float(u[k] << 16) * up, __uint_as_float(u[k + 2] << 16) * up);
+          r[2 * k + 1] = half_pair(__uint_as_float(u[k] & 0xFFFF0000u) * up, __uint_as_float(u[k + 2] & 0xFFFF0000u) * up);
         }
         st_shared16(q_s + i * SM::Q + (w >> 3) * (UK_ROWS * 128) + row * 128 + (((w & 7) ^ (row & 7)) << 4),
                     make_uint4(r[0], r[1], r[2], r[3]));
@@ -349,7 +324,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
       // the sum's three parts, 2^-8 of Q's scale (the offsets beside them have 2^8 of K's)
       const float v = sum * up * 0.00390625f;
       const float h = __half2float(__float2half_rn(v)), m = __half2float(__float2half_rn(v - h)), l = v - h - m;
-      st_shared16(chunk_32(sum_s + i * SM::SUM, row, 0), make_uint4(pack_half(h, m), pack_half(l, h), pack_half(m, l), 0u));
+      st_shared16(chunk_32(sum_s + i * SM::SUM, row, 0), make_uint4(half_pair(h, m), half_pair(l, h), half_pair(m, l), 0u));
       st_shared16(chunk_32(sum_s + i * SM::SUM, row, 1), make_uint4(0u, 0u, 0u, 0u));
       scale = scale_log2 * pow2(f - 140);   // K's part follows when it is known
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -393,7 +368,7 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
         const float mx = max3(fmaxf(most[0], most[1]), most[2], most[3]) * scale;   // scale > 0
         const bool grow = mx > m_ref + RESCALE_STEP;
         if (__any_sync(0xffffffffu, grow)) {
-          const float corr = grow ? ex2(m_ref - mx) : 1.f;
+          const float corr = grow ? exp2_approx(m_ref - mx) : 1.f;
           if (grow) m_ref = mx;
           l2.x *= corr;
           l2.y *= corr;
@@ -417,9 +392,9 @@ __global__ void __launch_bounds__(UK_THREADS, 1)
           scores(part, r);
 #pragma unroll
           for (int jj = 0; jj < 16; ++jj) {
-            const float2 e = fma2(make_float2(__uint_as_float(r[2 * jj]), __uint_as_float(r[2 * jj + 1])), scale2, ref2), p = make_float2(ex2(e.x), ex2(e.y));
+            const float2 e = fma2(make_float2(__uint_as_float(r[2 * jj]), __uint_as_float(r[2 * jj + 1])), scale2, ref2), p = make_float2(exp2_approx(e.x), exp2_approx(e.y));
             l2 = add2(l2, p);
-            pk[jj] = pack_half(p.x, p.y);
+            pk[jj] = half_pair(p.x, p.y);
           }
           tmem_st16(s_col + (uint32_t)(part * 16), pk);
         }

@@ -39,11 +39,6 @@ static __device__ int g_debug_skip = 0;
 constexpr int WK_TILE = 128, WK_KEYS = 2 * WK_TILE, WK_ROWS = 128, WK_STAGES = 2, WK_THREADS = 18 * 32, WK_MMA_WARP = 16,
               WK_Q_WARP = 17, WK_CLUSTER = 8;
 
-__device__ __forceinline__ float exp2_sfu(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // 2^x of two numbers on the FMA pipe: x split into an integer and the rest f of -1/2 .. 1/2, on which 1 + f P(f), P of degree 4,
 // stands for 2^f.  P: least largest relative error with the constant held at 1 (Remez exchange, then the coefficients rounded to
 // fp32 from the lowest on, the others fitted again each time): 2^-23.3 off, -1.7e-8 on average, 2^-22.6 with fp32's roundings.  (The
@@ -65,9 +60,6 @@ __device__ __forceinline__ float2 exp2_fma(float2 x) {
   return mul2(p, make_float2(__uint_as_float((__float_as_uint(r.x) << 23) + 0x3F800000u),
                              __uint_as_float((__float_as_uint(r.y) << 23) + 0x3F800000u)));
 }
-__device__ __forceinline__ void put16(uint32_t addr, uint4 v) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -78,15 +70,9 @@ __device__ __forceinline__ void parts3(float x, float (&p)[3]) {
   p[1] = __bfloat162float(__float2bfloat16_rn(x - p[0]));
   p[2] = x - p[0] - p[1];
 }
-// Sixteen bf16 per row: 32 bytes with the 32-byte swizzle, 8-row groups 256 bytes apart.
-__device__ __forceinline__ uint64_t desc_rows32(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(256 >> 4) << 32) | ((uint64_t)1 << 46) |
-         ((uint64_t)6 << 61);
-}
 __device__ __forceinline__ void put_rows32(uint32_t base, int row, uint4 lo, uint4 hi) {
-  const uint32_t turn = (uint32_t)((row >> 2) & 1) << 4;
-  put16(base + row * 32 + turn, lo);
-  put16(base + row * 32 + (16u ^ turn), hi);
+  st_shared16(chunk_32(base, row, 0), lo);
+  st_shared16(chunk_32(base, row, 1), hi);
 }
 
 // The rows of a KV head in tiles of 128: heads of `queries` queries, gbox of the G heads each, so that a tile is a box of the
@@ -204,7 +190,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
   const int used = til.queries * til.gbox;
   for (int i = tid; i < WK_STAGES * (HD / 64) * (WK_ROWS - used) * 8; i += WK_THREADS) {
     const int ch = i & 7, r = (i >> 3) % (WK_ROWS - used), part = (i >> 3) / (WK_ROWS - used);
-    put16(ring + (part / (HD / 64)) * SM::STAGE + (part % (HD / 64)) * (WK_ROWS * 128) + (used + r) * 128 + ch * 16, make_uint4(0, 0, 0, 0));
+    st_shared16(ring + (part / (HD / 64)) * SM::STAGE + (part % (HD / 64)) * (WK_ROWS * 128) + (used + r) * 128 + ch * 16, make_uint4(0, 0, 0, 0));
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   if (warp == WK_MMA_WARP) {
@@ -295,7 +281,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
         if (none[k])
 #pragma unroll 1
           for (int ch = 0; ch < HD / 8; ++ch)
-            put16(stage + (ch >> 3) * (WK_ROWS * 128) + (k * 32 + lane) * 128 + (ch & 7) * 16, make_uint4(0, 0, 0, 0));
+            st_shared16(stage + (ch >> 3) * (WK_ROWS * 128) + (k * 32 + lane) * 128 + (ch & 7) * 16, make_uint4(0, 0, 0, 0));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor cores read them
       __syncwarp();
     };
@@ -319,7 +305,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
               const uint64_t off = (uint64_t)(((ks >> 2) * (128 * 128) + (ks & 3) * 32) >> 4);
               umma_bf16(d, dk + off, dq + off, idesc, ks > 0 ? 1u : 0u);
             }
-            umma_bf16(d, desc_rows32(keys + SM::OPERAND), desc_rows32(row + SM::OPERAND), idesc, 1u);
+            umma_bf16(d, make_smem_desc_32(keys + SM::OPERAND), make_smem_desc_32(row + SM::OPERAND), idesc, 1u);
             umma_commit(smem_u32(&d_full[i][buf]));
           }
           __syncwarp();
@@ -367,7 +353,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
             p[e] = *reinterpret_cast<const uint32_t*>(&h);
           }
           const int chunk = (half * MINE + k) * 4 + jj;
-          put16(to + (chunk >> 3) * (WK_TILE * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), make_uint4(p[0], p[1], p[2], p[3]));
+          st_shared16(to + (chunk >> 3) * (WK_TILE * 128) + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), make_uint4(p[0], p[1], p[2], p[3]));
         }
       }
       if (half == 0) {
@@ -420,7 +406,7 @@ __global__ void __launch_bounds__(WK_THREADS, 1)
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const float2 y = mul2(make_float2(__uint_as_float(r[e]), __uint_as_float(r[e + 1])), make_float2(mul, mul));
-            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], (e >> 1) % 4 == 3 ? exp2_fma(y) : make_float2(exp2_sfu(y.x), exp2_sfu(y.y)));
+            sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], (e >> 1) % 4 == 3 ? exp2_fma(y) : make_float2(exp2_approx(y.x), exp2_approx(y.y)));
           }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
